@@ -72,13 +72,17 @@ enum {
 enum {
     READER_STATUS_BAD_TREE = 1, /* parents[b][0] != -1 or parents[b][i] not in [0, i) */
     READER_STATUS_BAD_PAGE = 2, /* a page id outside [0, num_pages) was met */
-    READER_STATUS_BAD_PATH = 4  /* accept_len/path entry out of range, or path longer than max_path */
+    READER_STATUS_BAD_PATH = 4, /* accept_len/path entry out of range, or path longer than max_path */
+    READER_STATUS_BAD_LENGTH = 8 /* a length, packed bound or position that the tensors, the page table or a table of positions do not hold */
 };
 
 enum {
     READER_MAX_T = 128,  /* draft-tree nodes per sequence */
     READER_PAGE_SIZE = 16,
-    READER_MAX_B = 4096  /* sequences per call (what the in-kernel prefix scan over the lengths is sized for) */
+    READER_MAX_B = 4096, /* sequences per call (what the in-kernel prefix scan over the lengths is sized for) */
+    READER_MAX_WINDOW = 65536,          /* query tokens per sequence of reader_prompt_key_weights */
+    READER_MAX_EVICT_UNITS = 1 << 20,   /* (layer, sequence, kv head) triples of reader_kv_evict */
+    READER_MAX_TOKENS = 1 << 25         /* rows of a packed batch */
 };
 
 /* Problem sizes; plain data, passed by const pointer (host memory). */
@@ -553,6 +557,164 @@ enum {
     READER_TUNE_COUNT_ = 9
 };
 int reader_tuning_override(int32_t which, int32_t value);
+
+/*
+ * ------------------------------------------------------------------ around the verification step
+ * A program fills the paged cache from its prompts, decodes over it, and may keep it within a budget.
+ *
+ * Packed prompts: the new tokens of all sequences are rows of one tensor, sequence b's are rows
+ * cu_tokens[b] .. cu_tokens[b + 1] - 1 (i32 [B + 1], not decreasing, cu_tokens[0] >= 0, cu_tokens[B] <= N); rows
+ * behind the last sequence are padding and stay as they were.  A sequence may have no new tokens.  Their keys and
+ * values go behind the seq_lens[b] positions that the cache holds (as a draft tree's do in the in-cache layout);
+ * every layer's calls see the same seq_lens, and the caller adds the new tokens to it after the last layer.
+ *
+ * Rotation table: f32 [max_positions, rot_dims], row `pos` holds rot_dims / 2 cosines and then as many sines of that
+ * position's angles (made by the caller, in 64 bits for far positions).  The first rot_dims values of a head are
+ * turned (rot_dims a multiple of 16, 0: none), pair i by angle i: values i and i + rot_dims / 2, or with
+ * `interleaved` values 2 i and 2 i + 1:  (a, b) -> (a cos - b sin, b cos + a sin).
+ *
+ * Norm weights: bf16 [D], or both NULL: no norm.  y = w * x / sqrt(mean(x^2) + eps) over the D values of each head, in
+ * front of the rotation.  eps in [0, 1].  fp32 throughout, one rounding to nearest even at the end; values of heads
+ * that nothing is done to, and v, keep their bits.
+ */
+
+/*
+ * Queries, keys and values of a draft tree's nodes from their projections, as reader_tree_attn and reader_verify_step
+ * take them.  The position of a node is the root's plus the node's depth.
+ *
+ *   qkv          bf16 [B, T, Hq + 2 Hkv, D]   in   query heads, key heads, value heads
+ *   parents      i32 [B, T]                   in
+ *   seq_lens     i32 [B]                      in   cached positions: the root's position, unless `positions` is given
+ *   positions    i32 [B] or NULL              in   position of the root (a cache that rows were evicted from is shorter
+ *                                                  than the text)
+ *   q_norm, k_norm  bf16 [D], both or neither in
+ *   cos_sin      f32 [max_positions, rot_dims] in  (may be NULL if rot_dims is 0)
+ *   q            bf16 [B, T, Hq, D]           out
+ *   k_tree, v_tree  bf16 [B, T, Hkv, D]       out  or both NULL: the in-cache layout, node n at cache position
+ *                                                  seq_lens[b] + n of
+ *   k_cache, v_cache  bf16 [num_pages, Hkv, page_size, D]  out, page_table i32 [B, max_pages_per_seq] in (else unused)
+ *   status       i32 [1] or NULL              in/out
+ *
+ * A bad link counts as a link to the root (READER_STATUS_BAD_TREE).  A node whose position the rotation table does not
+ * hold is left out (READER_STATUS_BAD_LENGTH); one that the page table does not hold (BAD_LENGTH) or whose page id is out of
+ * range (BAD_PAGE) gets its q but no K/V rows.  dims->sm_scale and max_path are not used.  One launch.
+ */
+int reader_tree_qkv(const reader_dims *dims, const void *qkv, const int32_t *parents, const int32_t *seq_lens,
+                    const int32_t *positions, const void *q_norm, const void *k_norm, float eps,
+                    const float *cos_sin, int32_t max_positions, int32_t rot_dims, int32_t interleaved,
+                    void *q, void *k_tree, void *v_tree, void *k_cache, void *v_cache,
+                    const int32_t *page_table, int32_t *status, void *stream);
+
+/*
+ * The same for packed prompts: row t of sequence b, its i-th new token, has position seq_lens[b] + i (positions[b] + i if
+ * `positions` is given) and its K/V rows go to cache position seq_lens[b] + i.
+ *
+ *   qkv          bf16 [N, Hq + 2 Hkv, D]      in
+ *   cu_tokens    i32 [B + 1]                  in
+ *   q            bf16 [N, Hq, D]              out
+ *   k_cache, v_cache  bf16 [num_pages, Hkv, page_size, D]  out
+ * The rest as above; dims->T and max_path have to be valid and are not used.  One launch.
+ */
+int reader_prompt_qkv(const reader_dims *dims, int32_t N, const void *qkv, const int32_t *cu_tokens,
+                      const int32_t *seq_lens, const int32_t *positions, const void *q_norm, const void *k_norm,
+                      float eps, const float *cos_sin, int32_t max_positions, int32_t rot_dims, int32_t interleaved,
+                      void *q, void *k_cache, void *v_cache, const int32_t *page_table, int32_t *status, void *stream);
+
+/*
+ * Causal attention of packed prompts over the paged cache: whole prompts (seq_lens[b] = 0), the next chunk of longer
+ * ones, single tokens, or all of them in one call.  The i-th new token of sequence b attends to cache positions
+ * 0 .. seq_lens[b] + i, its own among them (the keys and values of the new tokens are in the cache already):
+ *     out[t, hq, :] = sum_j softmax_j( sm_scale * <q[t, hq, :], k_j> ) * v_j
+ *
+ *   q            bf16 [N, Hq, D]                            in
+ *   k_cache, v_cache  bf16 [num_pages, Hkv, page_size, D]   in
+ *   page_table   i32 [B, max_pages_per_seq]                 in   must map pages for [0, seq_lens[b] + new tokens)
+ *   cu_tokens    i32 [B + 1], seq_lens i32 [B]              in
+ *   out          bf16 [N, Hq, D]                            out  fp32 accumulation, rounded to nearest even
+ *   lse          f32 [N, Hq] or NULL                        out  natural-log sum of exp of the scaled scores
+ *   max_seq_len  upper bound of seq_lens[b] + new tokens; keys at or behind it are left out and
+ *                READER_STATUS_BAD_LENGTH is set.  max_pages_per_seq * page_size >= max_seq_len
+ *   workspace    >= reader_prompt_workspace_bytes(dims, N, max_seq_len) bytes, 256-byte aligned; its contents are
+ *                meaningless between calls, calls that are ordered on one stream may share it
+ *   status       i32 [1] or NULL                            in/out
+ *
+ * Keys behind a page id out of range are left out (READER_STATUS_BAD_PAGE); a row that sees no key at all gives
+ * zeros and a log-sum-exp of -inf.  What a masked position holds, a NaN or an infinity too, does not reach the row.
+ * Softmax weights are rounded to bf16 before they multiply V.  dims->variant = 1 is the plain kernel (one wavefront per
+ * row, no workspace).  dims->T and max_path have to be valid and are not used.
+ */
+size_t reader_prompt_workspace_bytes(const reader_dims *dims, int32_t N, int32_t max_seq_len);
+int reader_prompt_attn(const reader_dims *dims, int32_t N, const void *q, const void *k_cache, const void *v_cache,
+                       const int32_t *page_table, const int32_t *cu_tokens, const int32_t *seq_lens,
+                       void *out, float *lse, int32_t max_seq_len, void *workspace, size_t workspace_bytes,
+                       int32_t *status, void *stream);
+
+/*
+ * Attention weight that every cached key has drawn, accumulated per kv head over the queries of committed tokens:
+ *     weights[b, hkv, j] = decay * weights[b, hkv, j] + sum_{t, g} exp(sm_scale * <q[t, hkv G + g, :], k_j> - lse[t, hkv G + g])
+ * over the query tokens t that see key j.  decay = 0 starts afresh: the old contents are not read, and positions behind
+ * the last key get zero up to max_positions.  Otherwise those stay as they are: they have to be zero, as eviction and a
+ * fresh start leave them, for the keys that come to live there.
+ *
+ * After a verification step: the query tokens are the accepted path, whose rows reader_kv_compact (or
+ * reader_verify_step) has appended: seq_lens is the new length, and node path[b][j] sits at position
+ * seq_lens[b] - (accept_len[b] + 1) + j and sees what lies in front of it and itself.
+ *
+ *   q            bf16 [B, T, Hq, D]                 in   as given to the attention
+ *   lse          f32 [B, Hq, T]                     in   as the attention left it
+ *   path         i32 [B, max_path], accept_len i32 [B]   in
+ *   k_cache      bf16 [num_pages, Hkv, page_size, D]     in
+ *   page_table   i32 [B, max_pages_per_seq], seq_lens i32 [B]   in
+ *   weights      f32 [B, Hkv, max_positions]        in/out
+ *   max_seq_len  upper bound of seq_lens[b]
+ *   status       i32 [1] or NULL                    in/out
+ *
+ * A sequence with an accept_len or path entry out of range (READER_STATUS_BAD_PATH), or longer than max_seq_len,
+ * max_positions or its pages (BAD_LENGTH), is left as it is.  A key behind a page id out of range draws nothing
+ * (BAD_PAGE).  No atomics: the same inputs give the same bits.  One launch.
+ */
+int reader_key_weights(const reader_dims *dims, const void *q, const float *lse, const int32_t *path,
+                       const int32_t *accept_len, const void *k_cache, const int32_t *page_table,
+                       const int32_t *seq_lens, float decay, float *weights, int32_t max_positions,
+                       int32_t max_seq_len, int32_t *status, void *stream);
+
+/*
+ * The same behind a prompt: the query tokens are the last `window` (0..READER_MAX_WINDOW) new tokens of every sequence, all
+ * of them where there are fewer.  q bf16 [N, Hq, D], lse f32 [N, Hq] and seq_lens (in front of the new tokens) as for
+ * reader_prompt_attn; max_seq_len bounds seq_lens[b] + new tokens.  A sequence whose packed bounds are out of order or of
+ * range is left as it is (READER_STATUS_BAD_LENGTH).
+ */
+int reader_prompt_key_weights(const reader_dims *dims, int32_t N, const void *q, const float *lse,
+                              const int32_t *cu_tokens, int32_t window, const void *k_cache,
+                              const int32_t *page_table, const int32_t *seq_lens, float decay, float *weights,
+                              int32_t max_positions, int32_t max_seq_len, int32_t *status, void *stream);
+
+/*
+ * Eviction from the cache by accumulated attention weight, all layers in one call.  In every sequence longer than `keep`,
+ * each (layer, kv head) keeps `keep` rows: the newest `recent` positions, and of the others the heaviest, the lowest
+ * position first among equal weights (a NaN is lighter than any number).  The kept rows of K and V, and their weights,
+ * move to positions 0 .. keep - 1 in their order, in place; weights of the freed positions become zero; seq_lens[b] =
+ * keep.  Rows at and behind the new length hold what is left there.  Other sequences are not touched.  What a head keeps
+ * is its own affair: rows carry their rotation with them, and the positions of later tokens are the caller's to count on
+ * (`positions` of reader_tree_qkv and reader_prompt_qkv).  Pages of an evicted sequence must not be shared with another.
+ *
+ *   num_layers   >= 1
+ *   keep, recent  0 <= recent <= keep
+ *   k_cache, v_cache  bf16 [num_layers, num_pages, Hkv, page_size, D]   in/out
+ *   page_table   i32 [B, max_pages_per_seq], seq_lens i32 [B] (in/out)
+ *   weights      f32 [num_layers, B, Hkv, max_positions]                in/out
+ *   workspace    >= reader_kv_evict_workspace_bytes(dims, num_layers, keep) bytes, 4-byte aligned
+ *   status       i32 [1] or NULL                                        in/out
+ *
+ * A sequence that is longer than max_positions or its pages (READER_STATUS_BAD_LENGTH), or has a page id out of range
+ * (BAD_PAGE), is left as it is.  Bit-exact copy.  At most READER_MAX_EVICT_UNITS (layer, sequence, kv head) triples.
+ * dims->Hq, T, max_path and sm_scale are not used.
+ */
+size_t reader_kv_evict_workspace_bytes(const reader_dims *dims, int32_t num_layers, int32_t keep);
+int reader_kv_evict(const reader_dims *dims, int32_t num_layers, int32_t keep, int32_t recent,
+                    void *k_cache, void *v_cache, const int32_t *page_table, int32_t *seq_lens,
+                    float *weights, int32_t max_positions, void *workspace, size_t workspace_bytes,
+                    int32_t *status, void *stream);
 
 #ifdef __cplusplus
 }

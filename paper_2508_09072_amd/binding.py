@@ -27,12 +27,15 @@ READER_EHIP = -4
 STATUS_BAD_TREE = 1
 STATUS_BAD_PAGE = 2
 STATUS_BAD_PATH = 4
+STATUS_BAD_LENGTH = 8
 TUNE_ATTN_ROWS, TUNE_ATTN_RANGES, TUNE_ATTN_PAIR_COST, TUNE_ATTN_AXIS64, TUNE_ATTN_WIDE, TUNE_ATTN_PAIR_FRONT, TUNE_ATTN_SHORT, TUNE_JOIN, TUNE_JOIN_SPREAD = 0, 1, 2, 3, 4, 5, 6, 7, 8
 
 EXPORTS = (
     "reader_version", "reader_strerror", "reader_last_error_detail", "reader_validate_tree", "reader_workspace_bytes",
     "reader_tree_attn", "reader_tree_attn_noalloc", "reader_accept_path", "reader_kv_compact", "reader_verify_step",
     "reader_kv_rearrange_scratch_bytes", "reader_kv_rearrange", "reader_target_argmax", "reader_target_sample", "reader_kv_compact_layers",
+    "reader_tree_qkv", "reader_prompt_qkv", "reader_prompt_workspace_bytes", "reader_prompt_attn", "reader_key_weights",
+    "reader_prompt_key_weights", "reader_kv_evict_workspace_bytes", "reader_kv_evict",
     "reader_trie_create", "reader_trie_destroy", "reader_trie_nodes", "reader_trie_insert", "reader_trie_search_path",
     "reader_trie_extract_tree", "reader_tree_attach_path", "reader_self_repetition", "reader_tree_prune_order",
     "reader_tree_select",
@@ -146,6 +149,23 @@ def load():
     lib.reader_kv_compact_layers.argtypes = [ctypes.POINTER(ReaderDims), i32, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.reader_target_sample.restype = ctypes.c_int
     lib.reader_target_sample.argtypes = [i32, i32, i32, vp, vp, vp, ctypes.c_float, vp, vp]
+    f32, sz = ctypes.c_float, ctypes.c_size_t
+    lib.reader_tree_qkv.restype = ctypes.c_int
+    lib.reader_tree_qkv.argtypes = [dp] + [vp] * 6 + [f32, vp, i32, i32, i32] + [vp] * 8
+    lib.reader_prompt_qkv.restype = ctypes.c_int
+    lib.reader_prompt_qkv.argtypes = [dp, i32] + [vp] * 6 + [f32, vp, i32, i32, i32] + [vp] * 6
+    lib.reader_prompt_workspace_bytes.restype = sz
+    lib.reader_prompt_workspace_bytes.argtypes = [dp, i32, i32]
+    lib.reader_prompt_attn.restype = ctypes.c_int
+    lib.reader_prompt_attn.argtypes = [dp, i32] + [vp] * 8 + [i32, vp, sz, vp, vp]
+    lib.reader_key_weights.restype = ctypes.c_int
+    lib.reader_key_weights.argtypes = [dp] + [vp] * 7 + [f32, vp, i32, i32, vp, vp]
+    lib.reader_prompt_key_weights.restype = ctypes.c_int
+    lib.reader_prompt_key_weights.argtypes = [dp, i32, vp, vp, vp, i32, vp, vp, vp, f32, vp, i32, i32, vp, vp]
+    lib.reader_kv_evict_workspace_bytes.restype = sz
+    lib.reader_kv_evict_workspace_bytes.argtypes = [dp, i32, i32]
+    lib.reader_kv_evict.restype = ctypes.c_int
+    lib.reader_kv_evict.argtypes = [dp, i32, i32, i32] + [vp] * 5 + [i32, vp, sz, vp, vp]
     lib.reader_profile_enable.restype = ctypes.c_int
     lib.reader_profile_enable.argtypes = [i32]
     lib.reader_profile_collect.restype = ctypes.c_int
@@ -316,6 +336,67 @@ def reader_target_sample(logits, parents, uniforms, temperature, target_tokens):
     code = (_native or _load_native()).target_sample(logits, parents, uniforms, temperature, target_tokens)
     if code:
         _check(code, "reader_target_sample")
+
+
+def reader_tree_qkv(dims, qkv, parents, seq_lens, positions, q_norm, k_norm, eps, cos_sin, interleaved, q, k_tree, v_tree,
+                    k_cache, v_cache, page_table, status=None):
+    """qkv: bf16 [B, T, Hq + 2 Hkv, D]; cos_sin: float32 [max_positions, rot_dims] or None (no rotation); k_tree, v_tree
+    both None: the K/V rows go into k_cache, v_cache behind each sequence."""
+    code = (_native or _load_native()).tree_qkv(dims, qkv, parents, seq_lens, positions, q_norm, k_norm, eps, cos_sin,
+                                                interleaved, q, k_tree, v_tree, k_cache, v_cache, page_table, status)
+    if code:
+        _check(code, "reader_tree_qkv")
+
+
+def reader_prompt_qkv(dims, qkv, cu_tokens, seq_lens, positions, q_norm, k_norm, eps, cos_sin, interleaved, q, k_cache, v_cache,
+                      page_table, status=None):
+    """qkv: bf16 [N, Hq + 2 Hkv, D]; cos_sin: float32 [max_positions, rot_dims] or None (no rotation)."""
+    code = (_native or _load_native()).prompt_qkv(dims, qkv, cu_tokens, seq_lens, positions, q_norm, k_norm, eps, cos_sin,
+                                                  interleaved, q, k_cache, v_cache, page_table, status)
+    if code:
+        _check(code, "reader_prompt_qkv")
+
+
+def reader_prompt_workspace_bytes(dims: ReaderDims, N: int, max_seq_len: int) -> int:
+    return int(load().reader_prompt_workspace_bytes(ctypes.byref(dims), int(N), int(max_seq_len)))
+
+
+def reader_prompt_attn(dims, q, k_cache, v_cache, page_table, cu_tokens, seq_lens, out, lse, max_seq_len, workspace, status=None):
+    """q, out: bf16 [N, Hq, D]; lse: float32 [N, Hq] or None."""
+    code = (_native or _load_native()).prompt_attn(dims, q, k_cache, v_cache, page_table, cu_tokens, seq_lens, out, lse,
+                                                   max_seq_len, workspace, status)
+    if code:
+        _check(code, "reader_prompt_attn")
+
+
+def reader_key_weights(dims, q, lse, path, accept_len, k_cache, page_table, seq_lens, decay, weights, max_seq_len, status=None):
+    """weights: float32 [B, Hkv, max_positions], updated in place."""
+    code = (_native or _load_native()).key_weights(dims, q, lse, path, accept_len, k_cache, page_table, seq_lens, decay, weights,
+                                                   max_seq_len, status)
+    if code:
+        _check(code, "reader_key_weights")
+
+
+def reader_prompt_key_weights(dims, q, lse, cu_tokens, window, k_cache, page_table, seq_lens, decay, weights, max_seq_len,
+                              status=None):
+    """q: bf16 [N, Hq, D]; lse: float32 [N, Hq]; weights: float32 [B, Hkv, max_positions], updated in place."""
+    code = (_native or _load_native()).prompt_key_weights(dims, q, lse, cu_tokens, window, k_cache, page_table, seq_lens, decay,
+                                                          weights, max_seq_len, status)
+    if code:
+        _check(code, "reader_prompt_key_weights")
+
+
+def reader_kv_evict_workspace_bytes(dims: ReaderDims, num_layers: int, keep: int) -> int:
+    return int(load().reader_kv_evict_workspace_bytes(ctypes.byref(dims), int(num_layers), int(keep)))
+
+
+def reader_kv_evict(dims, keep, recent, k_cache, v_cache, page_table, seq_lens, weights, workspace, status=None):
+    """k_cache, v_cache: bf16 [num_layers, num_pages, Hkv, page_size, D]; weights: float32 [num_layers, B, Hkv, max_positions];
+    all of them and seq_lens in place."""
+    code = (_native or _load_native()).kv_evict(dims, keep, recent, k_cache, v_cache, page_table, seq_lens, weights, workspace,
+                                                status)
+    if code:
+        _check(code, "reader_kv_evict")
 
 
 def _host_i32(a):

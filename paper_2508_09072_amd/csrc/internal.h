@@ -12,6 +12,9 @@ namespace reader {
 
 // Remember which HIP call failed (text returned by reader_last_error_detail()); returns e.
 hipError_t note_hip_error(const char *where, hipError_t e);
+void forget_stale_error();
+// The limits of reader.h on the sizes; false: *err says why.
+bool dims_ok(const reader_dims *d, int *err);
 
 // MI355X: 256 compute units in 8 XCDs; the launch planner is written for this part only.
 constexpr int kNumCU = 256;

@@ -1,0 +1,79 @@
+// What the operators around the verification step share: where a packed token belongs, and the parameters of their launches.
+#pragma once
+
+#include "internal.h"
+
+namespace reader {
+
+// Rows of a packed batch: sequence b owns rows cu_tokens[b] .. cu_tokens[b + 1] - 1 of N.  Nothing in a table that does
+// not hold that (a bound outside [0, N], or one below the bound in front of it) leads an access out of the tensors.
+__device__ inline int clamp_row(int row, int N) { return row < 0 ? 0 : (row > N ? N : row); }
+
+// Sequence of row t, found by a whole wavefront together: 64 bounds are compared at a time.  B: behind the last sequence.
+__device__ inline int sequence_of_row(const int32_t *__restrict__ cu_tokens, int B, int t, int lane) {
+    int lo = 0, len = B;
+    while (len > 64) {
+        const int step = (len + 63) >> 6, at = lo + (lane + 1) * step - 1;
+        const bool behind = at < lo + len && cu_tokens[at + 1] <= t;
+        const int n = __popcll(__ballot(behind));
+        lo += n * step;
+        len = min(step, len - n * step);
+        if (len <= 0) return lo;
+    }
+    const bool behind = lane < len && cu_tokens[lo + lane + 1] <= t;
+    return __builtin_amdgcn_readfirstlane(lo + __popcll(__ballot(behind)));
+}
+
+struct QkvParams {
+    const uint16_t *qkv, *q_norm, *k_norm;
+    const float *cos_sin;
+    const int32_t *cu_tokens;      // packed prompts, or null: trees
+    const int32_t *parents, *seq_lens, *positions, *page_table;
+    uint16_t *q, *k_tree, *v_tree, *k_cache, *v_cache;
+    int32_t *status;
+    int32_t B, T, N, Hq, Hkv, D, max_pages, max_positions, rot, interleaved;
+    float eps;
+    int64_t num_pages;
+};
+hipError_t launch_qkv(const QkvParams &p, hipStream_t stream);
+
+struct PromptParams {
+    const uint16_t *q, *k_cache, *v_cache;
+    const int32_t *page_table, *cu_tokens, *seq_lens;
+    uint16_t *out;
+    float *lse;
+    void *workspace;
+    int32_t *status;
+    int32_t B, N, Hq, Hkv, G, D, max_pages, max_seq_len;
+    int64_t num_pages;
+    float scale_log2;              // softmax scale * log2(e)
+};
+hipError_t launch_prompt_attn_scalar(const PromptParams &p, hipStream_t stream);
+
+struct KeyWeightsParams {
+    const uint16_t *q, *k_cache;
+    const float *lse;
+    const int32_t *path, *accept_len;              // a step's accepted path, or null: the last rows of packed prompts
+    const int32_t *cu_tokens;
+    const int32_t *page_table, *seq_lens;
+    float *weights;
+    int32_t *status;
+    int32_t B, T, N, Hq, Hkv, G, D, max_pages, max_path, max_seq_len, max_positions, window;
+    int64_t num_pages;
+    float scale_log2, decay, g_rcp;
+};
+hipError_t launch_key_weights(const KeyWeightsParams &p, hipStream_t stream);
+
+struct EvictParams {
+    uint16_t *k_cache, *v_cache;   // [NL, num_pages, Hkv, page_size, D]
+    const int32_t *page_table;
+    int32_t *seq_lens, *status;
+    float *weights;                // [NL, B, Hkv, max_positions]
+    int32_t *source;               // workspace: [NL * B * Hkv][keep] where each kept row comes from
+    int32_t *old_len;              // ... and [NL * B * Hkv] the length before the call (0: nothing to do)
+    int32_t NL, B, Hkv, D, max_pages, max_positions, keep, recent;
+    int64_t num_pages;
+};
+hipError_t launch_kv_evict(const EvictParams &p, hipStream_t stream);
+
+}  // namespace reader

@@ -28,14 +28,14 @@ static int tuning(int which) { return g_tuning[which].load(std::memory_order_rel
 
 // The runtime keeps the last error of the calling thread until somebody reads it, whoever caused
 // it: an error another library left behind must not be taken for a failed launch of ours.
-static void forget_stale_error() { (void)hipGetLastError(); }
+void forget_stale_error() { (void)hipGetLastError(); }
 
 hipError_t note_hip_error(const char *where, hipError_t e) {
     if (e != hipSuccess) snprintf(g_error_detail, sizeof g_error_detail, "%s: %s", where, hipGetErrorName(e));
     return e;
 }
 
-static bool dims_ok(const reader_dims *d, int *err) {
+bool dims_ok(const reader_dims *d, int *err) {
     if (!d) { *err = READER_EINVAL; return false; }
     if (d->B < 0 || d->T < 1 || d->Hq < 1 || d->Hkv < 1 || d->D < 1 || d->max_pages_per_seq < 0 ||
         d->max_path < 1 || d->num_pages < 0 || d->Hq % d->Hkv != 0 || d->max_path > d->T) {

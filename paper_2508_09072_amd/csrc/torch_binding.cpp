@@ -14,13 +14,16 @@
 #define NPY_NO_DEPRECATED_API NPY_1_7_API_VERSION
 #include <numpy/arrayobject.h>
 
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <dlfcn.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <memory>
 #include <new>
+#include <string>
 
 #include "reader.h"
 
@@ -32,6 +35,8 @@ struct Api {
 #define READER_FNS(X)                                                                                               \
     X(reader_tree_attn) X(reader_tree_attn_noalloc) X(reader_accept_path) X(reader_kv_compact) X(reader_verify_step) \
     X(reader_kv_rearrange) X(reader_target_argmax) X(reader_target_sample) X(reader_kv_compact_layers)               \
+    X(reader_tree_qkv) X(reader_prompt_qkv) X(reader_prompt_attn) X(reader_key_weights) X(reader_prompt_key_weights)  \
+    X(reader_kv_evict)                                                                                               \
     X(reader_trie_insert) X(reader_trie_search_path) X(reader_trie_extract_tree) X(reader_tree_attach_path)
     READER_FNS(READER_FN)
 #undef READER_FN
@@ -119,7 +124,28 @@ public:
             ok_ = false;
             return nullptr;
         }
+        if (t.numel() > 0) {
+            if (device_ == kNoDevice) device_ = t.get_device();
+            if (device_ != t.get_device()) several_ = true;
+        }
         return &t;
+    }
+    // a tensor of this shape (every tensor that an entry point describes by the dimensions)
+    const at::Tensor *shaped(at::ScalarType type, std::initializer_list<int64_t> shape, const char *what, bool optional = false) {
+        const at::Tensor *t = tensor(type, optional);
+        if (!t || t->sizes() == at::IntArrayRef(shape.begin(), shape.size())) return t;
+        std::string want, got;
+        for (int64_t n : shape) want += (want.empty() ? "" : ", ") + std::to_string(n);
+        for (int64_t n : t->sizes()) got += (got.empty() ? "" : ", ") + std::to_string(n);
+        PyErr_Format(PyExc_ValueError, "%s must be [%s], got [%s]", what, want.c_str(), got.c_str());
+        ok_ = false;
+        return nullptr;
+    }
+    // all tensors on the device whose current stream the launch goes to
+    void on_current_device() {
+        if (!ok_ || (!several_ && (device_ == kNoDevice || device_ == c10::hip::current_device()))) return;
+        PyErr_SetString(PyExc_ValueError, "tensors must live on the current device");
+        ok_ = false;
     }
     void *ptr(at::ScalarType type, bool optional = false) {
         const at::Tensor *t = tensor(type, optional);
@@ -162,9 +188,11 @@ public:
 private:
     static PyObject *Py_NewRef_(PyObject *o) { Py_INCREF(o); return o; }
     const reader_dims *fail() { ok_ = false; return nullptr; }
+    static constexpr int64_t kNoDevice = -2;
     PyObject *const *a_;
     Py_ssize_t i_ = 0;
-    bool ok_ = true;
+    bool ok_ = true, several_ = false;
+    int64_t device_ = kNoDevice;
     reader_dims dims_;
 };
 
@@ -336,6 +364,182 @@ PyObject *py_kv_compact_layers(PyObject *const *args, Py_ssize_t n) {
     return unlocked([&] { return api.reader_kv_compact_layers(d, NL, path, len, kp, vp, table, lens, status, st); });
 }
 
+// ------------------------------------------------------------------ around the verification step
+template <class T>
+T *data(const at::Tensor *t) { return t ? static_cast<T *>(t->data_ptr()) : nullptr; }
+
+// The rotation table [max_positions, rot_dims], or None.
+struct Rotation {
+    const float *cos_sin;
+    int32_t max_positions, rot_dims, interleaved;
+    explicit Rotation(Args &a) {
+        const at::Tensor *t = a.tensor(kF32, true);
+        if (t) a.want_dims(t, 2, "cos_sin");
+        interleaved = a.integer();
+        const bool there = t && a.ok();
+        cos_sin = there ? data<float>(t) : nullptr;
+        max_positions = there ? (int32_t)t->size(0) : 0;
+        rot_dims = there ? (int32_t)t->size(1) : 0;
+    }
+};
+
+PyObject *py_tree_qkv(PyObject *const *args, Py_ssize_t n) {
+    Args a(args, n, 17);
+    const reader_dims *d = a.dims();
+    if (!d) return nullptr;
+    const int64_t B = d->B, T = d->T, Hq = d->Hq, Hkv = d->Hkv, D = d->D;
+    const at::Tensor *qkv = a.shaped(kBf16, {B, T, Hq + 2 * Hkv, D}, "qkv"), *parents = a.shaped(kI32, {B, T}, "parents");
+    const at::Tensor *lens = a.shaped(kI32, {B}, "seq_lens"), *positions = a.shaped(kI32, {B}, "positions", true);
+    const at::Tensor *qn = a.shaped(kBf16, {D}, "q_norm", true), *kn = a.shaped(kBf16, {D}, "k_norm", true);
+    const double eps = a.number();
+    const Rotation r(a);
+    const at::Tensor *q = a.shaped(kBf16, {B, T, Hq, D}, "q");
+    const at::Tensor *kt = a.shaped(kBf16, {B, T, Hkv, D}, "k_tree", true), *vt = a.shaped(kBf16, {B, T, Hkv, D}, "v_tree", true);
+    const at::Tensor *kc = a.shaped(kBf16, {d->num_pages, Hkv, d->page_size, D}, "k_cache", true);
+    const at::Tensor *vc = a.shaped(kBf16, {d->num_pages, Hkv, d->page_size, D}, "v_cache", true);
+    const at::Tensor *table = a.shaped(kI32, {B, d->max_pages_per_seq}, "page_table", true);
+    int32_t *status = a.i32_out(true);
+    a.on_current_device();
+    if (!a.ok()) return nullptr;
+    void *st = stream();
+    return unlocked([&] {
+        return api.reader_tree_qkv(d, data<void>(qkv), data<int32_t>(parents), data<int32_t>(lens), data<int32_t>(positions), data<void>(qn),
+                                   data<void>(kn), (float)eps, r.cos_sin, r.max_positions, r.rot_dims, r.interleaved, data<void>(q),
+                                   data<void>(kt), data<void>(vt), data<void>(kc), data<void>(vc), data<int32_t>(table), status, st);
+    });
+}
+
+PyObject *py_prompt_qkv(PyObject *const *args, Py_ssize_t n) {
+    Args a(args, n, 15);
+    const reader_dims *d = a.dims();
+    const at::Tensor *qkv = a.tensor(kBf16);
+    a.want_dims(qkv, 3, "qkv");
+    if (!a.ok()) return nullptr;
+    const int64_t N = qkv->size(0), B = d->B, Hq = d->Hq, Hkv = d->Hkv, D = d->D;
+    if (qkv->size(1) != Hq + 2 * Hkv || qkv->size(2) != D) a.reject(PyExc_ValueError, "qkv must be [N, Hq + 2 Hkv, D]");
+    const at::Tensor *cu = a.shaped(kI32, {B + 1}, "cu_tokens"), *lens = a.shaped(kI32, {B}, "seq_lens");
+    const at::Tensor *positions = a.shaped(kI32, {B}, "positions", true);
+    const at::Tensor *qn = a.shaped(kBf16, {D}, "q_norm", true), *kn = a.shaped(kBf16, {D}, "k_norm", true);
+    const double eps = a.number();
+    const Rotation r(a);
+    const at::Tensor *q = a.shaped(kBf16, {N, Hq, D}, "q");
+    const at::Tensor *kc = a.shaped(kBf16, {d->num_pages, Hkv, d->page_size, D}, "k_cache");
+    const at::Tensor *vc = a.shaped(kBf16, {d->num_pages, Hkv, d->page_size, D}, "v_cache");
+    const at::Tensor *table = a.shaped(kI32, {B, d->max_pages_per_seq}, "page_table");
+    int32_t *status = a.i32_out(true);
+    a.on_current_device();
+    if (!a.ok()) return nullptr;
+    void *st = stream();
+    return unlocked([&] {
+        return api.reader_prompt_qkv(d, (int32_t)N, data<void>(qkv), data<int32_t>(cu), data<int32_t>(lens), data<int32_t>(positions),
+                                     data<void>(qn), data<void>(kn), (float)eps, r.cos_sin, r.max_positions, r.rot_dims, r.interleaved,
+                                     data<void>(q), data<void>(kc), data<void>(vc), data<int32_t>(table), status, st);
+    });
+}
+
+PyObject *py_prompt_attn(PyObject *const *args, Py_ssize_t n) {
+    Args a(args, n, 12);
+    const reader_dims *d = a.dims();
+    const at::Tensor *q = a.tensor(kBf16);
+    a.want_dims(q, 3, "q");
+    if (!a.ok()) return nullptr;
+    const int64_t N = q->size(0), B = d->B, Hq = d->Hq, Hkv = d->Hkv, D = d->D;
+    if (q->size(1) != Hq || q->size(2) != D) a.reject(PyExc_ValueError, "q must be [N, Hq, D]");
+    const at::Tensor *kc = a.shaped(kBf16, {d->num_pages, Hkv, d->page_size, D}, "k_cache");
+    const at::Tensor *vc = a.shaped(kBf16, {d->num_pages, Hkv, d->page_size, D}, "v_cache");
+    const at::Tensor *table = a.shaped(kI32, {B, d->max_pages_per_seq}, "page_table");
+    const at::Tensor *cu = a.shaped(kI32, {B + 1}, "cu_tokens"), *lens = a.shaped(kI32, {B}, "seq_lens");
+    const at::Tensor *out = a.shaped(kBf16, {N, Hq, D}, "out"), *lse = a.shaped(kF32, {N, Hq}, "lse", true);
+    const int32_t max_len = a.integer();
+    const at::Tensor *ws = a.tensor(kAny, true);
+    int32_t *status = a.i32_out(true);
+    a.on_current_device();
+    if (!a.ok()) return nullptr;
+    void *st = stream();
+    const size_t ws_bytes = ws ? ws->nbytes() : 0;
+    return unlocked([&] {
+        return api.reader_prompt_attn(d, (int32_t)N, data<void>(q), data<void>(kc), data<void>(vc), data<int32_t>(table), data<int32_t>(cu),
+                                      data<int32_t>(lens), data<void>(out), data<float>(lse), max_len, data<void>(ws), ws_bytes, status, st);
+    });
+}
+
+PyObject *py_key_weights(PyObject *const *args, Py_ssize_t n) {
+    Args a(args, n, 12);
+    const reader_dims *d = a.dims();
+    if (!d) return nullptr;
+    const int64_t B = d->B, T = d->T, Hq = d->Hq, Hkv = d->Hkv, D = d->D;
+    const at::Tensor *q = a.shaped(kBf16, {B, T, Hq, D}, "q"), *lse = a.shaped(kF32, {B, Hq, T}, "lse");
+    const at::Tensor *path = a.shaped(kI32, {B, d->max_path}, "path"), *len = a.shaped(kI32, {B}, "accept_len");
+    const at::Tensor *kc = a.shaped(kBf16, {d->num_pages, Hkv, d->page_size, D}, "k_cache");
+    const at::Tensor *table = a.shaped(kI32, {B, d->max_pages_per_seq}, "page_table"), *lens = a.shaped(kI32, {B}, "seq_lens");
+    const double decay = a.number();
+    const at::Tensor *w = a.tensor(kF32);
+    const int32_t max_len = a.integer();
+    int32_t *status = a.i32_out(true);
+    a.on_current_device();
+    if (a.ok() && (w->dim() != 3 || w->size(0) != B || w->size(1) != Hkv)) a.reject(PyExc_ValueError, "weights must be [B, Hkv, max_positions]");
+    if (!a.ok()) return nullptr;
+    void *st = stream();
+    return unlocked([&] {
+        return api.reader_key_weights(d, data<void>(q), data<float>(lse), data<int32_t>(path), data<int32_t>(len), data<void>(kc),
+                                      data<int32_t>(table), data<int32_t>(lens), (float)decay, data<float>(w), (int32_t)w->size(2), max_len,
+                                      status, st);
+    });
+}
+
+PyObject *py_prompt_key_weights(PyObject *const *args, Py_ssize_t n) {
+    Args a(args, n, 12);
+    const reader_dims *d = a.dims();
+    const at::Tensor *q = a.tensor(kBf16);
+    a.want_dims(q, 3, "q");
+    if (!a.ok()) return nullptr;
+    const int64_t N = q->size(0), B = d->B, Hq = d->Hq, Hkv = d->Hkv, D = d->D;
+    if (q->size(1) != Hq || q->size(2) != D) a.reject(PyExc_ValueError, "q must be [N, Hq, D]");
+    const at::Tensor *lse = a.shaped(kF32, {N, Hq}, "lse"), *cu = a.shaped(kI32, {B + 1}, "cu_tokens");
+    const int32_t window = a.integer();
+    const at::Tensor *kc = a.shaped(kBf16, {d->num_pages, Hkv, d->page_size, D}, "k_cache");
+    const at::Tensor *table = a.shaped(kI32, {B, d->max_pages_per_seq}, "page_table"), *lens = a.shaped(kI32, {B}, "seq_lens");
+    const double decay = a.number();
+    const at::Tensor *w = a.tensor(kF32);
+    const int32_t max_len = a.integer();
+    int32_t *status = a.i32_out(true);
+    a.on_current_device();
+    if (a.ok() && (w->dim() != 3 || w->size(0) != B || w->size(1) != Hkv)) a.reject(PyExc_ValueError, "weights must be [B, Hkv, max_positions]");
+    if (!a.ok()) return nullptr;
+    void *st = stream();
+    return unlocked([&] {
+        return api.reader_prompt_key_weights(d, (int32_t)N, data<void>(q), data<float>(lse), data<int32_t>(cu), window, data<void>(kc),
+                                             data<int32_t>(table), data<int32_t>(lens), (float)decay, data<float>(w), (int32_t)w->size(2),
+                                             max_len, status, st);
+    });
+}
+
+PyObject *py_kv_evict(PyObject *const *args, Py_ssize_t n) {
+    Args a(args, n, 10);
+    const reader_dims *d = a.dims();
+    const int32_t keep = a.integer(), recent = a.integer();
+    const at::Tensor *k = a.tensor(kBf16);
+    a.want_dims(k, 5, "k_cache");
+    if (!a.ok()) return nullptr;
+    const int64_t NL = k->size(0), B = d->B, Hkv = d->Hkv;
+    if (k->sizes() != at::IntArrayRef({NL, d->num_pages, Hkv, (int64_t)d->page_size, (int64_t)d->D}))
+        a.reject(PyExc_ValueError, "k_cache must be [num_layers, num_pages, Hkv, page_size, D]");
+    const at::Tensor *v = a.shaped(kBf16, {NL, d->num_pages, Hkv, d->page_size, d->D}, "v_cache");
+    const at::Tensor *table = a.shaped(kI32, {B, d->max_pages_per_seq}, "page_table"), *lens = a.shaped(kI32, {B}, "seq_lens");
+    const at::Tensor *w = a.tensor(kF32), *ws = a.tensor(kAny, true);
+    int32_t *status = a.i32_out(true);
+    a.on_current_device();
+    if (a.ok() && (w->dim() != 4 || w->size(0) != NL || w->size(1) != B || w->size(2) != Hkv))
+        a.reject(PyExc_ValueError, "weights must be [num_layers, B, Hkv, max_positions]");
+    if (!a.ok()) return nullptr;
+    void *st = stream();
+    const size_t ws_bytes = ws ? ws->nbytes() : 0;
+    return unlocked([&] {
+        return api.reader_kv_evict(d, (int32_t)NL, keep, recent, data<void>(k), data<void>(v), data<int32_t>(table), data<int32_t>(lens),
+                                   data<float>(w), (int32_t)w->size(3), data<void>(ws), ws_bytes, status, st);
+    });
+}
+
 // ------------------------------------------------------------------ the host-side drafter (numpy arrays)
 
 // Whole numbers as a C-contiguous int32 array: the object itself if it is one, else a converted copy.
@@ -448,7 +652,8 @@ PyMethodDef methods[] = {
     {"init", py_init, METH_VARARGS, "init(handle, dims_type): look the entry points up in a loaded library"},
     READER_FAST(tree_attn), READER_FAST(tree_attn_noalloc), READER_FAST(accept_path), READER_FAST(kv_compact),
     READER_FAST(verify_step), READER_FAST(kv_rearrange), READER_FAST(target_argmax), READER_FAST(target_sample),
-    READER_FAST(kv_compact_layers), READER_FAST(trie_insert), READER_FAST(trie_search_path), READER_FAST(trie_extract_tree),
+    READER_FAST(kv_compact_layers), READER_FAST(tree_qkv), READER_FAST(prompt_qkv), READER_FAST(prompt_attn),
+    READER_FAST(key_weights), READER_FAST(prompt_key_weights), READER_FAST(kv_evict), READER_FAST(trie_insert), READER_FAST(trie_search_path), READER_FAST(trie_extract_tree),
     READER_FAST(tree_attach_path), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_reader_torch", "torch and numpy arguments of the reader C ABI", -1, methods,

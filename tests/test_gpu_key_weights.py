@@ -1,0 +1,154 @@
+"""reader_key_weights and reader_prompt_key_weights against their 64-bit form."""
+import math
+
+import pytest
+import torch
+
+import prompt_helpers as P
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def R():
+    from paper_2508_09072_amd import binding
+    binding.load()
+    return binding
+
+
+def i32(x):
+    return torch.as_tensor(x, dtype=torch.int32).cuda()
+
+
+HEADS = [(4, 1, 128), (3, 1, 64), (8, 2, 64), (2, 2, 128), (16, 1, 128), (6, 2, 128)]
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", HEADS)
+@pytest.mark.parametrize("decay", [0.0, 1.0, 0.75])
+def test_step(R, Hq, Hkv, D, decay):
+    gen = torch.Generator().manual_seed(D + Hq)
+    T, accepted, L = 20, [1, 4, 9, 2, 1], [1, 0, 300, 63, 1000]     # (L: lengths in front of the step)
+    B, mp = len(L), 9
+    cache = P.Cache(gen, [l + n for l, n in zip(L, accepted)], Hkv, D)
+    path = torch.full((B, mp), -1, dtype=torch.int32)
+    for b in range(B):
+        cache.fill(gen, b, L[b] + accepted[b])
+        path[b, :accepted[b]] = torch.cat([torch.zeros(1), 1 + torch.randperm(T - 1, generator=gen)[:accepted[b] - 1].sort().values]).int()
+    q = torch.randn((B, T, Hq, D), generator=gen).bfloat16()
+    lse = 5 + torch.randn((B, Hq, T), generator=gen)
+    W = cache.max_pages * 16 + 5
+    old = torch.rand((B, Hkv, W), generator=gen)
+    got = old.cuda() if decay else torch.full_like(old, math.nan).cuda()
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    dims = R.make_dims(B, T, Hq, Hkv, D, cache.max_pages, mp, cache.num_pages)
+    lens = i32([l + n for l, n in zip(L, accepted)])
+    R.reader_key_weights(dims, q.cuda(), lse.cuda(), path.cuda(), i32([n - 1 for n in accepted]), cache.k.cuda(), cache.table.cuda(), lens,
+                         decay, got, 1009, status)
+    assert int(status) == 0
+    for b in range(B):
+        n, S = accepted[b], L[b] + accepted[b]
+        nodes = path[b, :n].long()
+        w, bound = P.key_weights(q[b, nodes], lse[b][:, nodes].t(), cache.rows(cache.k, b, S), L[b])
+        want = torch.zeros(Hkv, W, dtype=torch.float64) if decay == 0 else old[b].double().clone()
+        want[:, :S] = (decay * old[b, :, :S].double() if decay else 0) + w
+        full = torch.zeros(Hkv, W, dtype=torch.float64)
+        full[:, :S] = bound + 3 * P.F32 * want[:, :S]
+        P.check(got[b], want, full, "weights of sequence %d" % b)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", HEADS)
+@pytest.mark.parametrize("window", [0, 1, 7, 40, 1000])
+def test_prompt(R, Hq, Hkv, D, window):
+    gen = torch.Generator().manual_seed(D + window)
+    new, L = [0, 1, 50, 130, 17], [5, 0, 0, 700, 47]
+    B, N = len(new), sum(new) + 2
+    cache = P.Cache(gen, [l + n for l, n in zip(L, new)], Hkv, D)
+    for b in range(B):
+        cache.fill(gen, b, L[b] + new[b])
+    cu = torch.cat([torch.zeros(1), torch.cumsum(torch.tensor(new), 0)]).int()
+    q = torch.randn((N, Hq, D), generator=gen).bfloat16()
+    lse = 5 + torch.randn((N, Hq), generator=gen)
+    W = cache.max_pages * 16
+    got = torch.full((B, Hkv, W), math.nan, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    dims = R.make_dims(B, 1, Hq, Hkv, D, cache.max_pages, 1, cache.num_pages)
+    R.reader_prompt_key_weights(dims, q.cuda(), lse.cuda(), cu.cuda(), window, cache.k.cuda(), cache.table.cuda(), i32(L), 0.0, got, 830, status)
+    assert int(status) == 0
+    for b in range(B):
+        S, n, end = L[b] + new[b], min(window, new[b]), int(cu[b + 1])
+        want, full = torch.zeros(Hkv, W, dtype=torch.float64), torch.zeros(Hkv, W, dtype=torch.float64)
+        if n:
+            w, bound = P.key_weights(q[end - n:end], lse[end - n:end], cache.rows(cache.k, b, S), S - n)
+            want[:, :S], full[:, :S] = w, bound
+        P.check(got[b], want, full, "weights of sequence %d" % b)
+
+
+def test_weights_of_one_row_add_up_to_one(R):
+    """Against the attention's own log-sum-exp: the weights that a committed token spends are one per query head."""
+    gen = torch.Generator().manual_seed(3)
+    Hq, Hkv, D, new, L = 8, 2, 128, [33, 5], [400, 90]
+    cache = P.Cache(gen, [l + n for l, n in zip(L, new)], Hkv, D)
+    for b in range(2):
+        cache.fill(gen, b, L[b] + new[b])
+    N = sum(new)
+    q = torch.randn((N, Hq, D), generator=gen).bfloat16().cuda()
+    cu, lens = i32([0, 33, 38]), i32(L)
+    dims = R.make_dims(2, 1, Hq, Hkv, D, cache.max_pages, 1, cache.num_pages)
+    out, lse = torch.empty_like(q), torch.empty((N, Hq), device="cuda")
+    ws = torch.empty(max(256, R.reader_prompt_workspace_bytes(dims, N, 433)), dtype=torch.uint8, device="cuda")
+    kc, vc, table = cache.k.cuda(), cache.v.cuda(), cache.table.cuda()
+    R.reader_prompt_attn(dims, q, kc, vc, table, cu, lens, out, lse, 433, ws)
+    w = torch.empty((2, Hkv, cache.max_pages * 16), device="cuda")
+    R.reader_prompt_key_weights(dims, q, lse, cu, 1000, kc, table, lens, 0.0, w, 433)
+    total = w.double().sum(-1).cpu()
+    want = torch.tensor(new, dtype=torch.float64)[:, None] * (Hq // Hkv)
+    # every weight is off by a few score roundings (magnitudes of D = 128 products: sums below 16) on both sides
+    assert bool(((total - want).abs() <= want * 2 * (132 * 16 + 64) * P.F32).all())
+
+
+def test_sequences_that_do_not_fit_are_left_as_they_are(R):
+    gen = torch.Generator().manual_seed(4)
+    B, T, Hq, Hkv, D, mp = 6, 6, 2, 1, 64, 4
+    cache = P.Cache(gen, [40] * B, Hkv, D)
+    for b in range(B):
+        cache.fill(gen, b, 40)
+    q, lse = torch.randn((B, T, Hq, D), generator=gen).bfloat16().cuda(), torch.zeros((B, Hq, T), device="cuda")
+    path = torch.tensor([[0, 1, 2, 3], [0, 6, -1, -1], [0, -2, 3, 3], [0, 1, -1, -1], [0, -1, -1, -1], [0, 1, 2, 4]], dtype=torch.int32)
+    accept = [4, 1, 1, 1, 0, 3]                                # 4: more than max_path - 1
+    lens = [40, 40, 40, 41, 49, 3]                             # 49: no pages for it; 3: shorter than its path
+    status, w = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.full((B, Hkv, 48), 2.0, device="cuda")
+    dims = R.make_dims(B, T, Hq, Hkv, D, cache.max_pages, mp, cache.num_pages)
+    R.reader_key_weights(dims, q, lse, path.cuda(), i32(accept), cache.k.cuda(), cache.table.cuda(), i32(lens), 0.0, w, 40, status)
+    assert int(status) == R.STATUS_BAD_PATH | R.STATUS_BAD_LENGTH
+    assert bool((w == 2.0).all())
+
+
+def test_keys_behind_a_missing_page_draw_nothing(R):
+    gen = torch.Generator().manual_seed(5)
+    cache = P.Cache(gen, [100], 1, 64)
+    cache.fill(gen, 0, 100)
+    rows = cache.rows(cache.k, 0, 100)
+    cache.table[0, 3] = cache.num_pages
+    q, lse = torch.randn((1, 2, 64), generator=gen).bfloat16(), torch.full((1, 2), 4.0)
+    w, status = torch.ones((1, 1, 112), device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    dims = R.make_dims(1, 1, 2, 1, 64, cache.max_pages, 1, cache.num_pages)
+    R.reader_prompt_key_weights(dims, q.cuda(), lse.cuda(), i32([0, 1]), 4, cache.k.cuda(), cache.table.cuda(), i32([99]), 0.5, w, 100, status)
+    assert int(status) == R.STATUS_BAD_PAGE
+    want, bound = P.key_weights(q, lse, rows, 99)
+    want[:, 48:64], bound[:, 48:64] = 0, 0
+    P.check(w[0, :, :100], want + 0.5, bound + 4 * P.F32 * (want + 0.5), "weights")
+    assert bool((w[0, 0, 100:] == 1).all())
+
+
+def test_rows_that_saw_nothing_give_nothing(R):
+    gen = torch.Generator().manual_seed(6)
+    cache = P.Cache(gen, [20], 1, 128)
+    cache.fill(gen, 0, 20)
+    q = torch.randn((3, 1, 128), generator=gen).bfloat16()
+    lse = torch.tensor([[3.0], [-math.inf], [2.0]])
+    w = torch.zeros((1, 1, 32), device="cuda")
+    dims = R.make_dims(1, 1, 1, 1, 128, cache.max_pages, 1, cache.num_pages)
+    R.reader_prompt_key_weights(dims, q.cuda(), lse.cuda(), i32([0, 3]), 3, cache.k.cuda(), cache.table.cuda(), i32([17]), 1.0, w, 20)
+    a, ba = P.key_weights(q[:1], lse[:1], cache.rows(cache.k, 0, 20), 17)
+    c, bc = P.key_weights(q[2:], lse[2:], cache.rows(cache.k, 0, 20), 19)
+    P.check(w[0, :, :20], a + c, ba + bc + 3 * P.F32 * (a + c), "weights")
