@@ -22,7 +22,9 @@ STAMPS_LIB = os.path.join(HERE, "libreader_hip_stamps.so")
 # the extension module binding.py calls the library through (torch tensors and numpy arrays to pointers)
 NATIVE = os.path.join(HERE, "_reader_torch.so")
 SOURCES = ["reader_api.hip", "trie_drafter.cpp", "tree_shape.cpp", "accept_compact.hip", "kv_compact_layers.hip", "kv_rearrange.hip", "target_argmax.hip", "target_sample.hip", "tree_attn_scalar.hip", "tree_attn_mfma.hip", "tree_attn_wide.hip", "tree_attn_short.hip", "peak_probes.hip",
-           "prompt_api.hip", "qkv_prepare.hip", "prompt_attn_scalar.hip", "key_weights.hip", "kv_evict.hip"]
+           "prompt_api.hip", "qkv_prepare.hip", "prompt_attn.hip", "prompt_attn_scalar.hip", "key_weights.hip", "kv_evict.hip"]
+# kernels that manage the accumulation registers by hand
+HAND_MANAGED = ["tree_attn_wide.hip", "prompt_attn.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
     # keep the compiler from forming packed-fp32 instructions
@@ -65,7 +67,7 @@ def spilled_kernels(compiler_output: str):
 def foreign_agpr_uses(asm_text: str):
     """Lines of compiler-generated code (outside inline-asm blocks) that touch an accumulation register.
 
-    tree_attn_wide.hip keeps its output accumulators and query fragments in accumulation registers it names
+    The sources of HAND_MANAGED keep their output accumulators and query fragments in accumulation registers they name
     by number in inline asm; the register allocator does not know that, so it must never put anything
     there itself (a value parked in one would be overwritten, and an overwritten address faults the GPU)."""
     import re
@@ -80,18 +82,18 @@ def foreign_agpr_uses(asm_text: str):
     return bad
 
 
-def check_wide_kernel(hipcc: str, verbose: bool) -> None:
+def check_wide_kernel(hipcc: str, verbose: bool, source: str = "tree_attn_wide.hip") -> None:
     cmd = [hipcc] + [f for f in FLAGS if f not in ("-fPIC", "-shared", "-Rpass-analysis=kernel-resource-usage")]
     cmd += ["--cuda-device-only", "-S", "-I" + os.path.join(ROOT, "include"), "-I" + CSRC,
-            os.path.join(CSRC, "tree_attn_wide.hip"), "-o", "-"]
+            os.path.join(CSRC, source), "-o", "-"]
     res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.DEVNULL, text=True)
     if res.returncode != 0:
-        raise RuntimeError("hipcc -S of tree_attn_wide.hip failed")
+        raise RuntimeError("hipcc -S of %s failed" % source)
     bad = foreign_agpr_uses(res.stdout)
     if bad:
-        raise RuntimeError("the compiler uses accumulation registers of its own in tree_attn_wide.hip: %s" % bad[:5])
+        raise RuntimeError("the compiler uses accumulation registers of its own in %s: %s" % (source, bad[:5]))
     if verbose:
-        print("tree_attn_wide.hip: accumulation registers are touched by hand-written instructions only")
+        print("%s: accumulation registers are touched by hand-written instructions only" % source)
 
 
 def build_native(verbose: bool = False) -> str:
@@ -157,7 +159,8 @@ def build_library(verbose: bool = False, stamps: bool = False) -> str:
     if verbose and out.strip():
         print(out)
     try:
-        check_wide_kernel(hipcc, verbose)
+        for source in HAND_MANAGED:
+            check_wide_kernel(hipcc, verbose, source)
     except Exception:
         os.remove(tmp)
         raise

@@ -89,7 +89,7 @@ extern "C" int reader_prompt_qkv(const reader_dims *dims, int32_t N, const void 
 extern "C" size_t reader_prompt_workspace_bytes(const reader_dims *dims, int32_t N, int32_t max_seq_len) {
     int err = 0;
     if (!dims_ok(dims, &err) || rows_ok(dims, N) != READER_OK || max_seq_len < 0) return 0;
-    return 256;
+    return prompt_workspace_bytes(dims->D);
 }
 
 extern "C" int reader_prompt_attn(const reader_dims *dims, int32_t N, const void *q, const void *k_cache, const void *v_cache,
@@ -117,8 +117,12 @@ extern "C" int reader_prompt_attn(const reader_dims *dims, int32_t N, const void
         if (!workspace || ((uintptr_t)workspace & 255) != 0) return READER_EWORKSPACE;
         if (workspace_bytes < reader_prompt_workspace_bytes(dims, N, max_seq_len)) return READER_EWORKSPACE;
     }
+    p.g_rcp = 1.0f / (float)p.G;
+    p.tokens_per_block = 256 / p.G;
+    p.n_ranges = kNumCU;
     forget_stale_error();
-    return launch_prompt_attn_scalar(p, (hipStream_t)stream) == hipSuccess ? READER_OK : READER_EHIP;
+    return (dims->variant == 1 ? launch_prompt_attn_scalar(p, (hipStream_t)stream) : launch_prompt_attn(p, (hipStream_t)stream)) == hipSuccess
+               ? READER_OK : READER_EHIP;
 }
 
 static int key_weights_prepare(const reader_dims *dims, const void *q, const float *lse, const void *k_cache,

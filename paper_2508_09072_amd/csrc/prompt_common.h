@@ -47,7 +47,12 @@ struct PromptParams {
     int32_t B, N, Hq, Hkv, G, D, max_pages, max_seq_len;
     int64_t num_pages;
     float scale_log2;              // softmax scale * log2(e)
+    float g_rcp;                   // 1 / G
+    int32_t tokens_per_block;      // (matrix kernel) tokens whose heads fill a block of query rows
+    int32_t n_ranges;              // ... and workgroups of the launch
 };
+size_t prompt_workspace_bytes(int D);
+hipError_t launch_prompt_attn(const PromptParams &p, hipStream_t stream);
 hipError_t launch_prompt_attn_scalar(const PromptParams &p, hipStream_t stream);
 
 struct KeyWeightsParams {
