@@ -4,10 +4,13 @@
 // The log-sum-exp that the attention left turns a score into its softmax weight, so one product with the keys is all.
 //
 // S = Q.K^T on the matrix cores in blocks of 16 rows x 16 keys (one page): a lane then holds four rows of one key, and the
-// sum over rows is a sum over registers, with two exchanges between lanes at the very end.  A wavefront owns 64 keys, whose
-// rows (its operand for all query rows) are loaded from memory once, straight into the operand's layout: 16 lanes read 16
-// rows, 64 bytes of each per load.  Nobody else writes those keys' weights: no atomics, the same bits every time.
-// Bound by memory for the few rows of a step (K is read once), by the matrix cores and exponentials beyond some 128 rows.
+// sum over rows is a sum over registers, with two exchanges between lanes at the end.  A wavefront holds up to 128 query rows
+// as operands in registers and takes 64 keys a turn, whose pages travel to its own part of the LDS whole, 1 KB a copy
+// instruction, four pages ahead.  (Loaded straight into the operand's layout, 64 bytes of 16 rows an instruction, they came at 4
+// TB/s however many were asked for.)  Up to 128 rows a workgroup is one wavefront, which waits for nobody; beyond that two
+// or four of them share out the rows of the same keys and add up at the end of a turn (8 sequences of up to 2000 keys, 512 rows
+// each, head dimension 64: 45 -> 20 us), and beyond 512 the keys pass by again.  Nobody else writes a key's weight: no atomics, the same bits every time.
+// Bound by memory: K is read once; with 128 rows the exponentials come within a factor of two of that.
 #include "prompt_common.h"
 #include "tree_attn_common.h"
 
@@ -16,122 +19,214 @@ namespace reader {
 namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-constexpr int kKeysPerWave = 64, kWeightsThreads = 256, kKeysPerWg = kKeysPerWave * kWeightsThreads / 64;
+constexpr int kTurnPages = 4, kTurnKeys = kTurnPages * READER_PAGE_SIZE;
+constexpr int kMaxTurns = 64 / kTurnPages;               // of a wavefront: a lane holds a page id
 
-template <int D>
-__global__ __launch_bounds__(kWeightsThreads) void key_weights_kernel(KeyWeightsParams p) {
+// kBlocks: blocks of 16 query rows that a wavefront holds at a time
+template <int D, int kBlocks, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, kBlocks * D <= 512 ? 3 : 2) void key_weights_kernel(KeyWeightsParams p, int turns) {
     constexpr int kSteps = D / 32;                       // 32-deep steps of the product
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int hkv = blockIdx.y, b = blockIdx.z, j0 = (int)blockIdx.x * kKeysPerWg + wave * kKeysPerWave;
-    const int i16 = lane & 15, quad = lane >> 4;
+    constexpr int kRowBytes = D * 2, kChunks = D / 8, kPageBytes = READER_PAGE_SIZE * kRowBytes;
+    constexpr int kCopies = kPageBytes / 1024, kRowsPerCopy = 64 / kChunks;
+    __shared__ __attribute__((aligned(1024))) char s_ring[kWaves][kTurnPages * kPageBytes];   // of each wavefront: a turn's pages
+    __shared__ float s_old[2][kTurnKeys];                                              // what the keys of a turn have so far
+    __shared__ float s_sum[2][kWaves][kTurnKeys];                                      // what each wavefront's rows add
+    const int lane = threadIdx.x & 63, wave = kWaves == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i16 = lane & 15, quad = lane >> 4;
+    const int hkv = blockIdx.y, b = blockIdx.z, key0 = (int)blockIdx.x * turns * kTurnKeys;
+
+    // (what does not depend on one another is asked for together: pages of this wavefront's keys, path, lengths)
+    int page = p.page_table[(size_t)b * p.max_pages + min(key0 / READER_PAGE_SIZE + lane, p.max_pages - 1)];
+    const int32_t *path = p.path + (p.path ? (size_t)b * p.max_path : 0);
+    const int node = p.path ? path[min(lane, p.max_path - 1)] : 0, node2 = p.path ? path[min(lane + 64, p.max_path - 1)] : 0;
+    const int len = p.seq_lens[b];
 
     // rows: `n` query tokens, the first of them at position `first`; row r is token r / G, head r % G of the group
     int n, first, bad = 0, token0 = 0;
-    const int len = p.seq_lens[b];
     if (p.path) {
         n = p.accept_len[b] + 1;
         first = len - n;
         if (n < 1 || n > p.max_path || first < 0) bad = READER_STATUS_BAD_PATH;
+        else if (__any((lane < n && (node < 0 || node >= p.T)) || (lane + 64 < n && (node2 < 0 || node2 >= p.T)))) bad = READER_STATUS_BAD_PATH;
     } else {
-        const int c0 = clamp_row(p.cu_tokens[b], p.N), c1 = clamp_row(p.cu_tokens[b + 1], p.N);
+        const int lo = p.cu_tokens[b], hi = p.cu_tokens[b + 1], c0 = clamp_row(lo, p.N), c1 = clamp_row(hi, p.N);
         const int all = max(c1 - c0, 0);
         n = min(all, p.window);
         token0 = c1 - n;
         first = len + all - n;
-        if (len < 0 || p.cu_tokens[b] < 0 || p.cu_tokens[b + 1] < p.cu_tokens[b] || p.cu_tokens[b + 1] > p.N) bad = READER_STATUS_BAD_LENGTH;
+        if (len < 0 || lo < 0 || hi < lo || hi > p.N) bad = READER_STATUS_BAD_LENGTH;
     }
     const long long keys_all = (long long)first + n;
     const long long most = min((long long)min(p.max_seq_len, p.max_positions), (long long)p.max_pages * READER_PAGE_SIZE);
     if (!bad && keys_all > most) bad = READER_STATUS_BAD_LENGTH;
-    // (every workgroup of the sequence comes to the same verdict: it is left as it is)
-    if (!bad && p.path) {
-        const int node = lane < n ? p.path[(size_t)b * p.max_path + lane] : 0;
-        const int node2 = lane + 64 < n ? p.path[(size_t)b * p.max_path + lane + 64] : 0;
-        if (__any(node < 0 || node >= p.T || node2 < 0 || node2 >= p.T)) bad = READER_STATUS_BAD_PATH;
-    }
+    // (every wavefront of the sequence comes to the same verdict: it is left as it is)
     if (bad) {
         if (p.status && blockIdx.x == 0 && hkv == 0 && threadIdx.x == 0) atomicOr(p.status, bad);
         return;
     }
-    const int keys = (int)keys_all;
+    const int keys = (int)keys_all, rows = n * p.G;
     float *weights = p.weights + ((size_t)b * p.Hkv + hkv) * p.max_positions;
-    if (j0 >= keys) {
-        if (p.decay == 0.f && j0 + lane < p.max_positions) weights[j0 + lane] = 0.f;
+    if (p.decay == 0.f) {                                // a fresh start: nothing behind the last key
+        const int end = min(key0 + turns * kTurnKeys, p.max_positions);
+        for (int j = max(key0, keys) + (int)threadIdx.x; j < end; j += 64 * kWaves) weights[j] = 0.f;
+    }
+    if (key0 >= keys) return;
+    if (rows == 0) {                                     // nobody to draw anything
+        const int end = min(key0 + turns * kTurnKeys, keys);
+        for (int j = key0 + (int)threadIdx.x; j < end; j += 64 * kWaves) weights[j] = p.decay == 0.f ? 0.f : p.decay * weights[j];
         return;
     }
-
-    // the 64 keys as operands: page `pg` of the four, step s: row i16, values 32 s + 8 quad .. + 7
-    bf16x8 k[4][kSteps];
-    bool page_ok[4];
-#pragma unroll
-    for (int pg = 0; pg < 4; ++pg) {
-        const int j = j0 + pg * 16;
-        const int page = j < keys ? p.page_table[(size_t)b * p.max_pages + (j >> 4)] : 0;
-        page_ok[pg] = page >= 0 && page < p.num_pages;
-        if (!page_ok[pg]) bad = READER_STATUS_BAD_PAGE;
-        // (nothing is loaded behind a page that is not there; pages past the last key read page 0, whose scores are dropped)
-        const uint16_t *src = p.k_cache + (((size_t)(page_ok[pg] ? page : 0) * p.Hkv + hkv) * READER_PAGE_SIZE + i16) * D + quad * 8;
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) k[pg][s] = __builtin_bit_cast(bf16x8, ld16(src + s * 32));
+    turns = min(turns, (keys - key0 + kTurnKeys - 1) / kTurnKeys);
+    {
+        const bool there = lane < turns * kTurnPages && key0 + lane * READER_PAGE_SIZE < keys, ok = page >= 0 && page < p.num_pages;
+        if (__any(there && !ok) && p.status && threadIdx.x == 0) atomicOr(p.status, READER_STATUS_BAD_PAGE);
+        page = there && ok ? page : -1;
     }
-    float mine = 0.f;                                     // old weight of key j0 + lane
-    const int j_mine = j0 + lane;
-    if (p.decay != 0.f && j_mine < keys) mine = p.decay * weights[j_mine];
 
-    const int rows = n * p.G;
-    const bool causal = j0 + kKeysPerWave > first + 1;    // some row does not see some of these keys
-    float acc[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int r0 = 0; r0 < rows; r0 += 16) {
-        // operand row i16 of the block, and log-sum-exp and position of the four rows of this lane's results
-        auto place = [&](int r, int &t) {                 // token and head of row r
-            t = (int)(((float)r + 0.5f) * p.g_rcp);       // (r / G: half a row is far more than the product's rounding)
+    // this lane's part of a copy: 16 bytes of row i * kRowsPerCopy + lane / kChunks, chunks swizzled by row
+    unsigned copy_off[kCopies];
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) {
+        const int r = i * kRowsPerCopy + lane / kChunks;
+        copy_off[i] = r * kRowBytes + (((lane % kChunks) ^ swizzle_k<D>(r)) << 4);
+    }
+    char *const s_page = s_ring[wave];
+    const unsigned page_lds = (unsigned)(size_t)(lds_char *)s_page;
+    // Page `pg` of turn `turn` on its way to its place in the ring: kCopies instructions, whatever it is (a page that is not
+    // there reads page 0, whose weights are dropped).
+    auto copy_page = [&](int turn, int pg) {
+        const int id = __builtin_amdgcn_readlane(page, turn * kTurnPages + pg);
+        const char *base = reinterpret_cast<const char *>(p.k_cache) + ((size_t)max(id, 0) * p.Hkv + hkv) * kPageBytes;
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) copy16_uniform(base, copy_off[i], page_lds + pg * kPageBytes + i * 1024);
+    };
+    // what the keys of a turn have so far, by the same way: a load into a register would be waited for together with all copies
+    auto copy_old = [&](int turn) {
+        const float *src = weights + min(key0 + turn * kTurnKeys + lane, p.max_positions - 1);
+        const unsigned dst = (unsigned)(size_t)(lds_char *)reinterpret_cast<char *>(s_old[turn & 1]);
+        asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" :: "v"(src), "s"(dst) : "memory", "m0");
+    };
+
+    for (int r_all = 0; r_all < rows; r_all += kWaves * kBlocks * 16) {
+        const int r_base = r_all + wave * kBlocks * 16;
+        if (wave == 0) copy_old(0);
+#pragma unroll
+        for (int pg = 0; pg < kTurnPages; ++pg) copy_page(0, pg);
+        // the query rows as operands: block k, step s: row i16, values 32 s + 8 quad .. + 7; log-sum-exp (in
+        // powers of two) of the four rows of this lane's results
+        bf16x8 q[kBlocks][kSteps];
+        float ref[kBlocks][4];
+        auto place = [&](int r, int &t) {                // token and head of row r (half a row is far more than the product's rounding)
+            t = (int)(((float)r + 0.5f) * p.g_rcp);
             return hkv * p.G + r - t * p.G;
         };
-        int t;
-        const int rq = min(r0 + i16, rows - 1);
-        const int head = place(rq, t);
-        const size_t row = p.path ? (size_t)b * p.T + p.path[(size_t)b * p.max_path + t] : (size_t)token0 + t;
-        const uint16_t *q = p.q + (row * p.Hq + head) * D + quad * 8;
-        bf16x8 a[kSteps];
+        const int top = rows - 1;
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) a[s] = __builtin_bit_cast(bf16x8, ld16(q + s * 32));
-        float ref[4];
-        int last[4];
+        for (int k = 0; k < kBlocks; ++k) {
+            int t;
+            const int head = place(min(r_base + k * 16 + i16, top), t);
+            const size_t at = p.path ? (size_t)b * p.T + path[t] : (size_t)token0 + t;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = r0 + quad * 4 + i;
-            int ti;
-            const int hi = place(min(r, rows - 1), ti);
-            const float lse = p.path ? p.lse[((size_t)b * p.Hq + hi) * p.T + p.path[(size_t)b * p.max_path + ti]]
-                                     : p.lse[((size_t)token0 + ti) * p.Hq + hi];
-            // (a row behind the last one, and one that saw no key at all, gives nothing)
-            ref[i] = r < rows && lse != -INFINITY ? lse * 1.44269504088896340736f : INFINITY;
-            last[i] = first + ti;
-        }
-#pragma unroll
-        for (int pg = 0; pg < 4; ++pg) {
-            f32x4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[s], k[pg][s], x, 0, 0, 0);
+            for (int s = 0; s < kSteps; ++s) q[k][s] = __builtin_bit_cast(bf16x8, ld16(p.q + (at * p.Hq + head) * D + s * 32 + quad * 8));
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                float w = __builtin_amdgcn_exp2f(x[i] * p.scale_log2 - ref[i]);
-                if (causal && j0 + pg * 16 + i16 > last[i]) w = 0.f;
-                acc[pg] += w;
+                const int r = r_base + k * 16 + quad * 4 + i;
+                int ti;
+                const int hi = place(min(r, top), ti);
+                const float lse = p.path ? p.lse[((size_t)b * p.Hq + hi) * p.T + path[ti]] : p.lse[((size_t)token0 + ti) * p.Hq + hi];
+                // (a row behind the last one, and one that saw no key at all, gives nothing)
+                ref[k][i] = r < rows && lse != -INFINITY ? lse * 1.44269504088896340736f : INFINITY;
             }
         }
-    }
-    // a key's four quarters of the rows sit 16 lanes apart
+        for (int turn = 0; turn < turns; ++turn) {
+            const int j0 = key0 + turn * kTurnKeys, j_mine = j0 + lane;
+            const bool more = turn + 1 < turns;
+            const bool causal = j0 + kTurnKeys > first + 1;      // some row does not see some of these keys
+            float acc[kTurnPages];
 #pragma unroll
-    for (int pg = 0; pg < 4; ++pg) {
-        acc[pg] += __shfl_xor(acc[pg], 16);
-        acc[pg] += __shfl_xor(acc[pg], 32);
+            for (int pg = 0; pg < kTurnPages; ++pg) {
+                // behind this page's copies stand those of three more pages (or nothing is on its way any more)
+                if (more) wait_vmcnt<(kTurnPages - 1) * kCopies>();
+                else wait_vmcnt<0>();
+                asm volatile("" ::: "memory");
+                bf16x8 key[kSteps];
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s)
+                    key[s] = *reinterpret_cast<const bf16x8 *>(s_page + pg * kPageBytes + i16 * kRowBytes + (((4 * s + quad) ^ swizzle_k<D>(i16)) << 4));
+                // (the rows are in registers before the next turn's go to their place)
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s) asm volatile("" : "+v"(key[s]) :: "memory");
+                if (more) {
+                    if (pg == 0 && wave == 0) copy_old(turn + 1);
+                    copy_page(turn + 1, pg);
+                }
+                float sum = 0.f;
+                auto add = [&](auto &&sees) {
+#pragma unroll
+                    for (int k = 0; k < kBlocks; ++k) {
+                        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int s = 0; s < kSteps; ++s) x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[k][s], key[s], x, 0, 0, 0);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float w = __builtin_amdgcn_exp2f(x[i] * p.scale_log2 - ref[k][i]);
+                            sum += sees(k, i) ? w : 0.f;
+                        }
+                    }
+                };
+                if (causal)
+                    add([&](int k, int i) {
+                        int t;
+                        place(r_base + k * 16 + quad * 4 + i, t);
+                        return j0 + pg * 16 + i16 <= first + t;
+                    });
+                else add([](int, int) { return true; });
+                acc[pg] = sum;
+            }
+            // a key's four quarters of the rows sit 16 lanes apart; lane l then takes key l of the turn
+            float sum = 0.f;
+#pragma unroll
+            for (int pg = 0; pg < kTurnPages; ++pg) {
+                acc[pg] += __shfl_xor(acc[pg], 16);
+                acc[pg] += __shfl_xor(acc[pg], 32);
+                sum = quad == pg ? acc[pg] : sum;
+            }
+            if constexpr (kWaves > 1) {
+                s_sum[turn & 1][wave][lane] = sum;
+                __syncthreads();
+                if (wave > 0) continue;
+#pragma unroll
+                for (int w = 1; w < kWaves; ++w) sum += s_sum[turn & 1][w][lane];
+            }
+            const float old = s_old[turn & 1][lane];
+            const bool ok = __shfl(page, turn * kTurnPages + quad) >= 0;
+            if (j_mine < keys) weights[j_mine] = (r_all > 0 ? old : p.decay == 0.f ? 0.f : p.decay * old) + (ok ? sum : 0.f);
+        }
+        wait_vmcnt<0>();                                 // (what has been written is read again for the next rows)
+        asm volatile("" ::: "memory");
     }
-    const float sum = quad == 0 ? acc[0] : quad == 1 ? acc[1] : quad == 2 ? acc[2] : acc[3];
-    const bool ok = quad == 0 ? page_ok[0] : quad == 1 ? page_ok[1] : quad == 2 ? page_ok[2] : page_ok[3];
-    if (j_mine < keys) weights[j_mine] = mine + (ok ? sum : 0.f);
-    else if (p.decay == 0.f && j_mine < p.max_positions) weights[j_mine] = 0.f;
-    if (bad && p.status && lane == 0) atomicOr(p.status, bad);
+}
+
+template <int D, int kBlocks, int kWaves>
+hipError_t launch_blocks(const KeyWeightsParams &p, int span, hipStream_t stream) {
+    // turns of a wavefront: as many as leave the chip filled
+    const long long all = (long long)((span + kTurnKeys - 1) / kTurnKeys) * p.Hkv * p.B;
+    // (8 wavefronts a compute unit run at a time)
+    const long long n = all * kWaves / (kNumCU * 8);
+    const int turns = (int)(n < 1 ? 1 : n > kMaxTurns ? kMaxTurns : n);
+    const dim3 grid((unsigned)((span + turns * kTurnKeys - 1) / (turns * kTurnKeys)), (unsigned)p.Hkv, (unsigned)p.B);
+    hipLaunchKernelGGL((key_weights_kernel<D, kBlocks, kWaves>), grid, dim3(64 * kWaves), 0, stream, p, turns);
+    return note_hip_error("launch key_weights_kernel", hipGetLastError());
+}
+
+template <int D>
+hipError_t launch_rows(const KeyWeightsParams &p, int span, hipStream_t stream) {
+    const long long rows = (long long)(p.path ? p.max_path : p.window) * p.G;      // no sequence has more
+    if (rows <= 16) return launch_blocks<D, 1, 1>(p, span, stream);
+    if (rows <= 32) return launch_blocks<D, 2, 1>(p, span, stream);
+    if (rows <= 64) return launch_blocks<D, 4, 1>(p, span, stream);
+    if (rows <= 128) return launch_blocks<D, 8, 1>(p, span, stream);
+    if (rows <= 256) return launch_blocks<D, 8, 2>(p, span, stream);
+    return launch_blocks<D, 8, 4>(p, span, stream);
 }
 
 }  // namespace
@@ -139,10 +234,7 @@ __global__ __launch_bounds__(kWeightsThreads) void key_weights_kernel(KeyWeights
 hipError_t launch_key_weights(const KeyWeightsParams &p, hipStream_t stream) {
     const int span = p.decay == 0.f ? p.max_positions : min(p.max_seq_len, p.max_positions);   // (a fresh start clears the whole row)
     if (span <= 0) return hipSuccess;
-    const dim3 grid((unsigned)((span + kKeysPerWg - 1) / kKeysPerWg), (unsigned)p.Hkv, (unsigned)p.B);
-    if (p.D == 64) hipLaunchKernelGGL(key_weights_kernel<64>, grid, dim3(kWeightsThreads), 0, stream, p);
-    else hipLaunchKernelGGL(key_weights_kernel<128>, grid, dim3(kWeightsThreads), 0, stream, p);
-    return note_hip_error("launch key_weights_kernel", hipGetLastError());
+    return p.D == 64 ? launch_rows<64>(p, span, stream) : launch_rows<128>(p, span, stream);
 }
 
 }  // namespace reader

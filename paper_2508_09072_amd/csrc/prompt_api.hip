@@ -125,12 +125,12 @@ extern "C" int reader_prompt_attn(const reader_dims *dims, int32_t N, const void
                ? READER_OK : READER_EHIP;
 }
 
-static int key_weights_prepare(const reader_dims *dims, const void *q, const float *lse, const void *k_cache,
+static int key_weights_prepare(const reader_dims *dims, int32_t rows, const void *q, const float *lse, const void *k_cache,
                                const int32_t *page_table, const int32_t *seq_lens, float decay, float *weights,
                                int32_t max_positions, int32_t max_seq_len, int32_t *status, KeyWeightsParams &p) {
     if (max_positions < 0 || max_seq_len < 0 || !(decay >= 0.f && decay <= 1.f)) return READER_EINVAL;
     if (dims->Hkv > 65535) return READER_EUNSUPPORTED;                    // (a dimension of the grid)
-    if (!q || !lse || !seq_lens || !weights || !cache_ok(dims, k_cache, k_cache, page_table)) return READER_EINVAL;
+    if ((rows > 0 && (!q || !lse)) || !seq_lens || !weights || !cache_ok(dims, k_cache, k_cache, page_table)) return READER_EINVAL;
     p.q = (const uint16_t *)q; p.lse = lse; p.k_cache = (const uint16_t *)k_cache;
     p.page_table = page_table; p.seq_lens = seq_lens; p.weights = weights; p.status = status;
     p.B = dims->B; p.T = dims->T; p.Hq = dims->Hq; p.Hkv = dims->Hkv; p.G = dims->Hq / dims->Hkv; p.D = dims->D;
@@ -148,7 +148,7 @@ extern "C" int reader_key_weights(const reader_dims *dims, const void *q, const 
     if (!dims_ok(dims, &err)) return err;
     if (dims->B == 0) return READER_OK;
     KeyWeightsParams p = {};
-    const int rc = key_weights_prepare(dims, q, lse, k_cache, page_table, seq_lens, decay, weights, max_positions, max_seq_len, status, p);
+    const int rc = key_weights_prepare(dims, dims->B, q, lse, k_cache, page_table, seq_lens, decay, weights, max_positions, max_seq_len, status, p);
     if (rc != READER_OK) return rc;
     if (!path || !accept_len) return READER_EINVAL;
     p.path = path; p.accept_len = accept_len;
@@ -168,7 +168,7 @@ extern "C" int reader_prompt_key_weights(const reader_dims *dims, int32_t N, con
     if (window > READER_MAX_WINDOW) return READER_EUNSUPPORTED;
     if (dims->B == 0) return READER_OK;
     KeyWeightsParams p = {};
-    rc = key_weights_prepare(dims, q, lse, k_cache, page_table, seq_lens, decay, weights, max_positions, max_seq_len, status, p);
+    rc = key_weights_prepare(dims, N, q, lse, k_cache, page_table, seq_lens, decay, weights, max_positions, max_seq_len, status, p);
     if (rc != READER_OK) return rc;
     if (!cu_tokens) return READER_EINVAL;
     p.cu_tokens = cu_tokens; p.N = N; p.window = window;
