@@ -38,6 +38,15 @@ static bool cache_ok(const reader_dims *dims, const void *k_cache, const void *v
     return k_cache && v_cache && page_table && dims->num_pages >= 1 && dims->max_pages_per_seq >= 1;
 }
 
+// Which kernel: by the query rows that a sequence has for each kv head, on average (the host knows no more).
+static hipError_t launch_prompt(const PromptParams &p, int variant, hipStream_t stream) {
+    if (variant == 1) return launch_prompt_attn_scalar(p, stream);
+    const long long rows = (long long)p.N * p.G;
+    if (rows <= 16LL * p.B) return launch_prompt_few(p, 16, stream);
+    if (rows <= 32LL * p.B) return launch_prompt_few(p, 32, stream);
+    return launch_prompt_wide(p, stream);
+}
+
 }  // namespace reader
 
 using namespace reader;
@@ -89,7 +98,8 @@ extern "C" int reader_prompt_qkv(const reader_dims *dims, int32_t N, const void 
 extern "C" size_t reader_prompt_workspace_bytes(const reader_dims *dims, int32_t N, int32_t max_seq_len) {
     int err = 0;
     if (!dims_ok(dims, &err) || rows_ok(dims, N) != READER_OK || max_seq_len < 0) return 0;
-    return prompt_workspace_bytes(dims->D);
+    const size_t wide = prompt_wide_workspace_bytes(dims->D), few = prompt_few_workspace_bytes(dims->D);
+    return ((wide > few ? wide : few) + 255) & ~(size_t)255;
 }
 
 extern "C" int reader_prompt_attn(const reader_dims *dims, int32_t N, const void *q, const void *k_cache, const void *v_cache,
@@ -118,11 +128,8 @@ extern "C" int reader_prompt_attn(const reader_dims *dims, int32_t N, const void
         if (workspace_bytes < reader_prompt_workspace_bytes(dims, N, max_seq_len)) return READER_EWORKSPACE;
     }
     p.g_rcp = 1.0f / (float)p.G;
-    p.tokens_per_block = 256 / p.G;
-    p.n_ranges = kNumCU;
     forget_stale_error();
-    return (dims->variant == 1 ? launch_prompt_attn_scalar(p, (hipStream_t)stream) : launch_prompt_attn(p, (hipStream_t)stream)) == hipSuccess
-               ? READER_OK : READER_EHIP;
+    return launch_prompt(p, dims->variant, (hipStream_t)stream) == hipSuccess ? READER_OK : READER_EHIP;
 }
 
 static int key_weights_prepare(const reader_dims *dims, int32_t rows, const void *q, const float *lse, const void *k_cache,

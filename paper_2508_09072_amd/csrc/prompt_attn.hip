@@ -19,6 +19,7 @@
 #include <mutex>
 
 #include "prompt_attn_scalar.h"
+#include "prompt_ranges.h"
 #include "wide_registers.h"
 
 namespace reader {
@@ -32,6 +33,7 @@ constexpr int kPromptSeqsInLds = 2048;               // batches up to this size 
 // and writing behind), when the axis is cut.
 constexpr int kBlockFront = 3 * kTile, kBlockCost = 6 * kTile;
 constexpr int kMinRange = 4 * kTile;                 // no range is shorter than this: a range costs as much before its first tile
+using Block = PromptBlock<kTile, kBlockFront, kBlockCost>;
 
 // One tile of a workgroup's list.
 struct PromptTile {
@@ -51,56 +53,8 @@ enum {
     kTileHoles = 32,      // quarters behind a page id that does not exist
 };
 
-// What a range leaves for the launch behind it.
-struct RangeNote {
-    int tiles;            // 0: no record
-    int ends;             // its first segment continues a block of an earlier range, and ends it
-    int open;             // its last segment starts a block and does not end it: the block is
-    int head, row0, nt;   // ... this one
-    int pad[2];
-};
-constexpr size_t kNotesBytes = (size_t)kNumCU * sizeof(RangeNote);
 __host__ __device__ constexpr size_t prompt_record_floats(int D) { return (size_t)kPromptRows * (D + 2); }
 
-// Lengths and bounds of the sequences, from LDS or from memory.
-struct Sequences {
-    const int32_t *lens, *cu;
-    int N, max_len;
-    // (rows behind the bound on the lengths see what lies in front of it)
-    __device__ __forceinline__ int length(int b) const { return min(max(lens[b], 0), max_len); }
-    __device__ __forceinline__ int first(int b) const { return clamp_row(cu[b], N); }
-    __device__ __forceinline__ int tokens(int b) const { return max(clamp_row(cu[b + 1], N) - first(b), 0); }
-};
-
-// A block of query rows, and a walk over the blocks of a range.
-struct Block {
-    int head, b, k;       // kv head, sequence, number of the block there
-    int L, n, c0;         // the sequence: cached positions, new tokens, first packed row
-    __device__ __forceinline__ void load(const Sequences &s) { L = s.length(b); n = s.tokens(b); c0 = s.first(b); }
-    __device__ __forceinline__ int tokens(int tb) const { return min(tb, n - k * tb); }
-    // keys that the block's last token sees
-    __device__ __forceinline__ int keys(int tb, int max_len) const {
-        const long long end = (long long)L + k * tb + tokens(tb);
-        return (int)(end < max_len ? end : max_len);
-    }
-    __device__ __forceinline__ int tiles(int tb, int max_len) const { return max(1, (keys(tb, max_len) + kTile - 1) / kTile); }
-    __device__ __forceinline__ void next(const Sequences &s, int B, int tb) {
-        if (++k * tb < n) return;
-        k = 0;
-        do {
-            if (++b == B) { b = 0; ++head; }
-        } while (s.tokens(b) == 0);          // (some sequence has tokens, or there would be no block)
-        load(s);
-    }
-};
-
-// cost of the first k blocks of a sequence, none of them its last
-__device__ __forceinline__ long long blocks_cost(int L, int tb, long long k) { return k * ((long long)L + kBlockCost) + tb * (k * (k + 1) / 2); }
-__device__ __forceinline__ long long sequence_cost(int L, int n, int tb) {
-    if (n <= 0) return 0;
-    const long long nb = (n + tb - 1) / tb;
-    return blocks_cost(L, tb, nb - 1) + (long long)L + kBlockCost + n;
-}
 }  // namespace
 
 template <int D>
@@ -149,7 +103,7 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
                     if (b == p.B - 1) s_seq[2 * p.B] = hi;
                 }
                 const int nn = seqs.tokens(b);
-                c = sequence_cost(seqs.length(b), nn, tb);
+                c = Block::sequence_cost(seqs.length(b), nn, tb);
                 if (len < 0 || lo < 0 || hi < lo || hi > p.N || (long long)len + nn > p.max_seq_len) bad |= READER_STATUS_BAD_LENGTH;
             }
 #pragma unroll
@@ -182,88 +136,34 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
         return;
     }
     // first tile at or behind position x of the axis
-    auto locate = [&](long long x, int &t) {
-        Block o;
+    auto locate = [&](long long x, Block &o) {
         if (x >= total) {
-            o.head = p.Hkv; o.b = 0; o.k = 0; o.L = o.n = o.c0 = 0;
-            t = 0;
-            return o;
+            o = Block{p.Hkv, 0, 0, 0, 0, 0};
+            return 0;
         }
         o.head = (int)(x / per_head);
-        long long r = x - o.head * per_head;
+        const long long r = x - o.head * per_head;
         int lo = 0, hi = p.B - 1;
         while (lo < hi) {                            // last sequence that starts at or in front of r
             const int mid = (lo + hi + 1) >> 1;
             if (s_pref[mid] <= r) lo = mid; else hi = mid - 1;
         }
         o.b = lo;
-        r -= s_pref[lo];
         o.load(seqs);
-        const int nb = (o.n + tb - 1) / tb;
-        // k with blocks_cost(k) <= r < blocks_cost(k + 1): the root of a parabola, then a step either way for its rounding
-        const double a = 0.5 * tb, q = (double)o.L + kBlockCost + a;
-        long long k = (long long)((sqrt(q * q + 4.0 * a * (double)r) - q) / (2.0 * a));
-        k = k < 0 ? 0 : (k > nb - 1 ? nb - 1 : k);
-        while (k > 0 && blocks_cost(o.L, tb, k) > r) --k;
-        while (k < nb - 1 && blocks_cost(o.L, tb, k + 1) <= r) ++k;
-        o.k = (int)k;
-        const long long keys_in = r - blocks_cost(o.L, tb, k) - kBlockFront;
-        const int tiles = o.tiles(tb, p.max_seq_len);
-        t = keys_in <= 0 ? 0 : (int)((keys_in + kTile - 1) / kTile < tiles ? (keys_in + kTile - 1) / kTile : tiles);
-        if (t == tiles) {                            // behind the block's tiles: the next block's first
-            t = 0;
-            o.next(seqs, p.B, tb);                   // (may step behind the last head: the end)
-        }
-        return o;
+        return o.locate(r - s_pref[lo], seqs, p.B, tb);
     };
-    int t_lo, t_hi;
-    Block at = locate(range * total / n_ranges, t_lo), stop = locate((range + 1) * total / n_ranges, t_hi);
-    auto uniform = [](Block &o) {
-        o.head = __builtin_amdgcn_readfirstlane(o.head); o.b = __builtin_amdgcn_readfirstlane(o.b); o.k = __builtin_amdgcn_readfirstlane(o.k);
-        o.L = __builtin_amdgcn_readfirstlane(o.L); o.n = __builtin_amdgcn_readfirstlane(o.n); o.c0 = __builtin_amdgcn_readfirstlane(o.c0);
-    };
-    uniform(at);
-    t_lo = __builtin_amdgcn_readfirstlane(t_lo);
-    t_hi = __builtin_amdgcn_readfirstlane(t_hi);
-    const int stop_head = __builtin_amdgcn_readfirstlane(stop.head), stop_b = __builtin_amdgcn_readfirstlane(stop.b);
-    const int stop_k = __builtin_amdgcn_readfirstlane(stop.k);
-    auto is_stop = [&](const Block &o) { return o.head == stop_head && (o.head == p.Hkv || (o.b == stop_b && o.k == stop_k)); };
-    // tiles of a block that belong to this range, [from, to)
-    auto share = [&](const Block &o, bool first, int &from, int &to) {
-        from = first ? t_lo : 0;
-        to = is_stop(o) ? t_hi : o.tiles(tb, p.max_seq_len);
-    };
-    // the range's tiles, and what it leaves to the merge
-    int n_iter = 0;
-    {
-        RangeNote note = {};
-        Block o = at;
-        for (bool first = true;; first = false) {
-            if (o.head >= p.Hkv || (is_stop(o) && t_hi == 0)) break;
-            int from, to;
-            share(o, first, from, to);
-            const int tiles = o.tiles(tb, p.max_seq_len);
-            if (to > from) {
-                n_iter += to - from;
-                if (from > 0 && to == tiles) note.ends = 1;
-                if (from == 0 && to < tiles) {
-                    note.open = 1;
-                    note.head = o.head; note.row0 = o.c0 + o.k * tb; note.nt = o.tokens(tb);
-                }
-            }
-            if (is_stop(o)) break;
-            o.next(seqs, p.B, tb);
-        }
-        note.tiles = n_iter;
-        if (tid == 0) notes[range] = note;
-    }
-    n_iter = __builtin_amdgcn_readfirstlane(n_iter);
+    Block from, to;
+    const int t_from = locate(range * total / n_ranges, from), t_to = locate((range + 1) * total / n_ranges, to);
+    const PromptRange<Block> rg(from, t_from, to, t_to, p.Hkv);
+    const RangeNote note = rg.note(seqs, p.B, tb);
+    if (tid == 0) notes[range] = note;
+    const int n_iter = __builtin_amdgcn_readfirstlane(note.tiles);
     if (n_iter == 0) return;
     __syncthreads();                                 // (everybody is done with the prefix sums: the ring is free)
 
     // ---- the tile list
     // Item i, found by walking the blocks from `walk`, whose first tile in the range is item walk_item; a thread each.
-    Block walk = at;
+    Block walk = rg.at;
     int walk_item = 0;
     bool walk_first = true;
     auto write_item = [&](int i) {
@@ -271,7 +171,7 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
         bool first = walk_first;
         int from, to, item = walk_item;
         for (;;) {
-            share(o, first, from, to);
+            rg.share(o, first, tb, p.max_seq_len, from, to);
             if (i < item + (to - from)) break;
             item += to - from;
             first = false;
@@ -302,12 +202,12 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
     auto move_walk = [&](int item) {
         for (;;) {
             int from, to;
-            share(walk, walk_first, from, to);
+            rg.share(walk, walk_first, tb, p.max_seq_len, from, to);
             if (item < walk_item + (to - from)) break;
             walk_item += to - from;
             walk_first = false;
             walk.next(seqs, p.B, tb);
-            uniform(walk);
+            walk.make_uniform();
         }
     };
     __syncthreads();   // the list is written
@@ -860,55 +760,6 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
     if (p.status && bad) atomicOr(p.status, bad);
 }
 
-// Blocks that were cut: the ranges that hold a part of one follow one another, the first has noted it as open, the last as ended.
-// A workgroup takes the block that its range left open, and a slice of the columns; a thread a row.
-constexpr int kMergeColumns = 16;
-template <int D>
-__global__ __launch_bounds__(kPromptRows) void prompt_merge_kernel(PromptParams p) {
-    const RangeNote *notes = reinterpret_cast<const RangeNote *>(p.workspace);
-    const int range = blockIdx.x, slice = blockIdx.y, row = threadIdx.x;
-    const RangeNote mine = notes[range];
-    if (!mine.open) return;
-    const float *records = reinterpret_cast<const float *>(reinterpret_cast<const char *>(p.workspace) + kNotesBytes);
-    const int tok = (int)(((float)row + 0.5f) * p.g_rcp), g = row - tok * p.G;
-    constexpr int kChunks = kMergeColumns / 4;
-    float m = -INFINITY, l = 0.f;
-    float4 acc[kChunks] = {};
-    for (int w = range; w < p.n_ranges; ++w) {
-        const RangeNote note = w == range ? mine : notes[w];
-        if (note.tiles == 0) continue;
-        const float *rec = records + (size_t)(2 * w + (w == range ? 1 : 0)) * prompt_record_floats(D);
-        const float m2 = rec[(size_t)kPromptRows * D + row], l2 = rec[(size_t)kPromptRows * (D + 1) + row];
-        const float4 *from = reinterpret_cast<const float4 *>(rec) + (size_t)slice * kChunks * kPromptRows + row;
-        float4 v[kChunks];
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c) v[c] = from[(size_t)c * kPromptRows];
-        // (a part that the row sees nothing of has a sum of zero; a sum that is not a number shows)
-        if (l2 != 0.f) {
-            const float m_new = fmaxf(m, m2);
-            const float a = l == 0.f ? 0.f : l * __builtin_amdgcn_exp2f(m - m_new), b = l2 * __builtin_amdgcn_exp2f(m2 - m_new);
-            const float inv = 1.f / (a + b);
-            const float fa = a * inv, fb = b * inv;
-#pragma unroll
-            for (int c = 0; c < kChunks; ++c) {
-                acc[c].x = acc[c].x * fa + v[c].x * fb; acc[c].y = acc[c].y * fa + v[c].y * fb;
-                acc[c].z = acc[c].z * fa + v[c].z * fb; acc[c].w = acc[c].w * fa + v[c].w * fb;
-            }
-            m = m_new;
-            l = a + b;
-        }
-        if (w != range && note.ends) break;
-    }
-    if (row >= p.tokens_per_block * p.G || tok >= mine.nt) return;
-    const size_t out_row = ((size_t)mine.row0 + tok) * p.Hq + (size_t)mine.head * p.G + g;
-    uint16_t *out = p.out + out_row * D + slice * kMergeColumns;
-#pragma unroll
-    for (int c = 0; c < kChunks; c += 2)
-        *reinterpret_cast<uint4 *>(out + c * 4) = make_uint4(pack_bf16x2(acc[c].x, acc[c].y), pack_bf16x2(acc[c].z, acc[c].w),
-                                                             pack_bf16x2(acc[c + 1].x, acc[c + 1].y), pack_bf16x2(acc[c + 1].z, acc[c + 1].w));
-    if (slice == 0 && p.lse) p.lse[out_row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
-}
-
 template <int D>
 static hipError_t launch_prompt(const PromptParams &p, hipStream_t stream) {
     using G = Geometry<D, 4>;
@@ -926,15 +777,17 @@ static hipError_t launch_prompt(const PromptParams &p, hipStream_t stream) {
         }
     }
     hipLaunchKernelGGL((prompt_attn_kernel<D>), dim3(p.n_ranges), dim3(kPromptThreads), lds, stream, p, p.page_table);
-    hipError_t e = hipGetLastError();
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return note_hip_error("launch prompt_attn_kernel", e);
-    hipLaunchKernelGGL((prompt_merge_kernel<D>), dim3(p.n_ranges, D / kMergeColumns), dim3(kPromptRows), 0, stream, p);
-    return note_hip_error("launch prompt_merge_kernel", hipGetLastError());
+    return launch_prompt_merge(p, kPromptRows, stream);
 }
 
-size_t prompt_workspace_bytes(int D) { return kNotesBytes + (size_t)2 * kNumCU * prompt_record_floats(D) * sizeof(float); }
+size_t prompt_wide_workspace_bytes(int D) { return kNotesBytes + (size_t)2 * kNumCU * prompt_record_floats(D) * sizeof(float); }
 
-hipError_t launch_prompt_attn(const PromptParams &p, hipStream_t stream) {
+hipError_t launch_prompt_wide(const PromptParams &params, hipStream_t stream) {
+    PromptParams p = params;
+    p.tokens_per_block = kPromptRows / p.G;
+    p.n_ranges = kNumCU;
     return p.D == 64 ? launch_prompt<64>(p, stream) : launch_prompt<128>(p, stream);
 }
 

@@ -48,11 +48,16 @@ struct PromptParams {
     int64_t num_pages;
     float scale_log2;              // softmax scale * log2(e)
     float g_rcp;                   // 1 / G
-    int32_t tokens_per_block;      // (matrix kernel) tokens whose heads fill a block of query rows
+    int32_t tokens_per_block;      // (matrix kernels) tokens whose heads fill a block of query rows
     int32_t n_ranges;              // ... and workgroups of the launch
 };
-size_t prompt_workspace_bytes(int D);
-hipError_t launch_prompt_attn(const PromptParams &p, hipStream_t stream);
+// 256 rows a workgroup (prompt_attn.hip); 16 or 32 rows a wavefront (prompt_attn_few.hip); what both leave is folded by a second
+// launch (prompt_merge.hip)
+size_t prompt_wide_workspace_bytes(int D);
+hipError_t launch_prompt_wide(const PromptParams &p, hipStream_t stream);
+size_t prompt_few_workspace_bytes(int D);
+hipError_t launch_prompt_few(const PromptParams &p, int rows, hipStream_t stream);
+hipError_t launch_prompt_merge(const PromptParams &p, int record_rows, hipStream_t stream);
 hipError_t launch_prompt_attn_scalar(const PromptParams &p, hipStream_t stream);
 
 struct KeyWeightsParams {

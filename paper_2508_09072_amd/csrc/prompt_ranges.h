@@ -1,0 +1,129 @@
+// The (head, sequence, block of query rows, key) axis of the prompts' attention, and what the ranges it is cut into leave for the
+// launch that folds their parts together.
+#pragma once
+
+#include "prompt_common.h"
+
+namespace reader {
+
+namespace {
+
+// What a range leaves for the launch behind it.
+struct RangeNote {
+    int tiles;            // 0: no record
+    int ends;             // its first segment continues a block of an earlier range, and ends it
+    int open;             // its last segment starts a block and does not end it: the block is
+    int head, row0, nt;   // ... this one: kv head, first packed row, tokens
+    int pad[2];
+};
+constexpr int kMaxRanges = kNumCU * 8;
+constexpr size_t kNotesBytes = (size_t)kMaxRanges * sizeof(RangeNote);   // in front of the records, two a range
+
+// Lengths and bounds of the sequences, from LDS or from memory.
+struct Sequences {
+    const int32_t *lens, *cu;
+    int N, max_len;
+    // (rows behind the bound on the lengths see what lies in front of it)
+    __device__ __forceinline__ int length(int b) const { return min(max(lens[b], 0), max_len); }
+    __device__ __forceinline__ int first(int b) const { return clamp_row(cu[b], N); }
+    __device__ __forceinline__ int tokens(int b) const { return max(clamp_row(cu[b + 1], N) - first(b), 0); }
+};
+
+// A block of query rows: `tb` tokens of a sequence (the last one of it: what is left) with all query heads of a kv head.  On the
+// axis it takes as many positions as its last token sees keys, and kCost for what it costs beyond them: positions of a
+// sequence's blocks add up to a closed form.
+template <int kTileKeys, int kFront, int kCost>
+struct PromptBlock {
+    int head, b, k;       // kv head, sequence, number of the block there
+    int L, n, c0;         // the sequence: cached positions, new tokens, first packed row
+    __device__ __forceinline__ void load(const Sequences &s) { L = s.length(b); n = s.tokens(b); c0 = s.first(b); }
+    __device__ __forceinline__ int tokens(int tb) const { return min(tb, n - k * tb); }
+    // keys that the block's last token sees
+    __device__ __forceinline__ int keys(int tb, int max_len) const {
+        const long long end = (long long)L + k * tb + tokens(tb);
+        return (int)(end < max_len ? end : max_len);
+    }
+    __device__ __forceinline__ int tiles(int tb, int max_len) const { return max(1, (keys(tb, max_len) + kTileKeys - 1) / kTileKeys); }
+    __device__ __forceinline__ void next(const Sequences &s, int B, int tb) {
+        if (++k * tb < n) return;
+        k = 0;
+        do {
+            if (++b == B) { b = 0; ++head; }
+        } while (s.tokens(b) == 0);          // (some sequence has tokens, or there would be no block)
+        load(s);
+    }
+    // positions of the first k blocks of a sequence, none of them its last; of all of them
+    __device__ static __forceinline__ long long blocks_cost(int L, int tb, long long k) { return k * ((long long)L + kCost) + tb * (k * (k + 1) / 2); }
+    __device__ static __forceinline__ long long sequence_cost(int L, int n, int tb) {
+        if (n <= 0) return 0;
+        const long long nb = (n + tb - 1) / tb;
+        return blocks_cost(L, tb, nb - 1) + (long long)L + kCost + n;
+    }
+    // The first tile at or behind position r of this sequence's part of the axis (head, b and what load() reads are set): its
+    // block is set, its number returned.  Positions behind the block's tiles: the next block's first.
+    __device__ __forceinline__ int locate(long long r, const Sequences &s, int B, int tb) {
+        const int nb = (n + tb - 1) / tb;
+        // k with blocks_cost(k) <= r < blocks_cost(k + 1): the root of a parabola, then a step either way for its rounding
+        const double a = 0.5 * tb, q = (double)L + kCost + a;
+        long long i = (long long)((sqrt(q * q + 4.0 * a * (double)r) - q) / (2.0 * a));
+        i = i < 0 ? 0 : (i > nb - 1 ? nb - 1 : i);
+        while (i > 0 && blocks_cost(L, tb, i) > r) --i;
+        while (i < nb - 1 && blocks_cost(L, tb, i + 1) <= r) ++i;
+        k = (int)i;
+        const long long in = r - blocks_cost(L, tb, i) - kFront;
+        const int all = tiles(tb, s.max_len);
+        const int t = in <= 0 ? 0 : (int)((in + kTileKeys - 1) / kTileKeys < all ? (in + kTileKeys - 1) / kTileKeys : all);
+        if (t < all) return t;
+        next(s, B, tb);                      // (may step behind the last head: the end)
+        return 0;
+    }
+    // every lane of the wavefront has the same
+    __device__ __forceinline__ void make_uniform() {
+        head = __builtin_amdgcn_readfirstlane(head); b = __builtin_amdgcn_readfirstlane(b); k = __builtin_amdgcn_readfirstlane(k);
+        L = __builtin_amdgcn_readfirstlane(L); n = __builtin_amdgcn_readfirstlane(n); c0 = __builtin_amdgcn_readfirstlane(c0);
+    }
+};
+
+// A range: from tile t_lo of block `at` up to tile t_hi of block `stop`.
+template <class Block>
+struct PromptRange {
+    Block at;
+    int t_lo, t_hi, stop_head, stop_b, stop_k, heads;
+    __device__ __forceinline__ PromptRange(const Block &from, int t_from, const Block &to, int t_to, int Hkv) : at(from), heads(Hkv) {
+        at.make_uniform();
+        t_lo = __builtin_amdgcn_readfirstlane(t_from); t_hi = __builtin_amdgcn_readfirstlane(t_to);
+        stop_head = __builtin_amdgcn_readfirstlane(to.head); stop_b = __builtin_amdgcn_readfirstlane(to.b); stop_k = __builtin_amdgcn_readfirstlane(to.k);
+    }
+    __device__ __forceinline__ bool is_stop(const Block &o) const { return o.head == stop_head && (o.head == heads || (o.b == stop_b && o.k == stop_k)); }
+    __device__ __forceinline__ bool behind(const Block &o) const { return o.head >= heads || (is_stop(o) && t_hi == 0); }
+    // tiles of a block of the range that belong to it, [from, to)
+    __device__ __forceinline__ void share(const Block &o, bool first, int tb, int max_len, int &from, int &to) const {
+        from = first ? t_lo : 0;
+        to = is_stop(o) ? t_hi : o.tiles(tb, max_len);
+    }
+    // its tiles, and what it leaves to the merge
+    __device__ __forceinline__ RangeNote note(const Sequences &s, int B, int tb) const {
+        RangeNote r = {};
+        Block o = at;
+        for (bool first = true; !behind(o); first = false) {
+            int from, to;
+            share(o, first, tb, s.max_len, from, to);
+            const int all = o.tiles(tb, s.max_len);
+            if (to > from) {
+                r.tiles += to - from;
+                if (from > 0 && to == all) r.ends = 1;
+                if (from == 0 && to < all) {
+                    r.open = 1;
+                    r.head = o.head; r.row0 = o.c0 + o.k * tb; r.nt = o.tokens(tb);
+                }
+            }
+            if (is_stop(o)) break;
+            o.next(s, B, tb);
+        }
+        return r;
+    }
+};
+
+}  // namespace
+
+}  // namespace reader
