@@ -29,12 +29,13 @@ STATUS_BAD_PAGE = 2
 STATUS_BAD_PATH = 4
 STATUS_BAD_LENGTH = 8
 TUNE_ATTN_ROWS, TUNE_ATTN_RANGES, TUNE_ATTN_PAIR_COST, TUNE_ATTN_AXIS64, TUNE_ATTN_WIDE, TUNE_ATTN_PAIR_FRONT, TUNE_ATTN_SHORT, TUNE_JOIN, TUNE_JOIN_SPREAD = 0, 1, 2, 3, 4, 5, 6, 7, 8
+TUNE_PROMPT_ROWS = 9
 
 EXPORTS = (
     "reader_version", "reader_strerror", "reader_last_error_detail", "reader_validate_tree", "reader_workspace_bytes",
     "reader_tree_attn", "reader_tree_attn_noalloc", "reader_accept_path", "reader_kv_compact", "reader_verify_step",
     "reader_kv_rearrange_scratch_bytes", "reader_kv_rearrange", "reader_target_argmax", "reader_target_sample", "reader_kv_compact_layers",
-    "reader_tree_qkv", "reader_prompt_qkv", "reader_prompt_workspace_bytes", "reader_prompt_attn", "reader_key_weights",
+    "reader_tree_qkv", "reader_prompt_qkv", "reader_prompt_workspace_bytes", "reader_prompt_rows", "reader_prompt_attn", "reader_key_weights",
     "reader_prompt_key_weights", "reader_kv_evict_workspace_bytes", "reader_kv_evict",
     "reader_trie_create", "reader_trie_destroy", "reader_trie_nodes", "reader_trie_insert", "reader_trie_search_path",
     "reader_trie_extract_tree", "reader_tree_attach_path", "reader_self_repetition", "reader_tree_prune_order",
@@ -156,6 +157,8 @@ def load():
     lib.reader_prompt_qkv.argtypes = [dp, i32] + [vp] * 6 + [f32, vp, i32, i32, i32] + [vp] * 6
     lib.reader_prompt_workspace_bytes.restype = sz
     lib.reader_prompt_workspace_bytes.argtypes = [dp, i32, i32]
+    lib.reader_prompt_rows.restype = ctypes.c_int
+    lib.reader_prompt_rows.argtypes = [dp, i32, i32]
     lib.reader_prompt_attn.restype = ctypes.c_int
     lib.reader_prompt_attn.argtypes = [dp, i32] + [vp] * 8 + [i32, vp, sz, vp, vp]
     lib.reader_key_weights.restype = ctypes.c_int
@@ -359,6 +362,14 @@ def reader_prompt_qkv(dims, qkv, cu_tokens, seq_lens, positions, q_norm, k_norm,
 
 def reader_prompt_workspace_bytes(dims: ReaderDims, N: int, max_seq_len: int) -> int:
     return int(load().reader_prompt_workspace_bytes(ctypes.byref(dims), int(N), int(max_seq_len)))
+
+
+def reader_prompt_rows(dims: ReaderDims, N: int, max_seq_len: int) -> int:
+    """Query rows of a kv head that a workgroup of reader_prompt_attn takes (host only)."""
+    rows = int(load().reader_prompt_rows(ctypes.byref(dims), int(N), int(max_seq_len)))
+    if rows < 0:
+        _check(rows, "reader_prompt_rows")
+    return rows
 
 
 def reader_prompt_attn(dims, q, k_cache, v_cache, page_table, cu_tokens, seq_lens, out, lse, max_seq_len, workspace, status=None):

@@ -22,7 +22,7 @@ STAMPS_LIB = os.path.join(HERE, "libreader_hip_stamps.so")
 # the extension module binding.py calls the library through (torch tensors and numpy arrays to pointers)
 NATIVE = os.path.join(HERE, "_reader_torch.so")
 SOURCES = ["reader_api.hip", "trie_drafter.cpp", "tree_shape.cpp", "accept_compact.hip", "kv_compact_layers.hip", "kv_rearrange.hip", "target_argmax.hip", "target_sample.hip", "tree_attn_scalar.hip", "tree_attn_mfma.hip", "tree_attn_wide.hip", "tree_attn_short.hip", "peak_probes.hip",
-           "prompt_api.hip", "qkv_prepare.hip", "prompt_attn.hip", "prompt_attn_few.hip", "prompt_merge.hip",
+           "prompt_api.hip", "qkv_prepare.hip", "prompt_attn.hip", "prompt_attn_mid.hip", "prompt_attn_few.hip", "prompt_merge.hip",
            "prompt_attn_scalar.hip", "key_weights.hip", "kv_evict.hip"]
 # kernels that manage the accumulation registers by hand
 HAND_MANAGED = ["tree_attn_wide.hip", "prompt_attn.hip"]

@@ -13,6 +13,7 @@ namespace reader {
 // Remember which HIP call failed (text returned by reader_last_error_detail()); returns e.
 hipError_t note_hip_error(const char *where, hipError_t e);
 void forget_stale_error();
+int tuning(int which);   // value set through reader_tuning_override, or -1
 // The limits of reader.h on the sizes; false: *err says why.
 bool dims_ok(const reader_dims *d, int *err);
 

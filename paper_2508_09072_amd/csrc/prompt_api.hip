@@ -38,13 +38,50 @@ static bool cache_ok(const reader_dims *dims, const void *k_cache, const void *v
     return k_cache && v_cache && page_table && dims->num_pages >= 1 && dims->max_pages_per_seq >= 1;
 }
 
-// Which kernel: by the query rows that a sequence has for each kv head, on average (the host knows no more).
-static hipError_t launch_prompt(const PromptParams &p, int variant, hipStream_t stream) {
-    if (variant == 1) return launch_prompt_attn_scalar(p, stream);
-    const long long rows = (long long)p.N * p.G;
-    if (rows <= 16LL * p.B) return launch_prompt_few(p, 16, stream);
-    if (rows <= 32LL * p.B) return launch_prompt_few(p, 32, stream);
-    return launch_prompt_wide(p, stream);
+// Query rows a workgroup takes (reader_prompt_rows).
+//
+// Up to 16 or 32 rows that a sequence has for each kv head, on average (the host knows no more): the kernel that streams keys for
+// few rows.  Measured against the 256-row kernel: 16 single tokens on 1 to 16 K positions 99 to 122 us; 8 chunks of 8 tokens (32
+// rows) on 2 to 9 K 45 to 55 and, with 64 rows, where it is not taken, 63 to 90.
+//
+// Beyond that the shortest of three estimates, for blocks that are never cut (64 or 128 rows) and for the 256-row kernel, which cuts
+// the keys of all blocks evenly.  The first two last as long as the longest block's steps of 32 keys, one after the other, or as long
+// as all blocks' steps take the compute units; the third 30 us of start, merge and imbalance, and per block what its tiles of 64
+// keys and its ends take.  The constants are fitted to 100 shapes (5 head layouts; 1 to 64 sequences of 100 to 3000 tokens, chunks on
+// up to 8 K positions): of the 98 with more than 32 rows the estimates pick the fastest of the three on 85
+// and are 1 % behind it on average, 22 % at most.  Some
+// of them, 256, 64 and 128 rows: one prompt of 100 tokens 19.5, 6.5 and 8.1 us; of 800 39.6, 24.0, 28.2; of 3000 106, 137, 106; 16
+// of 300 48.9, 48.8, 42.3; 16 of 800 167, 198, 157; 256 tokens on 8 K positions 76, 189, 229 (32 query and 8 kv heads, D 128).
+static int prompt_rows(const reader_dims &d, int32_t N, int32_t max_seq_len) {
+    if (d.variant == 1) return 0;
+    const int forced = tuning(READER_TUNE_PROMPT_ROWS), G = d.Hq / d.Hkv;
+    if (forced == 16 || forced == 32 || forced == 64 || forced == 128 || forced == 256) return forced;
+    if (d.B == 0 || (long long)N * G <= 16LL * d.B) return 16;
+    if ((long long)N * G <= 32LL * d.B) return 32;
+    const double tokens = (double)N / d.B;                        // of a sequence
+    const double longest = max_seq_len > tokens ? max_seq_len : tokens, average = longest - 0.5 * tokens;   // keys of a block
+    auto blocks = [&](int rows) { return (double)d.Hkv * d.B * ceil(tokens / (rows / G)); };
+    auto uncut = [&](int rows, double step, double busy) {
+        const double chain = step * (longest / 32 + 0.5), all = busy * blocks(rows) * (average / 32 + 0.5) / kNumCU;
+        return 5.5 + (chain > all ? chain : all);
+    };
+    const bool wide_heads = d.D == 128;
+    const double rows64 = wide_heads ? uncut(64, 0.76, 0.60) : uncut(64, 0.50, 0.32);
+    const double rows128 = wide_heads ? uncut(128, 0.93, 0.87) : uncut(128, 0.64, 0.51);
+    const double rows256 = 30.0 + blocks(256) / kNumCU * (wide_heads ? 11.0 + 1.65 * (average / 64 + 0.5) : 8.0 + 0.9 * (average / 64 + 0.5));
+    // (block numbers of the uncut kernels are counted with the threads of a launch)
+    const bool countable = ((long long)N / (64 / G) + d.B) * d.Hkv < (1 << 23);
+    if (!countable || (rows256 <= rows64 && rows256 <= rows128)) return 256;
+    return rows64 <= rows128 ? 64 : 128;
+}
+
+static hipError_t launch_prompt(const PromptParams &p, int rows, hipStream_t stream) {
+    switch (rows) {
+        case 0: return launch_prompt_attn_scalar(p, stream);
+        case 16: case 32: return launch_prompt_few(p, rows, stream);
+        case 64: case 128: return launch_prompt_mid(p, rows, stream);
+        default: return launch_prompt_wide(p, stream);
+    }
 }
 
 }  // namespace reader
@@ -102,6 +139,15 @@ extern "C" size_t reader_prompt_workspace_bytes(const reader_dims *dims, int32_t
     return ((wide > few ? wide : few) + 255) & ~(size_t)255;
 }
 
+extern "C" int reader_prompt_rows(const reader_dims *dims, int32_t N, int32_t max_seq_len) {
+    int err = 0;
+    if (!dims_ok(dims, &err)) return err;
+    const int rc = rows_ok(dims, N);
+    if (rc != READER_OK) return rc;
+    if (max_seq_len < 0 || (dims->variant != 0 && dims->variant != 1)) return READER_EINVAL;
+    return prompt_rows(*dims, N, max_seq_len);
+}
+
 extern "C" int reader_prompt_attn(const reader_dims *dims, int32_t N, const void *q, const void *k_cache, const void *v_cache,
                                   const int32_t *page_table, const int32_t *cu_tokens, const int32_t *seq_lens, void *out,
                                   float *lse, int32_t max_seq_len, void *workspace, size_t workspace_bytes, int32_t *status,
@@ -129,7 +175,7 @@ extern "C" int reader_prompt_attn(const reader_dims *dims, int32_t N, const void
     }
     p.g_rcp = 1.0f / (float)p.G;
     forget_stale_error();
-    return launch_prompt(p, dims->variant, (hipStream_t)stream) == hipSuccess ? READER_OK : READER_EHIP;
+    return launch_prompt(p, prompt_rows(*dims, N, max_seq_len), (hipStream_t)stream) == hipSuccess ? READER_OK : READER_EHIP;
 }
 
 static int key_weights_prepare(const reader_dims *dims, int32_t rows, const void *q, const float *lse, const void *k_cache,

@@ -135,14 +135,15 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
         if (tid == 0) notes[blockIdx.x >= n_ranges ? blockIdx.x : range] = RangeNote{};
         return;
     }
+    const PromptAxis axis(per_head, p.Hkv, (int)n_ranges);
     // first tile at or behind position x of the axis
     auto locate = [&](long long x, Block &o) {
         if (x >= total) {
             o = Block{p.Hkv, 0, 0, 0, 0, 0};
             return 0;
         }
-        o.head = (int)(x / per_head);
-        const long long r = x - o.head * per_head;
+        long long r;
+        o.head = axis.head(x, r);
         int lo = 0, hi = p.B - 1;
         while (lo < hi) {                            // last sequence that starts at or in front of r
             const int mid = (lo + hi + 1) >> 1;
@@ -153,13 +154,65 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
         return o.locate(r - s_pref[lo], seqs, p.B, tb);
     };
     Block from, to;
-    const int t_from = locate(range * total / n_ranges, from), t_to = locate((range + 1) * total / n_ranges, to);
+    const int t_from = locate(axis.begin(range), from), t_to = locate(axis.begin(range + 1), to);
     const PromptRange<Block> rg(from, t_from, to, t_to, p.Hkv);
     const RangeNote note = rg.note(seqs, p.B, tb);
     if (tid == 0) notes[range] = note;
     const int n_iter = __builtin_amdgcn_readfirstlane(note.tiles);
     if (n_iter == 0) return;
     __syncthreads();                                 // (everybody is done with the prefix sums: the ring is free)
+
+    // ---- this lane's two query rows: token within the block and head within the group, kept in accumulation registers
+    static_for<2>([&](auto rc) {
+        constexpr int r = decltype(rc)::value;
+        const int row = wave_s * 64 + r * 32 + n;
+        const int tok = (int)(((float)row + 0.5f) * p.g_rcp);         // row / G (half a row is far more than the product's rounding)
+        acc_write<Acc::node(r)>((uint32_t)(row < tb * p.G ? tok : 0x3fffffff));   // (a row that no block uses: behind every token)
+        acc_write<Acc::group(r)>((uint32_t)(row < tb * p.G ? row - tok * p.G : 0));
+    });
+    auto token_of = [](auto rc) { return (int)acc_read_u32<Acc::node(decltype(rc)::value)>(); };
+    auto group_of = [](auto rc) { return (int)acc_read_u32<Acc::group(decltype(rc)::value)>(); };
+    const int wave_token = wave_s * 64 < tb * p.G ? (int)(((float)(wave_s * 64) + 0.5f) * p.g_rcp) : 0x3fffffff;   // first token of this wavefront's rows
+
+    // the segment that is being computed
+    int seg_head = 0, seg_row0 = 0, seg_p0 = 0, seg_nt = 0, seg_t0 = 0;
+    bool wave_active = false;
+    auto q_row = [&](auto rc, int head, int row0, int nt) {
+        const int tok = min(token_of(rc), nt - 1);                     // (rows behind the last token read its row)
+        return p.q + (((size_t)row0 + tok) * p.Hq + (size_t)head * p.G + group_of(rc)) * D;
+    };
+    // The query rows as B operands of the first product: once per segment into the accumulation registers.
+    struct QueryRows {
+        u32x4 w[2][G::kKSteps];
+    };
+    auto fetch_q = [&](QueryRows &q) {
+        static_for<2>([&](auto rc) {
+            constexpr int r = decltype(rc)::value;
+            const uint16_t *src = q_row(rc, seg_head, seg_row0, seg_nt);
+#pragma unroll
+            for (int kk = 0; kk < G::kKSteps; ++kk) q.w[r][kk] = ld16(src + kk * 16 + h * 8);
+        });
+    };
+    auto put_q = [&](const QueryRows &q) {
+        static_for<2>([&](auto rc) {
+            constexpr int r = decltype(rc)::value;
+            const bool real = token_of(rc) < seg_nt;
+            static_for<G::kKSteps>([&](auto kc) {
+                constexpr int kk = decltype(kc)::value;
+                const u32x4 w = keep_if(real, q.w[r][kk]);
+                acc_write<Acc::q(r, kk)>(w.x);
+                acc_write<Acc::q(r, kk) + 1>(w.y);
+                acc_write<Acc::q(r, kk) + 2>(w.z);
+                acc_write<Acc::q(r, kk) + 3>(w.w);
+            });
+        });
+        asm volatile("s_nop 3");
+    };
+    // (those of the first segment are on their way while the tile list is made: asked for behind the first tiles, they would be
+    // waited for together with them)
+    seg_head = rg.at.head; seg_row0 = rg.at.c0 + rg.at.k * tb; seg_nt = rg.at.tokens(tb);
+    QueryRows first_q;
+    fetch_q(first_q);
 
     // ---- the tile list
     // Item i, found by walking the blocks from `walk`, whose first tile in the range is item walk_item; a thread each.
@@ -211,51 +264,11 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
         }
     };
     __syncthreads();   // the list is written
+    put_q(first_q);
 
     auto desc_of = [&](int i) -> const PromptTile * { return s_tile + (i & (kPromptSlots - 1)); };
     auto word = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
 
-    // ---- this lane's two query rows: token within the block and head within the group, kept in accumulation registers
-    static_for<2>([&](auto rc) {
-        constexpr int r = decltype(rc)::value;
-        const int row = wave_s * 64 + r * 32 + n;
-        const int tok = (int)(((float)row + 0.5f) * p.g_rcp);         // row / G (half a row is far more than the product's rounding)
-        acc_write<Acc::node(r)>((uint32_t)(row < tb * p.G ? tok : 0x3fffffff));   // (a row that no block uses: behind every token)
-        acc_write<Acc::group(r)>((uint32_t)(row < tb * p.G ? row - tok * p.G : 0));
-    });
-    auto token_of = [](auto rc) { return (int)acc_read_u32<Acc::node(decltype(rc)::value)>(); };
-    auto group_of = [](auto rc) { return (int)acc_read_u32<Acc::group(decltype(rc)::value)>(); };
-    const int wave_token = wave_s * 64 < tb * p.G ? (int)(((float)(wave_s * 64) + 0.5f) * p.g_rcp) : 0x3fffffff;   // first token of this wavefront's rows
-
-    // the segment that is being computed
-    int seg_head = 0, seg_row0 = 0, seg_p0 = 0, seg_nt = 0, seg_t0 = 0;
-    bool wave_active = false;
-    auto q_row = [&](auto rc, int head, int row0, int nt) {
-        const int tok = min(token_of(rc), nt - 1);                     // (rows behind the last token read its row)
-        return p.q + (((size_t)row0 + tok) * p.Hq + (size_t)head * p.G + group_of(rc)) * D;
-    };
-    // The query rows as B operands of the first product: loaded once per segment into the accumulation registers.
-    auto load_q = [&]() {
-        u32x4 w[2][G::kKSteps];
-        static_for<2>([&](auto rc) {
-            constexpr int r = decltype(rc)::value;
-            const uint16_t *q = q_row(rc, seg_head, seg_row0, seg_nt);
-            const bool real = token_of(rc) < seg_nt;
-#pragma unroll
-            for (int kk = 0; kk < G::kKSteps; ++kk) w[r][kk] = keep_if(real, ld16(q + kk * 16 + h * 8));
-        });
-        static_for<2>([&](auto rc) {
-            constexpr int r = decltype(rc)::value;
-            static_for<G::kKSteps>([&](auto kc) {
-                constexpr int kk = decltype(kc)::value;
-                acc_write<Acc::q(r, kk)>(w[r][kk].x);
-                acc_write<Acc::q(r, kk) + 1>(w[r][kk].y);
-                acc_write<Acc::q(r, kk) + 2>(w[r][kk].z);
-                acc_write<Acc::q(r, kk) + 3>(w[r][kk].w);
-            });
-        });
-        asm volatile("s_nop 3");
-    };
     // touch the next segment's query rows one tile before they are needed
     auto prefetch_q = [&](int head, int row0, int nt) {
         static_for<2>([&](auto rc) {
@@ -712,7 +725,11 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
             seg_head = word(d->head); seg_row0 = word(d->row0); seg_p0 = word(d->p0); seg_nt = word(d->nt); seg_t0 = word(d->t);
             wave_active = wave_token < seg_nt;
             reset_state();
-            load_q();
+            if (it > 0) {
+                QueryRows q;
+                fetch_q(q);
+                put_q(q);
+            }
         }
         Iter I = begin_iteration(it);
         if (!wave_active) continue;

@@ -1,0 +1,121 @@
+// Causal attention of packed prompts over the paged cache, blocks of 128 query rows that are never cut: short prompts, batches of
+// them.  One launch and no records: where the blocks of a call are about as many as the chip runs at a time, cutting them evenly
+// costs more than it gains (what is written and read again for a row is as much as 2 tiles of keys, and a second launch).
+//
+// A workgroup is 4 wavefronts of 32 rows (prompt_rows.h) that share the keys, 32 at a time, in a ring of four stages in LDS; two
+// workgroups run on a compute unit and fill each other's waits.  Each wavefront copies one of the four pages of a step.
+#include "prompt_rows.h"
+
+namespace reader {
+
+namespace {
+
+constexpr int kMidThreads = 256, kMidStages = 4;
+
+// kBlocks: blocks of 16 query rows that a wavefront carries
+template <int D, int kBlocks>
+__global__ __launch_bounds__(kMidThreads, 2) void prompt_mid_kernel(PromptParams p) {
+    using Rows = PromptRows<D, kBlocks>;
+    using Page = PageLayout<D>;
+    constexpr int kStageBytes = 2 * kStepPages * Page::kPageBytes;
+    __shared__ __attribute__((aligned(1024))) char s_stage[kMidStages][kStageBytes];   // pages of K, then of V
+    __shared__ int s_ids[4][2][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int i16 = lane & 15, quad = lane >> 4, tb = p.tokens_per_block;
+    int bad = 0;
+
+    // Block number j of a kv head, the last ones first (they are the longest).  Sequence b's are numbers cu[b] / tb + b and on: no two
+    // the same, some nobody's.  With two workgroups a compute unit at once, the second round runs the other way, so that a long
+    // block meets a short one; heads change fastest, so that those of one run on one XCD and share its L2.
+    const int n_ids = p.n_ranges;
+    int j = (int)blockIdx.x / p.Hkv;
+    const int head = (int)blockIdx.x - j * p.Hkv;
+    {
+        const int half = (kNumCU + p.Hkv - 1) / p.Hkv;
+        if (n_ids > half && n_ids <= 2 * half && j >= half) j = half + (n_ids - 1 - j);
+    }
+    const int id = n_ids - 1 - j;
+    // the last sequence whose blocks start at or in front of it
+    auto first_id = [&](int b) { return clamp_row(p.cu_tokens[b], p.N) / tb + b; };
+    int b = 0, len = p.B;                                // the one is among b .. b + len - 1
+    while (len > 1) {
+        const int step = (len + 63) >> 6, at = b + min((lane + 1) * step, len);
+        const int n = (int)__popcll(__ballot((lane + 1) * step < len && first_id(min(at, p.B - 1)) <= id));
+        b += n * step;
+        len = min(step, len - n * step);
+    }
+    b = __builtin_amdgcn_readfirstlane(b);
+    const int lo = p.cu_tokens[b], hi = p.cu_tokens[b + 1], cached = p.seq_lens[b];
+    const int c0 = clamp_row(lo, p.N), n = max(clamp_row(hi, p.N) - c0, 0), L = min(max(cached, 0), p.max_seq_len);
+    const int k = id - (c0 / tb + b);
+    if (k < 0 || (long long)k * tb >= n) return;
+    if (k == 0 && (cached < 0 || lo < 0 || hi < lo || hi > p.N || (long long)cached + n > p.max_seq_len)) bad |= READER_STATUS_BAD_LENGTH;
+    const int nt = min(tb, n - k * tb), row0 = c0 + k * tb;
+    const long long p0 = (long long)L + k * tb;
+    const int keys = (int)min(p0 + nt, (long long)p.max_seq_len), steps = max(1, (keys + kStep - 1) / kStep);
+
+    const Page page(lane);
+    const unsigned stage_lds = (unsigned)(size_t)(lds_char *)&s_stage[0][0];
+    PageIds ids(p.page_table + (size_t)b * p.max_pages, 0, p.max_pages, &s_ids[wave][0][0]);
+    // this wavefront's page of step i: page wave % 2, of K or of V
+    const char *cache = reinterpret_cast<const char *>(wave < 2 ? p.k_cache : p.v_cache);
+    auto issue = [&](int i, int now) {
+        const int at = i * kStepPages + (wave & 1), pid = ids.get(at, now, keys, p.num_pages);
+        const int rows = pid < 0 ? 0 : keys - at * READER_PAGE_SIZE;
+        const char *src = cache + ((size_t)max(pid, 0) * p.Hkv + head) * Page::kPageBytes;
+        const unsigned dst = stage_lds + (i & (kMidStages - 1)) * kStageBytes + wave * Page::kPageBytes;
+        if (wave < 2) page.copy(src, page.k_off, rows, dst, lane);
+        else page.copy(src, page.v_off, rows, dst, lane);
+    };
+    ids.load(0, lane);
+    Rows rows;
+    const int first = wave * 16 * kBlocks;
+    rows.load(p, head, row0, p0, nt, first, i16, quad);
+    const int first_tok = (int)(((float)first + 0.5f) * p.g_rcp);
+    const bool active = first_tok < nt;
+    wait_vmcnt<0>();                                     // the first page ids are there
+    asm volatile("" ::: "memory");
+    ids.begin(lane);
+    for (int i = 0; i < min(kMidStages - 1, steps); ++i) issue(i, 0);
+    const int all_see = (int)min(p0 + first_tok + 1, (long long)p.max_seq_len);   // keys that every row of this wavefront sees
+    for (int i = 0; i < steps; ++i) {
+        ids.advance<1>(i, steps, lane);
+        // this wavefront's page of step i has landed once at most those of the next two steps are on their way
+        if (i + 2 < steps) wait_vmcnt<2 * Page::kCopies>();
+        else wait_vmcnt<0>();
+        __syncthreads();                                 // ... and everybody's; nobody reads step i - 1 any more
+        if (i + kMidStages - 1 < steps) issue(i + kMidStages - 1, i);
+        const int j0 = i * kStep;
+        const bool hole0 = j0 < keys && ids.get(i * kStepPages, i, keys, p.num_pages) < 0;
+        const bool hole1 = j0 + READER_PAGE_SIZE < keys && ids.get(i * kStepPages + 1, i, keys, p.num_pages) < 0;
+        if (hole0 || hole1) bad |= READER_STATUS_BAD_PAGE;
+        const char *stage = s_stage[i & (kMidStages - 1)];
+        rows.scores(stage, i16, quad);
+        rows.weights(j0, i == 0, j0 + kStep > all_see || hole0 || hole1, hole0, hole1, p.scale_log2, quad);
+        rows.template products<false>(stage + kStepPages * Page::kPageBytes, i16, quad, [] {});
+    }
+    if (active) {
+        rows.finish_sums();
+        if (rows.write(p, head, row0, nt, first, i16, quad))
+            rows_the_plain_way<D>(p, ids.table, head, row0, p0, first, min(first + 16 * kBlocks, nt * p.G), 0, keys, nullptr, 0, lane, bad);
+    }
+    if (p.status && bad) atomicOr(p.status, bad);
+}
+
+
+template <int D, int kBlocks>
+hipError_t launch_mid(PromptParams p, hipStream_t stream) {
+    p.tokens_per_block = 64 * kBlocks / p.G;
+    p.n_ranges = p.N / p.tokens_per_block + p.B;         // (block numbers of a kv head)
+    hipLaunchKernelGGL((prompt_mid_kernel<D, kBlocks>), dim3((unsigned)p.n_ranges * p.Hkv), dim3(kMidThreads), 0, stream, p);
+    return note_hip_error("launch prompt_mid_kernel", hipGetLastError());
+}
+
+}  // namespace
+
+hipError_t launch_prompt_mid(const PromptParams &p, int rows, hipStream_t stream) {
+    if (rows == 64) return p.D == 64 ? launch_mid<64, 1>(p, stream) : launch_mid<128, 1>(p, stream);
+    return p.D == 64 ? launch_mid<64, 2>(p, stream) : launch_mid<128, 2>(p, stream);
+}
+
+}  // namespace reader

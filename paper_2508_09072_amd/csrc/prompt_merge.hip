@@ -17,7 +17,10 @@ __global__ __launch_bounds__(64 * kMergeWaves) void prompt_merge_kernel(PromptPa
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i16 = lane & 15, quad = lane >> 4;
     const int range = blockIdx.x, row = blockIdx.y * kMergeRows + i16;
     const RangeNote *notes = reinterpret_cast<const RangeNote *>(p.workspace);
+    // (this range's note and the 64 behind it are asked for together)
     const RangeNote mine = notes[range];
+    auto note_at = [&](int w) { return *reinterpret_cast<const int2 *>(&notes[min(w, p.n_ranges - 1)].tiles); };   // tiles, ends
+    int2 note = note_at(range + 1 + lane);
     if (!mine.open || blockIdx.y * kMergeRows >= mine.nt * p.G) return;
     const size_t record_floats = (size_t)record_rows * (D + 2);
     const float *records = reinterpret_cast<const float *>(reinterpret_cast<const char *>(p.workspace) + kNotesBytes);
@@ -36,27 +39,39 @@ __global__ __launch_bounds__(64 * kMergeWaves) void prompt_merge_kernel(PromptPa
         l = l * a + b;
         m = top;
     };
-    auto part = [&](int w) {
-        const float *rec = records + (size_t)(2 * w + (w == range ? 1 : 0)) * record_floats;
-        const float m2 = rec[(size_t)record_rows * D + row], l2 = rec[(size_t)record_rows * (D + 1) + row];
-        const float4 *from = reinterpret_cast<const float4 *>(rec) + (size_t)quad * kChunks * record_rows + row;
+    struct Part {
+        float m, l;
         float4 v[kChunks];
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c) v[c] = from[(size_t)c * record_rows];
-        fold(m2, l2, v);
     };
-    if (wave == 0) part(range);
+    auto load = [&](int w, Part &o) {
+        const float *rec = records + (size_t)(2 * w + (w == range ? 1 : 0)) * record_floats;
+        o.m = rec[(size_t)record_rows * D + row];
+        o.l = rec[(size_t)record_rows * (D + 1) + row];
+        const float4 *from = reinterpret_cast<const float4 *>(rec) + (size_t)quad * kChunks * record_rows + row;
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) o.v[c] = from[(size_t)c * record_rows];
+    };
+    // (a part is asked for before the one in front of it is folded)
+    Part held, next;
+    bool any = wave == 0;
+    if (any) load(range, held);
+    auto part = [&](int w) {
+        load(w, next);
+        if (any) fold(held.m, held.l, held.v);
+        held = next;
+        any = true;
+    };
     // the ranges behind it, 64 notes at a time, up to the one that ends the block
     for (int base = range + 1, turn = 1; base < p.n_ranges; base += 64) {
-        const int w = base + lane;
-        const RangeNote note = notes[min(w, p.n_ranges - 1)];
-        const bool held = w < p.n_ranges && note.tiles > 0;
-        unsigned long long parts = __ballot(held), ends = __ballot(held && note.ends);
+        const bool there = base + lane < p.n_ranges && note.x > 0;
+        unsigned long long parts = __ballot(there), ends = __ballot(there && note.y != 0);
         if (ends) parts &= (2ull << __builtin_ctzll(ends)) - 1ull;   // (nothing behind the first that ends)
         for (; parts; parts &= parts - 1, ++turn)
             if (turn % kMergeWaves == wave) part(base + (int)__builtin_ctzll(parts));
         if (ends) break;
+        note = note_at(base + 64 + lane);
     }
+    if (any) fold(held.m, held.l, held.v);
     // the four wavefronts' sums, in their order
     __shared__ float s_part[kMergeWaves - 1][4 * kChunks + 2][64];
     if (wave > 0) {

@@ -84,6 +84,26 @@ struct PromptBlock {
     }
 };
 
+// The axis: `per_head` positions for each of `heads` kv heads, cut into n ranges.
+struct PromptAxis {
+    long long per_head, total;
+    double width, per_head_rcp;
+    int n;
+    __device__ __forceinline__ PromptAxis(long long head_positions, int heads, int n_ranges)
+        : per_head(head_positions), total(head_positions * heads), width((double)total / n_ranges), per_head_rcp(1.0 / (double)per_head), n(n_ranges) {}
+    // where range r begins (in floating point, which is as good as any other rule that all workgroups share: 64-bit division costs a
+    // workgroup a microsecond)
+    __device__ __forceinline__ long long begin(int r) const { return r >= n ? total : (long long)(r * width); }
+    // kv head of position x, and the position within it
+    __device__ __forceinline__ int head(long long x, long long &r) const {
+        int h = (int)((double)x * per_head_rcp);
+        r = x - h * per_head;
+        while (r < 0) { --h; r += per_head; }
+        while (r >= per_head) { ++h; r -= per_head; }
+        return h;
+    }
+};
+
 // A range: from tile t_lo of block `at` up to tile t_hi of block `stop`.
 template <class Block>
 struct PromptRange {

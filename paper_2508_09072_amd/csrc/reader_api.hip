@@ -19,12 +19,12 @@ namespace reader {
 static char g_error_detail[256] = "";
 
 // Planner overrides set through reader_tuning_override (tests, experiments); -1 = the planner decides.
-static std::atomic<int32_t> g_tuning[READER_TUNE_COUNT_] = {{-1}, {-1}, {-1}, {-1}, {-1}, {-1}, {-1}, {-1}, {-1}};
-static_assert(READER_TUNE_COUNT_ == 9, "every override starts at -1");
+static std::atomic<int32_t> g_tuning[READER_TUNE_COUNT_] = {{-1}, {-1}, {-1}, {-1}, {-1}, {-1}, {-1}, {-1}, {-1}, {-1}};
+static_assert(READER_TUNE_COUNT_ == 10, "every override starts at -1");
 #ifdef READER_WG_STAMPS
 static std::atomic<long long *> g_wg_stamps{nullptr};
 #endif
-static int tuning(int which) { return g_tuning[which].load(std::memory_order_relaxed); }
+int tuning(int which) { return g_tuning[which].load(std::memory_order_relaxed); }
 
 // The runtime keeps the last error of the calling thread until somebody reads it, whoever caused
 // it: an error another library left behind must not be taken for a failed launch of ours.
