@@ -646,9 +646,9 @@ int reader_prompt_qkv(const reader_dims *dims, int32_t N, const void *qkv, const
  * row, no workspace).  dims->T and max_path have to be valid and are not used.
  */
 size_t reader_prompt_workspace_bytes(const reader_dims *dims, int32_t N, int32_t max_seq_len);
-/* Query rows of a kv head that a workgroup of reader_prompt_attn takes for these sizes: 16 or 32 (few rows a sequence; keys cut
- * into ranges), 64 or 128 (short problems, blocks of rows never cut), 256 (keys cut into ranges), 0 for dims->variant = 1;
- * or the error that reader_prompt_attn would return for the sizes.  Pure host function; honours reader_tuning_override. */
+/* Query rows of a kv head that a workgroup of reader_prompt_attn takes for these sizes: 16 or 32 (few rows; keys cut into
+ * ranges), 64 or 128 (blocks of rows that are never cut), 256 (keys cut into ranges), by an estimate of their times; 0 for
+ * dims->variant = 1; or the error that reader_prompt_attn would return for the sizes.  Pure host function; honours reader_tuning_override. */
 int reader_prompt_rows(const reader_dims *dims, int32_t N, int32_t max_seq_len);
 int reader_prompt_attn(const reader_dims *dims, int32_t N, const void *q, const void *k_cache, const void *v_cache,
                        const int32_t *page_table, const int32_t *cu_tokens, const int32_t *seq_lens,

@@ -40,39 +40,53 @@ static bool cache_ok(const reader_dims *dims, const void *k_cache, const void *v
 
 // Query rows a workgroup takes (reader_prompt_rows).
 //
-// Up to 16 or 32 rows that a sequence has for each kv head, on average (the host knows no more): the kernel that streams keys for
-// few rows.  Measured against the 256-row kernel: 16 single tokens on 1 to 16 K positions 99 to 122 us; 8 chunks of 8 tokens (32
-// rows) on 2 to 9 K 45 to 55 and, with 64 rows, where it is not taken, 63 to 90.
+// Up to 16 rows that a sequence has for each kv head, on average (the host knows no more): the kernel that streams keys for few
+// rows.  Measured against the 256-row kernel: 16 single tokens on 1 to 16 K positions 98 against 122 us.
 //
-// Beyond that the shortest of three estimates, for blocks that are never cut (64 or 128 rows) and for the 256-row kernel, which cuts
-// the keys of all blocks evenly.  The first two last as long as the longest block's steps of 32 keys, one after the other, or as long
-// as all blocks' steps take the compute units; the third 30 us of start, merge and imbalance, and per block what its tiles of 64
-// keys and its ends take.  The constants are fitted to 100 shapes (5 head layouts; 1 to 64 sequences of 100 to 3000 tokens, chunks on
-// up to 8 K positions): of the 98 with more than 32 rows the estimates pick the fastest of the three on 85
-// and are 1 % behind it on average, 22 % at most.  Some
-// of them, 256, 64 and 128 rows: one prompt of 100 tokens 19.5, 6.5 and 8.1 us; of 800 39.6, 24.0, 28.2; of 3000 106, 137, 106; 16
-// of 300 48.9, 48.8, 42.3; 16 of 800 167, 198, 157; 256 tokens on 8 K positions 76, 189, 229 (32 query and 8 kv heads, D 128).
+// Beyond that the shortest of five estimates, in us:
+//   16, 32 rows: start and merge, and steps of 32 keys, which all blocks share out evenly (four wavefronts a compute unit); keys of
+//     a call that do not stay in the caches come from memory for every block;
+//   64, 128 rows, blocks never cut: the longest block's steps, one after the other (slower where every compute unit has one of
+//     full length), or what all blocks' steps take the compute units;
+//   256 rows: start, merge and imbalance, and per block what its tiles of 64 keys and its ends take, shared out evenly.
+// The constants are fitted to 168 shapes (7 head layouts; 1 to 64 sequences of 12 to 3000 tokens, chunks on up to 30 K positions).
+// Some of them, 16, 32, 64, 128 and 256 rows (32 query and 8 kv heads, D 128): one prompt of 100 tokens -, -, 6.5, 8.1, 19.5; of 800
+// -, -, 24.0, 28.2, 39.6; of 3000 -, -, 137, 106, 106; 16 of 300 -, -, 48.8, 42.3, 48.9; 64 tokens on 8 K positions 61, 42, 188, 229,
+// 79; 32 sequences of 12 on 8 K 476, 327, 216, 278, 196.  The estimates pick the fastest of the five on 138 of the 168 and are 1.6 %
+// behind it on average, 62 % at most (1500 tokens, 6 query heads and 1 kv head: 59 against 37 us).
 static int prompt_rows(const reader_dims &d, int32_t N, int32_t max_seq_len) {
     if (d.variant == 1) return 0;
     const int forced = tuning(READER_TUNE_PROMPT_ROWS), G = d.Hq / d.Hkv;
     if (forced == 16 || forced == 32 || forced == 64 || forced == 128 || forced == 256) return forced;
     if (d.B == 0 || (long long)N * G <= 16LL * d.B) return 16;
-    if ((long long)N * G <= 32LL * d.B) return 32;
     const double tokens = (double)N / d.B;                        // of a sequence
     const double longest = max_seq_len > tokens ? max_seq_len : tokens, average = longest - 0.5 * tokens;   // keys of a block
+    const bool large = d.D == 128;
     auto blocks = [&](int rows) { return (double)d.Hkv * d.B * ceil(tokens / (rows / G)); };
-    auto uncut = [&](int rows, double step, double busy) {
-        const double chain = step * (longest / 32 + 0.5), all = busy * blocks(rows) * (average / 32 + 0.5) / kNumCU;
+    auto few = [&](int rows, double start, double step) {
+        const bool far = (double)d.Hkv * d.B * longest * d.D * 4 > 64e6;
+        const double from_memory = large ? 0.62 : 0.33;
+        return start + (far && step < from_memory ? from_memory : step) * blocks(rows) * (average / 32 + 14) / kNumCU;
+    };
+    auto uncut = [&](int rows, double step, double step_busy, double all_steps) {
+        const bool busy = blocks(rows) * average >= 0.8 * kNumCU * longest;
+        const double chain = (busy ? step_busy : step) * (longest / 32 + 0.5), all = all_steps * blocks(rows) * (average / 32 + 4) / kNumCU;
         return 5.5 + (chain > all ? chain : all);
     };
-    const bool wide_heads = d.D == 128;
-    const double rows64 = wide_heads ? uncut(64, 0.76, 0.60) : uncut(64, 0.50, 0.32);
-    const double rows128 = wide_heads ? uncut(128, 0.93, 0.87) : uncut(128, 0.64, 0.51);
-    const double rows256 = 30.0 + blocks(256) / kNumCU * (wide_heads ? 11.0 + 1.65 * (average / 64 + 0.5) : 8.0 + 0.9 * (average / 64 + 0.5));
+    const double parts = blocks(256) < kNumCU / 4 ? (large ? 20.0 : 10.0) : 0.0;     // (every range leaves records, nothing else)
+    double best = 30.0 + parts + blocks(256) / kNumCU * (large ? 11.0 + 1.65 * (average / 64 + 0.5) : 8.0 + 0.9 * (average / 64 + 0.5));
+    int rows = 256;
+    auto offer = [&](int r, double us) {
+        if (us < best) { best = us; rows = r; }
+    };
+    offer(16, large ? few(16, 17.0, 0.33) : few(16, 16.5, 0.155));
+    offer(32, large ? few(32, 18.0, 0.42) : few(32, 17.0, 0.24));
     // (block numbers of the uncut kernels are counted with the threads of a launch)
-    const bool countable = ((long long)N / (64 / G) + d.B) * d.Hkv < (1 << 23);
-    if (!countable || (rows256 <= rows64 && rows256 <= rows128)) return 256;
-    return rows64 <= rows128 ? 64 : 128;
+    if (((long long)N / (64 / G) + d.B) * d.Hkv < (1 << 23)) {
+        offer(128, large ? uncut(128, 0.93, 1.2, 0.72) : uncut(128, 0.64, 0.8, 0.43));
+        offer(64, large ? uncut(64, 0.76, 0.76, 0.50) : uncut(64, 0.50, 0.50, 0.27));
+    }
+    return rows;
 }
 
 static hipError_t launch_prompt(const PromptParams &p, int rows, hipStream_t stream) {
