@@ -7,12 +7,17 @@
 // sum over rows is a sum over registers, with two exchanges between lanes at the end.  A wavefront holds up to 128 query rows
 // as operands in registers and takes 64 keys a turn, whose pages travel to its own part of the LDS whole, 1 KB a copy
 // instruction, four pages ahead.  (Loaded straight into the operand's layout, 64 bytes of 16 rows an instruction, they came at 4
-// TB/s however many were asked for.)  Up to 128 rows a workgroup is one wavefront, which waits for nobody; beyond that two
-// or four of them share out the rows of the same keys and add up at the end of a turn (8 sequences of up to 2000 keys, 512 rows
-// each, head dimension 64: 45 -> 20 us), and beyond 512 the keys pass by again.  Nobody else writes a key's weight: no atomics, the same bits every time.
-// Bound by memory: K is read once; with 128 rows the exponentials come within a factor of two of that.
+// TB/s however many were asked for.)  Up to 128 rows a workgroup is one wavefront, which waits for nobody; beyond that two, four or
+// eight of them share out the rows of the same keys and add up at the end of a turn (8 sequences of up to 2000 keys, 512 rows
+// each, head dimension 64: 45 -> 20 us), and rows beyond those go through the keys once more.  Nobody else writes a key's weight: no
+// atomics, the same bits every time.
+// Bound by memory with few rows: 16 sequences of 1 to 4 K keys, 32 query and 8 kv heads, D 128, 6 tokens 19 us, 4.6 TB/s with the
+// launch.  With 128 rows matrix instructions and exponentials take as long as the bytes, a SIMD's two wavefronts overlap them only
+// in part: 4 sequences of 20 to 32 K keys, 32 tokens 53 us, 4.2 TB/s.
 #include "prompt_common.h"
 #include "tree_attn_common.h"
+
+#include <type_traits>
 
 namespace reader {
 
@@ -22,7 +27,81 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr int kTurnPages = 4, kTurnKeys = kTurnPages * READER_PAGE_SIZE;
 constexpr int kMaxTurns = 64 / kTurnPages;               // of a wavefront: a lane holds a page id
 
-// kBlocks: blocks of 16 query rows that a wavefront holds at a time
+// positions of sequence `b` that may hold keys of it (0: none, or lengths that are no lengths)
+__device__ inline int keys_of(const KeyWeightsParams &p, int b) {
+    long long keys = p.seq_lens[b];
+    bool ok = keys >= 0;
+    if (!p.path) {
+        const int lo = p.cu_tokens[b], hi = p.cu_tokens[b + 1];
+        ok = ok && lo >= 0 && hi >= lo && hi <= p.N;
+        keys += (long long)hi - lo;
+    }
+    return ok && keys <= min((long long)min(p.max_seq_len, p.max_positions), (long long)p.max_pages * READER_PAGE_SIZE) ? (int)keys : 0;
+}
+
+struct Share { int b, hkv, part, parts, turns; };
+
+// A workgroup's share where all turns are more than the chip runs at a time: from the lengths themselves, which the host does not
+// know, the fewest turns a workgroup with which all of them run at once (against an equal number of turns that the host takes from
+// the longest length, rounded down: 16 sequences of 4000 keys, 128 rows, D 128 55 -> 43 us; rounded up that did as well, but ragged
+// lengths then took 65 instead of 57).  A lane looks after up to kLaneSeqs sequences.
+constexpr int kLaneSeqs = 4;
+template <int kWaves>
+__device__ inline Share share_of(const KeyWeightsParams &p, int lane) {
+    const int per = (p.B + 63) / 64, slots = kNumCU * 8 / kWaves;
+    int mine[kLaneSeqs], sum = 0;
+#pragma unroll
+    for (int i = 0; i < kLaneSeqs; ++i) {
+        mine[i] = -1;                                    // no sequence
+        if (i < per) {
+            const int b = lane * per + i, keys = keys_of(p, min(b, p.B - 1));
+            if (b < p.B) mine[i] = (keys + kTurnKeys - 1) / kTurnKeys;
+        }
+        sum += max(mine[i], 0);
+    }
+    auto over_lanes = [&](int x) {
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
+        return __builtin_amdgcn_readfirstlane(x);
+    };
+    auto parts_of = [](int m, int t) { return m < 0 ? 0 : max((m + t - 1) / t, 1); };
+    auto parts_here = [&](int t) {
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < kLaneSeqs; ++i)
+            if (i < per) n += parts_of(mine[i], t);
+        return n;
+    };
+    const long long total = (long long)over_lanes(sum) * p.Hkv;
+    int t = (int)min(max((total + slots - 1) / slots, 1LL), (long long)kMaxTurns);
+    while (t < kMaxTurns && (long long)over_lanes(parts_here(t)) * p.Hkv > slots) ++t;
+    const int here = parts_here(t);
+    int upto = here;                                     // parts of this lane's sequences and those before
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int x = __shfl_up(upto, d);
+        if (lane >= d) upto += x;
+    }
+    Share s = {};
+    const int at = (int)blockIdx.x / p.Hkv;
+    s.hkv = (int)blockIdx.x - at * p.Hkv;
+    const unsigned long long behind = __ballot(upto > at);
+    if (behind == 0) return s;                           // more workgroups than parts
+    const int owner = __builtin_ctzll(behind);
+    int left = at - (upto - here), b = 0, parts = 0;     // (of the owner's lane, the others' are dropped)
+#pragma unroll
+    for (int i = kLaneSeqs - 1, before = here; i >= 0; --i) {
+        const int n = i < per ? parts_of(mine[i], t) : 0;
+        before -= n;
+        if (n > 0 && parts == 0 && left >= before) b = lane * per + i, parts = n, left -= before;
+    }
+    s.b = __shfl(b, owner), s.part = __shfl(left, owner), s.parts = __shfl(parts, owner), s.turns = t;
+    s.b = __builtin_amdgcn_readfirstlane(s.b), s.part = __builtin_amdgcn_readfirstlane(s.part), s.parts = __builtin_amdgcn_readfirstlane(s.parts);
+    return s;
+}
+
+// kBlocks: blocks of 16 query rows that a wavefront holds at a time.  turns: of a workgroup of the grid (parts, kv heads,
+// sequences), or 0: shared out by the lengths
 template <int D, int kBlocks, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, kBlocks * D <= 512 ? 3 : 2) void key_weights_kernel(KeyWeightsParams p, int turns) {
     constexpr int kSteps = D / 32;                       // 32-deep steps of the product
@@ -32,7 +111,15 @@ __global__ __launch_bounds__(64 * kWaves, kBlocks * D <= 512 ? 3 : 2) void key_w
     __shared__ float s_old[2][kTurnKeys];                                              // what the keys of a turn have so far
     __shared__ float s_sum[2][kWaves][kTurnKeys];                                      // what each wavefront's rows add
     const int lane = threadIdx.x & 63, wave = kWaves == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i16 = lane & 15, quad = lane >> 4;
-    const int hkv = blockIdx.y, b = blockIdx.z, key0 = (int)blockIdx.x * turns * kTurnKeys;
+    // b, hkv: whose keys; turns from key0 on; this is part `part` of `parts` of them
+    int hkv, b, key0, part, parts;
+    if (turns > 0) {
+        hkv = blockIdx.y, b = blockIdx.z, part = blockIdx.x, parts = gridDim.x, key0 = part * turns * kTurnKeys;
+    } else {
+        const Share s = share_of<kWaves>(p, lane);
+        if (s.turns == 0) return;
+        hkv = s.hkv, b = s.b, part = s.part, parts = s.parts, turns = s.turns, key0 = part * turns * kTurnKeys;
+    }
 
     // (what does not depend on one another is asked for together: pages of this wavefront's keys, path, lengths)
     int page = p.page_table[(size_t)b * p.max_pages + min(key0 / READER_PAGE_SIZE + lane, p.max_pages - 1)];
@@ -60,15 +147,13 @@ __global__ __launch_bounds__(64 * kWaves, kBlocks * D <= 512 ? 3 : 2) void key_w
     if (!bad && keys_all > most) bad = READER_STATUS_BAD_LENGTH;
     // (every wavefront of the sequence comes to the same verdict: it is left as it is)
     if (bad) {
-        if (p.status && blockIdx.x == 0 && hkv == 0 && threadIdx.x == 0) atomicOr(p.status, bad);
+        if (p.status && part == 0 && hkv == 0 && threadIdx.x == 0) atomicOr(p.status, bad);
         return;
     }
     const int keys = (int)keys_all, rows = n * p.G;
     float *weights = p.weights + ((size_t)b * p.Hkv + hkv) * p.max_positions;
-    if (p.decay == 0.f) {                                // a fresh start: nothing behind the last key
-        const int end = min(key0 + turns * kTurnKeys, p.max_positions);
-        for (int j = max(key0, keys) + (int)threadIdx.x; j < end; j += 64 * kWaves) weights[j] = 0.f;
-    }
+    if (p.decay == 0.f)                                  // a fresh start: nothing behind the last key
+        for (long long j = keys + part * 64LL * kWaves + threadIdx.x; j < p.max_positions; j += parts * 64LL * kWaves) weights[j] = 0.f;
     if (key0 >= keys) return;
     if (rows == 0) {                                     // nobody to draw anything
         const int end = min(key0 + turns * kTurnKeys, keys);
@@ -108,6 +193,17 @@ __global__ __launch_bounds__(64 * kWaves, kBlocks * D <= 512 ? 3 : 2) void key_w
 
     for (int r_all = 0; r_all < rows; r_all += kWaves * kBlocks * 16) {
         const int r_base = r_all + wave * kBlocks * 16;
+        if constexpr (kWaves > 1) {
+            if (r_base >= rows) {                        // a wavefront without rows adds nothing (rows do not come back either)
+                for (int turn = 0; turn < turns; ++turn) {
+                    s_sum[turn & 1][wave][lane] = 0.f;
+                    __syncthreads();
+                }
+                __syncthreads();
+                continue;
+            }
+        }
+        const bool few = rows - r_base <= kBlocks * 4;   // a quarter of the blocks holds them
         if (wave == 0) copy_old(0);
 #pragma unroll
         for (int pg = 0; pg < kTurnPages; ++pg) copy_page(0, pg);
@@ -160,9 +256,9 @@ __global__ __launch_bounds__(64 * kWaves, kBlocks * D <= 512 ? 3 : 2) void key_w
                     copy_page(turn + 1, pg);
                 }
                 float sum = 0.f;
-                auto add = [&](auto &&sees) {
+                auto add = [&](auto count, auto &&sees) {
 #pragma unroll
-                    for (int k = 0; k < kBlocks; ++k) {
+                    for (int k = 0; k < decltype(count)::value; ++k) {
                         f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                         for (int s = 0; s < kSteps; ++s) x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[k][s], key[s], x, 0, 0, 0);
@@ -173,13 +269,17 @@ __global__ __launch_bounds__(64 * kWaves, kBlocks * D <= 512 ? 3 : 2) void key_w
                         }
                     }
                 };
-                if (causal)
-                    add([&](int k, int i) {
-                        int t;
-                        place(r_base + k * 16 + quad * 4 + i, t);
-                        return j0 + pg * 16 + i16 <= first + t;
-                    });
-                else add([](int, int) { return true; });
+                auto seen = [&](int k, int i) {
+                    int t;
+                    place(r_base + k * 16 + quad * 4 + i, t);
+                    return j0 + pg * 16 + i16 <= first + t;
+                };
+                auto all = [](int, int) { return true; };
+                if (kBlocks >= 4 && few) {
+                    if (causal) add(std::integral_constant<int, kBlocks / 4>(), seen);
+                    else add(std::integral_constant<int, kBlocks / 4>(), all);
+                } else if (causal) add(std::integral_constant<int, kBlocks>(), seen);
+                else add(std::integral_constant<int, kBlocks>(), all);
                 acc[pg] = sum;
             }
             // a key's four quarters of the rows sit 16 lanes apart; lane l then takes key l of the turn
@@ -203,30 +303,37 @@ __global__ __launch_bounds__(64 * kWaves, kBlocks * D <= 512 ? 3 : 2) void key_w
         }
         wait_vmcnt<0>();                                 // (what has been written is read again for the next rows)
         asm volatile("" ::: "memory");
+        if constexpr (kWaves > 1) __syncthreads();       // (the next rows' first sums take the place of sums that may still be read)
     }
 }
 
 template <int D, int kBlocks, int kWaves>
 hipError_t launch_blocks(const KeyWeightsParams &p, int span, hipStream_t stream) {
-    // turns of a wavefront: as many as leave the chip filled
-    const long long all = (long long)((span + kTurnKeys - 1) / kTurnKeys) * p.Hkv * p.B;
-    // (8 wavefronts a compute unit run at a time)
-    const long long n = all * kWaves / (kNumCU * 8);
-    const int turns = (int)(n < 1 ? 1 : n > kMaxTurns ? kMaxTurns : n);
-    const dim3 grid((unsigned)((span + turns * kTurnKeys - 1) / (turns * kTurnKeys)), (unsigned)p.Hkv, (unsigned)p.B);
+    // turns of a workgroup: one, where all of them run at a time (8 wavefronts a compute unit).  Where they do not, up to 256
+    // sequences are shared out by their lengths (every part of a sequence but its last is full, so there are at most `slots` of
+    // full ones, or as many as the most turns leave); more sequences even out by themselves
+    const long long all = (long long)((span + kTurnKeys - 1) / kTurnKeys) * p.Hkv * p.B, slots = kNumCU * 8 / kWaves;
+    const long long most = max(slots, all / kMaxTurns) + (long long)p.B * p.Hkv;
+    const bool shared = all > slots && p.B <= 64 * kLaneSeqs && most * 64 * kWaves < (1LL << 32);   // (a launch counts threads in 32 bits)
+    int turns = shared ? 0 : (int)min(max(all / slots, 1LL), (long long)kMaxTurns);
+    dim3 grid((unsigned)((span + turns * kTurnKeys - 1) / max(turns * kTurnKeys, 1)), (unsigned)p.Hkv, (unsigned)p.B);
+    if (shared) grid = dim3((unsigned)most, 1, 1);
     hipLaunchKernelGGL((key_weights_kernel<D, kBlocks, kWaves>), grid, dim3(64 * kWaves), 0, stream, p, turns);
     return note_hip_error("launch key_weights_kernel", hipGetLastError());
 }
 
 template <int D>
 hipError_t launch_rows(const KeyWeightsParams &p, int span, hipStream_t stream) {
-    const long long rows = (long long)(p.path ? p.max_path : p.window) * p.G;      // no sequence has more
+    const long long rows = (long long)(p.path ? p.max_path : min(p.window, p.N)) * p.G;      // no sequence has more
     if (rows <= 16) return launch_blocks<D, 1, 1>(p, span, stream);
     if (rows <= 32) return launch_blocks<D, 2, 1>(p, span, stream);
     if (rows <= 64) return launch_blocks<D, 4, 1>(p, span, stream);
     if (rows <= 128) return launch_blocks<D, 8, 1>(p, span, stream);
     if (rows <= 256) return launch_blocks<D, 8, 2>(p, span, stream);
-    return launch_blocks<D, 8, 4>(p, span, stream);
+    if (rows <= 512 || (long long)((span + kTurnKeys - 1) / kTurnKeys) * p.Hkv * p.B > 2 * kNumCU) return launch_blocks<D, 8, 4>(p, span, stream);
+    // (where a workgroup of eight is all that a compute unit gets.  2 sequences of 1000 keys, 984 rows: 32 -> 23 us; 64 of 3000, 800
+    // rows: 94, and 125 with eight)
+    return launch_blocks<D, 8, 8>(p, span, stream);
 }
 
 }  // namespace

@@ -152,3 +152,54 @@ def test_rows_that_saw_nothing_give_nothing(R):
     a, ba = P.key_weights(q[:1], lse[:1], cache.rows(cache.k, 0, 20), 17)
     c, bc = P.key_weights(q[2:], lse[2:], cache.rows(cache.k, 0, 20), 19)
     P.check(w[0, :, :20], a + c, ba + bc + 3 * P.F32 * (a + c), "weights")
+
+
+# rows of a sequence up to 16, 128, 256, 512, more; one to four sequences a lane, and more than are shared out; few and many
+# keys: all that a workgroup's share depends on
+@pytest.mark.parametrize("Hq,Hkv,D,B,longest,bound,window", [
+    (2, 2, 64, 9, 8000, 8000, 5), (4, 1, 128, 3, 5000, 60000, 32), (8, 2, 64, 4, 3000, 20000, 40), (16, 2, 64, 5, 4000, 9000, 31),
+    (16, 1, 64, 3, 5000, 11000, 37), (8, 1, 64, 2, 9000, 9000, 100), (16, 1, 128, 2, 2000, 17000, 66), (1, 1, 64, 70, 300, 3000, 4),
+    (2, 1, 64, 130, 120, 2000, 8), (6, 3, 128, 250, 60, 300, 6), (2, 1, 64, 300, 90, 1500, 20)])
+@pytest.mark.parametrize("decay", [0.0, 0.5])
+def test_keys_shared_out(R, Hq, Hkv, D, B, longest, bound, window, decay):
+    gen = torch.Generator().manual_seed(B + window)
+    total = torch.randint(0, longest + 1, (B,), generator=gen).tolist()
+    total[0], total[-1] = longest, 0
+    new = [min(t, int(torch.randint(0, 2 * window, (1,), generator=gen))) for t in total]
+    new[0] = min(longest, 2 * window)
+    L, N = [t - n for t, n in zip(total, new)], sum(new)
+    cache = P.Cache(gen, total, Hkv, D)
+    for b in range(B):
+        cache.fill(gen, b, total[b])
+    W = bound + 3
+    table = torch.full((B, (bound + 15) // 16), -1, dtype=torch.int32)
+    table[:, :cache.max_pages] = cache.table
+    cu = torch.cat([torch.zeros(1), torch.cumsum(torch.tensor(new), 0)]).int()
+    q, lse = torch.randn((N, Hq, D), generator=gen).bfloat16(), 5 + torch.randn((N, Hq), generator=gen)
+    old = torch.rand((B, Hkv, W), generator=gen)
+    bad = B - 2                                              # one sequence with a length that does not fit: left as it is
+    lens = L[:bad] + [bound + 1] + L[bad + 1:]
+    dims = R.make_dims(B, 1, Hq, Hkv, D, table.shape[1], 1, cache.num_pages)
+    args = (q.cuda(), lse.cuda(), cu.cuda(), window, cache.k.cuda(), table.cuda(), i32(lens), decay)
+    got, status = old.cuda() if decay else torch.full_like(old, math.nan).cuda(), torch.zeros(1, dtype=torch.int32, device="cuda")
+    was = got.clone()
+    R.reader_prompt_key_weights(dims, *args, got, bound, status)
+    again = was.clone()
+    R.reader_prompt_key_weights(dims, *args, again, bound, status)
+    assert int(status) == R.STATUS_BAD_LENGTH
+    assert torch.equal(got.view(torch.int32), again.view(torch.int32))
+    assert torch.equal(got[bad].view(torch.int32), was[bad].view(torch.int32))
+    for b in range(B):
+        if b == bad:
+            continue
+        S, n, end = total[b], min(window, new[b]), int(cu[b + 1])
+        want, full = torch.zeros(Hkv, W, dtype=torch.float64), torch.zeros(Hkv, W, dtype=torch.float64)
+        if decay:
+            want = old[b].double()
+            want[:, :S] *= decay
+            full[:, :S] = 3 * P.F32 * want[:, :S]
+        if n:
+            w, error = P.key_weights(q[end - n:end], lse[end - n:end], cache.rows(cache.k, b, S), S - n)
+            want[:, :S] += w
+            full[:, :S] += error + 3 * P.F32 * w
+        P.check(got[b], want, full, "weights of sequence %d" % b)
