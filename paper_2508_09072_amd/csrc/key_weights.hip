@@ -128,21 +128,22 @@ __global__ __launch_bounds__(64 * kWaves, kBlocks * D <= 512 ? 3 : 2) void key_w
     const int len = p.seq_lens[b];
 
     // rows: `n` query tokens, the first of them at position `first`; row r is token r / G, head r % G of the group
-    int n, first, bad = 0, token0 = 0;
+    int n, bad = 0, token0 = 0;
+    long long first_all;                                 // (lengths up to 2^31 - 1 add up to more)
     if (p.path) {
         n = p.accept_len[b] + 1;
-        first = len - n;
-        if (n < 1 || n > p.max_path || first < 0) bad = READER_STATUS_BAD_PATH;
+        first_all = (long long)len - n;
+        if (n < 1 || n > p.max_path || first_all < 0) bad = READER_STATUS_BAD_PATH;
         else if (__any((lane < n && (node < 0 || node >= p.T)) || (lane + 64 < n && (node2 < 0 || node2 >= p.T)))) bad = READER_STATUS_BAD_PATH;
     } else {
         const int lo = p.cu_tokens[b], hi = p.cu_tokens[b + 1], c0 = clamp_row(lo, p.N), c1 = clamp_row(hi, p.N);
         const int all = max(c1 - c0, 0);
         n = min(all, p.window);
         token0 = c1 - n;
-        first = len + all - n;
+        first_all = (long long)len + all - n;
         if (len < 0 || lo < 0 || hi < lo || hi > p.N) bad = READER_STATUS_BAD_LENGTH;
     }
-    const long long keys_all = (long long)first + n;
+    const long long keys_all = first_all + n;
     const long long most = min((long long)min(p.max_seq_len, p.max_positions), (long long)p.max_pages * READER_PAGE_SIZE);
     if (!bad && keys_all > most) bad = READER_STATUS_BAD_LENGTH;
     // (every wavefront of the sequence comes to the same verdict: it is left as it is)
@@ -150,7 +151,7 @@ __global__ __launch_bounds__(64 * kWaves, kBlocks * D <= 512 ? 3 : 2) void key_w
         if (p.status && part == 0 && hkv == 0 && threadIdx.x == 0) atomicOr(p.status, bad);
         return;
     }
-    const int keys = (int)keys_all, rows = n * p.G;
+    const int first = (int)first_all, keys = (int)keys_all, rows = n * p.G;
     float *weights = p.weights + ((size_t)b * p.Hkv + hkv) * p.max_positions;
     if (p.decay == 0.f)                                  // a fresh start: nothing behind the last key
         for (long long j = keys + part * 64LL * kWaves + threadIdx.x; j < p.max_positions; j += parts * 64LL * kWaves) weights[j] = 0.f;

@@ -123,6 +123,25 @@ def test_sequences_that_do_not_fit_are_left_as_they_are(R):
     assert bool((w == 2.0).all())
 
 
+@pytest.mark.parametrize("decay", [0.0, 1.0])
+def test_lengths_at_the_end_of_their_type(R, decay):
+    """A length that new tokens, or a path, carry past 2^31 is one that does not fit."""
+    gen = torch.Generator().manual_seed(14)
+    cache = P.Cache(gen, [40, 40], 1, 64)
+    q, lse = torch.randn((8, 2, 64), generator=gen).bfloat16().cuda(), torch.zeros((8, 2), device="cuda")
+    lens = i32([2 ** 31 - 1, 2 ** 31 - 3])
+    status, w = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.full((2, 1, 48), 2.0, device="cuda")
+    dims = R.make_dims(2, 4, 2, 1, 64, cache.max_pages, 4, cache.num_pages)
+    R.reader_prompt_key_weights(dims, q, lse, i32([0, 3, 8]), 2, cache.k.cuda(), cache.table.cuda(), lens, decay, w, 40, status)
+    assert int(status) == R.STATUS_BAD_LENGTH
+    status.zero_()
+    for bad in (lens, i32([-2 ** 31, -1])):
+        R.reader_key_weights(dims, q.view(2, 4, 2, 64), lse.view(2, 2, 4), i32([[0, 1, 2, 3]] * 2), i32([3, 0]), cache.k.cuda(), cache.table.cuda(),
+                             bad, decay, w, 40, status)
+    assert int(status) == R.STATUS_BAD_LENGTH | R.STATUS_BAD_PATH
+    assert bool((w == 2.0).all())
+
+
 def test_keys_behind_a_missing_page_draw_nothing(R):
     gen = torch.Generator().manual_seed(5)
     cache = P.Cache(gen, [100], 1, 64)
