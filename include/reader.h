@@ -570,6 +570,9 @@ int reader_tuning_override(int32_t which, int32_t value);
  * values go behind the seq_lens[b] positions that the cache holds (as a draft tree's do in the in-cache layout);
  * every layer's calls see the same seq_lens, and the caller adds the new tokens to it after the last layer.
  *
+ * bf16 tensors and the rotation table start at a multiple of 16 bytes (READER_EINVAL otherwise).  No output overlaps an
+ * input, but for what is named in/out.
+ *
  * Rotation table: f32 [max_positions, rot_dims], row `pos` holds rot_dims / 2 cosines and then as many sines of that
  * position's angles (made by the caller, in 64 bits for far positions).  The first rot_dims values of a head are
  * turned (rot_dims a multiple of 16, 0: none), pair i by angle i: values i and i + rot_dims / 2, or with

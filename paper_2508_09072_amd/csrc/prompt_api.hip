@@ -10,6 +10,10 @@ static float softmax_scale_log2(const reader_dims &d) {
     return (d.sm_scale > 0.f ? d.sm_scale : 1.0f / sqrtf((float)d.D)) * 1.44269504088896340736f;
 }
 
+// Wide loads and copies into LDS take 16 bytes: tensors start at a multiple of them.
+template <class... Pointers>
+static bool aligned(const Pointers *...p) { return (((uintptr_t)p | ...) & 15) == 0; }
+
 // What both forms of the projections' operator check and fill.
 static int qkv_prepare(const reader_dims *dims, const void *qkv, const int32_t *seq_lens, const int32_t *positions,
                        const void *q_norm, const void *k_norm, float eps, const float *cos_sin, int32_t max_positions,
@@ -19,6 +23,7 @@ static int qkv_prepare(const reader_dims *dims, const void *qkv, const int32_t *
     if ((q_norm == nullptr) != (k_norm == nullptr)) return READER_EINVAL;
     if (q_norm && !(eps >= 0.f && eps <= 1.f)) return READER_EINVAL;
     if (!qkv || !seq_lens || !q || (rot_dims > 0 && !cos_sin)) return READER_EINVAL;
+    if (!aligned(qkv, q_norm, k_norm, q) || (rot_dims > 0 && !aligned(cos_sin))) return READER_EINVAL;
     p.qkv = (const uint16_t *)qkv; p.q_norm = (const uint16_t *)q_norm; p.k_norm = (const uint16_t *)k_norm;
     p.cos_sin = cos_sin; p.seq_lens = seq_lens; p.positions = positions; p.q = (uint16_t *)q; p.status = status;
     p.B = dims->B; p.T = dims->T; p.Hq = dims->Hq; p.Hkv = dims->Hkv; p.D = dims->D;
@@ -35,7 +40,7 @@ static int rows_ok(const reader_dims *dims, int32_t N) {
 
 // The cache and page table of a call that reads or writes them.
 static bool cache_ok(const reader_dims *dims, const void *k_cache, const void *v_cache, const int32_t *page_table) {
-    return k_cache && v_cache && page_table && dims->num_pages >= 1 && dims->max_pages_per_seq >= 1;
+    return k_cache && v_cache && page_table && dims->num_pages >= 1 && dims->max_pages_per_seq >= 1 && aligned(k_cache, v_cache);
 }
 
 // Query rows a workgroup takes (reader_prompt_rows).
@@ -115,6 +120,7 @@ extern "C" int reader_tree_qkv(const reader_dims *dims, const void *qkv, const i
     if (rc != READER_OK) return rc;
     if (!parents || (k_tree == nullptr) != (v_tree == nullptr)) return READER_EINVAL;
     if (!k_tree && !cache_ok(dims, k_cache, v_cache, page_table)) return READER_EINVAL;
+    if (!aligned(k_tree, v_tree)) return READER_EINVAL;
     p.N = dims->B * dims->T;
     rc = rows_ok(dims, p.N);
     if (rc != READER_OK) return rc;
@@ -172,7 +178,7 @@ extern "C" int reader_prompt_attn(const reader_dims *dims, int32_t N, const void
     if (rc != READER_OK) return rc;
     if (max_seq_len < 0 || (dims->variant != 0 && dims->variant != 1)) return READER_EINVAL;
     if (dims->B == 0 || N == 0) return READER_OK;
-    if (!q || !cu_tokens || !seq_lens || !out || !cache_ok(dims, k_cache, v_cache, page_table)) return READER_EINVAL;
+    if (!q || !cu_tokens || !seq_lens || !out || !cache_ok(dims, k_cache, v_cache, page_table) || !aligned(q, out)) return READER_EINVAL;
     if ((long long)dims->max_pages_per_seq * dims->page_size < max_seq_len) return READER_EINVAL;
     PromptParams p = {};
     p.q = (const uint16_t *)q; p.k_cache = (const uint16_t *)k_cache; p.v_cache = (const uint16_t *)v_cache;
@@ -197,7 +203,7 @@ static int key_weights_prepare(const reader_dims *dims, int32_t rows, const void
                                int32_t max_positions, int32_t max_seq_len, int32_t *status, KeyWeightsParams &p) {
     if (max_positions < 0 || max_seq_len < 0 || !(decay >= 0.f && decay <= 1.f)) return READER_EINVAL;
     if (dims->Hkv > 65535) return READER_EUNSUPPORTED;                    // (a dimension of the grid)
-    if ((rows > 0 && (!q || !lse)) || !seq_lens || !weights || !cache_ok(dims, k_cache, k_cache, page_table)) return READER_EINVAL;
+    if ((rows > 0 && (!q || !lse)) || !seq_lens || !weights || !cache_ok(dims, k_cache, k_cache, page_table) || !aligned(q)) return READER_EINVAL;
     p.q = (const uint16_t *)q; p.lse = lse; p.k_cache = (const uint16_t *)k_cache;
     p.page_table = page_table; p.seq_lens = seq_lens; p.weights = weights; p.status = status;
     p.B = dims->B; p.T = dims->T; p.Hq = dims->Hq; p.Hkv = dims->Hkv; p.G = dims->Hq / dims->Hkv; p.D = dims->D;

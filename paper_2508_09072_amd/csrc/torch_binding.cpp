@@ -141,6 +141,16 @@ public:
         ok_ = false;
         return nullptr;
     }
+    // a size that is handed on as 32 bits
+    int32_t size(const at::Tensor *t, int64_t dim, const char *what) {
+        if (!ok_ || !t) return 0;
+        if (t->size(dim) > INT32_MAX) {
+            PyErr_Format(PyExc_ValueError, "%s: a dimension of %lld is more than 32 bits hold", what, (long long)t->size(dim));
+            ok_ = false;
+            return 0;
+        }
+        return (int32_t)t->size(dim);
+    }
     // all tensors on the device whose current stream the launch goes to
     void on_current_device() {
         if (!ok_ || (!several_ && (device_ == kNoDevice || device_ == c10::hip::current_device()))) return;
@@ -378,8 +388,8 @@ struct Rotation {
         interleaved = a.integer();
         const bool there = t && a.ok();
         cos_sin = there ? data<float>(t) : nullptr;
-        max_positions = there ? (int32_t)t->size(0) : 0;
-        rot_dims = there ? (int32_t)t->size(1) : 0;
+        max_positions = there ? a.size(t, 0, "cos_sin") : 0;
+        rot_dims = there ? a.size(t, 1, "cos_sin") : 0;
     }
 };
 
@@ -414,8 +424,9 @@ PyObject *py_prompt_qkv(PyObject *const *args, Py_ssize_t n) {
     const reader_dims *d = a.dims();
     const at::Tensor *qkv = a.tensor(kBf16);
     a.want_dims(qkv, 3, "qkv");
+    const int64_t N = a.size(qkv, 0, "qkv");
     if (!a.ok()) return nullptr;
-    const int64_t N = qkv->size(0), B = d->B, Hq = d->Hq, Hkv = d->Hkv, D = d->D;
+    const int64_t B = d->B, Hq = d->Hq, Hkv = d->Hkv, D = d->D;
     if (qkv->size(1) != Hq + 2 * Hkv || qkv->size(2) != D) a.reject(PyExc_ValueError, "qkv must be [N, Hq + 2 Hkv, D]");
     const at::Tensor *cu = a.shaped(kI32, {B + 1}, "cu_tokens"), *lens = a.shaped(kI32, {B}, "seq_lens");
     const at::Tensor *positions = a.shaped(kI32, {B}, "positions", true);
@@ -442,8 +453,9 @@ PyObject *py_prompt_attn(PyObject *const *args, Py_ssize_t n) {
     const reader_dims *d = a.dims();
     const at::Tensor *q = a.tensor(kBf16);
     a.want_dims(q, 3, "q");
+    const int64_t N = a.size(q, 0, "q");
     if (!a.ok()) return nullptr;
-    const int64_t N = q->size(0), B = d->B, Hq = d->Hq, Hkv = d->Hkv, D = d->D;
+    const int64_t B = d->B, Hq = d->Hq, Hkv = d->Hkv, D = d->D;
     if (q->size(1) != Hq || q->size(2) != D) a.reject(PyExc_ValueError, "q must be [N, Hq, D]");
     const at::Tensor *kc = a.shaped(kBf16, {d->num_pages, Hkv, d->page_size, D}, "k_cache");
     const at::Tensor *vc = a.shaped(kBf16, {d->num_pages, Hkv, d->page_size, D}, "v_cache");
@@ -478,11 +490,12 @@ PyObject *py_key_weights(PyObject *const *args, Py_ssize_t n) {
     int32_t *status = a.i32_out(true);
     a.on_current_device();
     if (a.ok() && (w->dim() != 3 || w->size(0) != B || w->size(1) != Hkv)) a.reject(PyExc_ValueError, "weights must be [B, Hkv, max_positions]");
+    const int32_t positions = a.size(w, 2, "weights");
     if (!a.ok()) return nullptr;
     void *st = stream();
     return unlocked([&] {
         return api.reader_key_weights(d, data<void>(q), data<float>(lse), data<int32_t>(path), data<int32_t>(len), data<void>(kc),
-                                      data<int32_t>(table), data<int32_t>(lens), (float)decay, data<float>(w), (int32_t)w->size(2), max_len,
+                                      data<int32_t>(table), data<int32_t>(lens), (float)decay, data<float>(w), positions, max_len,
                                       status, st);
     });
 }
@@ -492,8 +505,9 @@ PyObject *py_prompt_key_weights(PyObject *const *args, Py_ssize_t n) {
     const reader_dims *d = a.dims();
     const at::Tensor *q = a.tensor(kBf16);
     a.want_dims(q, 3, "q");
+    const int64_t N = a.size(q, 0, "q");
     if (!a.ok()) return nullptr;
-    const int64_t N = q->size(0), B = d->B, Hq = d->Hq, Hkv = d->Hkv, D = d->D;
+    const int64_t B = d->B, Hq = d->Hq, Hkv = d->Hkv, D = d->D;
     if (q->size(1) != Hq || q->size(2) != D) a.reject(PyExc_ValueError, "q must be [N, Hq, D]");
     const at::Tensor *lse = a.shaped(kF32, {N, Hq}, "lse"), *cu = a.shaped(kI32, {B + 1}, "cu_tokens");
     const int32_t window = a.integer();
@@ -505,11 +519,12 @@ PyObject *py_prompt_key_weights(PyObject *const *args, Py_ssize_t n) {
     int32_t *status = a.i32_out(true);
     a.on_current_device();
     if (a.ok() && (w->dim() != 3 || w->size(0) != B || w->size(1) != Hkv)) a.reject(PyExc_ValueError, "weights must be [B, Hkv, max_positions]");
+    const int32_t positions = a.size(w, 2, "weights");
     if (!a.ok()) return nullptr;
     void *st = stream();
     return unlocked([&] {
         return api.reader_prompt_key_weights(d, (int32_t)N, data<void>(q), data<float>(lse), data<int32_t>(cu), window, data<void>(kc),
-                                             data<int32_t>(table), data<int32_t>(lens), (float)decay, data<float>(w), (int32_t)w->size(2),
+                                             data<int32_t>(table), data<int32_t>(lens), (float)decay, data<float>(w), positions,
                                              max_len, status, st);
     });
 }
@@ -531,12 +546,13 @@ PyObject *py_kv_evict(PyObject *const *args, Py_ssize_t n) {
     a.on_current_device();
     if (a.ok() && (w->dim() != 4 || w->size(0) != NL || w->size(1) != B || w->size(2) != Hkv))
         a.reject(PyExc_ValueError, "weights must be [num_layers, B, Hkv, max_positions]");
+    const int32_t positions = a.size(w, 3, "weights"), layers = a.size(k, 0, "k_cache");
     if (!a.ok()) return nullptr;
     void *st = stream();
     const size_t ws_bytes = ws ? ws->nbytes() : 0;
     return unlocked([&] {
-        return api.reader_kv_evict(d, (int32_t)NL, keep, recent, data<void>(k), data<void>(v), data<int32_t>(table), data<int32_t>(lens),
-                                   data<float>(w), (int32_t)w->size(3), data<void>(ws), ws_bytes, status, st);
+        return api.reader_kv_evict(d, layers, keep, recent, data<void>(k), data<void>(v), data<int32_t>(table), data<int32_t>(lens),
+                                   data<float>(w), positions, data<void>(ws), ws_bytes, status, st);
     });
 }
 

@@ -78,6 +78,13 @@ def test_null_pointers(R, name):
 
 
 @pytest.mark.parametrize("name", NAMES)
+def test_tensors_that_start_between_16_bytes(R, name):
+    wide = {"qkv", "cos_sin", "q", "q_norm", "k_norm", "k_tree", "v_tree", "k_cache", "v_cache", "out"}
+    for p in wide & set(POINTERS[name]):
+        assert call(R, name, dims(R), **{p: ctypes.c_void_p(4096 + 8)}) == EINVAL, p
+
+
+@pytest.mark.parametrize("name", NAMES)
 def test_an_empty_batch_is_nothing_to_do(R, name):
     assert call(R, name, dims(R, B=0), **{p: None for p in POINTERS[name]}) == OK
 
