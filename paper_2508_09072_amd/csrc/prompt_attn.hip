@@ -30,8 +30,9 @@ constexpr int kPromptThreads = 256, kPromptStages = 4, kPromptRows = 256;
 constexpr int kPromptSlots = 256;                    // tiles of the list that are kept in LDS
 constexpr int kPromptSeqsInLds = 2048;               // batches up to this size keep lengths and bounds in LDS
 // What a block costs beyond its tiles, in keys (the query rows to fetch and the first tile's maxima in front, masks, normalising
-// and writing behind), when the axis is cut.
-constexpr int kBlockFront = 3 * kTile, kBlockCost = 6 * kTile;
+// and writing behind), when the axis is cut.  (Six tiles instead of eight: the range with the first, short blocks of a head of 16384
+// tokens took 13 % longer than the others, the whole call 4 %; ten: the same there, ragged prompts 3 % longer.)
+constexpr int kBlockFront = 4 * kTile, kBlockCost = 8 * kTile;
 constexpr int kMinRange = 4 * kTile;                 // no range is shorter than this: a range costs as much before its first tile
 using Block = PromptBlock<kTile, kBlockFront, kBlockCost>;
 
@@ -185,10 +186,10 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
     struct QueryRows {
         u32x4 w[2][G::kKSteps];
     };
-    auto fetch_q = [&](QueryRows &q) {
+    auto fetch_q = [&](QueryRows &q, int head, int row0, int nt) {
         static_for<2>([&](auto rc) {
             constexpr int r = decltype(rc)::value;
-            const uint16_t *src = q_row(rc, seg_head, seg_row0, seg_nt);
+            const uint16_t *src = q_row(rc, head, row0, nt);
 #pragma unroll
             for (int kk = 0; kk < G::kKSteps; ++kk) q.w[r][kk] = ld16(src + kk * 16 + h * 8);
         });
@@ -212,7 +213,7 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
     // waited for together with them)
     seg_head = rg.at.head; seg_row0 = rg.at.c0 + rg.at.k * tb; seg_nt = rg.at.tokens(tb);
     QueryRows first_q;
-    fetch_q(first_q);
+    fetch_q(first_q, seg_head, seg_row0, seg_nt);
 
     // ---- the tile list
     // Item i, found by walking the blocks from `walk`, whose first tile in the range is item walk_item; a thread each.
@@ -508,6 +509,22 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
         });
     };
 
+    // The reference of row block r: the maximum of the scores in the registers.  (A row that sees no key of the segment's first tile
+    // sees none of a later one either, by its place; behind pages that do not exist it may: its weights then are too large for the
+    // reference, and it is computed again.)
+    auto set_reference = [&](auto rc, bool holes) {
+        constexpr int r = decltype(rc)::value;
+        float mx = fmaxf(s[0][r][0], s[1][r][0]);
+#pragma unroll
+        for (int i = 1; i < 16; ++i) mx = fmaxf(fmaxf(mx, s[0][r][i]), s[1][r][i]);
+        // the other half of the row's keys sits in lane ^ 32
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+        mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+        const float ref = holes ? fmaxf(mx, -1e30f) : mx;
+        acc_write<Acc::m_ref(r)>(__float_as_uint(ref));
+        mc[r] = ref == -INFINITY ? 0.f : ref * c2;
+    };
+
     // Any tile, one step after the other: scores, masks, (first tile of a segment) row maxima, weights, products.
     auto tile_plain = [&](const char *stage, int flags, int n_valid, int t) {
         const bool first = (flags & kTileFresh) != 0;
@@ -521,19 +538,7 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
                 for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) s[kb][r][i] = keep(kb, r, i) ? s[kb][r][i] : -INFINITY;
-                if (first) {
-                    float mx = fmaxf(s[0][r][0], s[1][r][0]);
-#pragma unroll
-                    for (int i = 1; i < 16; ++i) mx = fmaxf(fmaxf(mx, s[0][r][i]), s[1][r][i]);
-                    // the other half of the row's keys sits in lane ^ 32
-                    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-                    mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
-                    // (a row that sees no key of this tile sees none of a later one either, by its place; behind pages that
-                    // do not exist it may: its weights then are too large for the reference, and it is computed again)
-                    const float ref = holes ? fmaxf(mx, -1e30f) : mx;
-                    acc_write<Acc::m_ref(r)>(__float_as_uint(ref));
-                    mc[r] = ref == -INFINITY ? 0.f : ref * c2;
-                }
+                if (first) set_reference(rc, holes != 0);
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -587,7 +592,7 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
             const float l = l_mine + __shfl_xor(l_mine, 32);
             const float inv = l == 0.f ? 0.f : 1.f / l;                 // (a row may see no key of a part)
             const float ref = __uint_as_float(acc_read_u32<Acc::m_ref(r)>()) * c2;
-            float check = l < kTooLarge ? 0.f : __builtin_nanf("");
+            float check[4] = {l < kTooLarge ? 0.f : __builtin_nanf(""), 0.f, 0.f, 0.f};
             uint16_t *orow = p.out + (((size_t)seg_row0 + tok) * p.Hq + (size_t)seg_head * p.G + group_of(rc)) * D;
             // A lane holds, per 8-wide chunk of the output row, 4 values and its partner lane (lane ^ 32) the other 4.
             static_for<G::kOBlocks * 2>([&](auto cc) {
@@ -596,7 +601,7 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
                 static_for<8>([&](auto ec) {
                     constexpr int e = decltype(ec)::value;
                     v[e] = acc_read<Acc::o(r, db) + 4 * i4 + e>() * inv;
-                    check = __builtin_fmaf(v[e], 0.f, check);            // (not a number once any value is none)
+                    check[e % 4] = __builtin_fmaf(v[e], 0.f, check[e % 4]);   // (not a number once any value is none)
                 });
                 if (whole) {
                     const uint32_t a0 = pack_bf16x2(v[0], v[1]), a1 = pack_bf16x2(v[2], v[3]);
@@ -623,7 +628,7 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
                         l == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(l)) * kLn2;
                 }
             }
-            again = again || __any(real && !(check == 0.f));
+            again = again || __any(real && !(check[0] + check[1] + check[2] + check[3] == 0.f));
         });
         if (!again) return;
         // the plain way, row after row: what has just been written is written again, behind it
@@ -671,7 +676,8 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
     int2 d_nxt = *reinterpret_cast<const int2 *>(&desc_of(1)->n_valid);
     int2 d_cpy = *reinterpret_cast<const int2 *>(&desc_of(kS - 1)->n_valid);
     int d_blk = desc_of(kS - 1)->blk[cw];
-    auto is_whole = [](int valid, int flags) { return ((valid ^ kTile) | (flags & (kTileFresh | kTileMasked | kTileHoles))) == 0; };
+    auto is_whole = [](int valid, int flags) { return ((valid ^ kTile) | (flags & (kTileMasked | kTileHoles))) == 0; };
+    auto goes_on = [](int valid, int flags) { return ((valid ^ kTile) | (flags & (kTileFresh | kTileMasked | kTileHoles))) == 0; };
 
     struct Iter {
         int t_valid, t_flags;          // the tile to compute
@@ -703,7 +709,7 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
         const bool copy_next = it + kS - 1 < n_iter;
         I.copy_stage_lds = ring_lds + ((unsigned)(it + kS - 1) % kS) * G::kStageBytes;
         I.whole = is_whole(I.t_valid, I.t_flags);
-        I.pipelined = wave_active && I.whole && !I.last_iter && is_whole(n_valid, n_flags);
+        I.pipelined = wave_active && I.whole && !I.last_iter && goes_on(n_valid, n_flags);
         const bool whole_next = I.c_blk >= 0 && (cw + 1) * G::kRowsPerWave <= c_valid;
         I.copy_inside = copy_next && I.pipelined && whole_next;
         if (copy_next && !I.copy_inside) issue_tile(I.c_blk, c_valid, I.copy_stage_lds);
@@ -715,29 +721,22 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
     };
     auto whole_at = [&](int i) {
         const int2 d = *reinterpret_cast<const int2 *>(&desc_of(i)->n_valid);
-        return is_whole(word(d.x), word(d.y));
+        return goes_on(word(d.x), word(d.y));
     };
     auto stage_of = [&](int it) { return ring + ((unsigned)it % kS) * G::kStageBytes; };
 
+    seg_p0 = word(desc_of(0)->p0); seg_t0 = word(desc_of(0)->t);
+    wave_active = wave_token < seg_nt;
+    reset_state();
     for (int it = 0; it < n_iter; ++it) {
-        if (word(d_cur.y) & kTileFresh) {
-            const PromptTile *d = desc_of(it);
-            seg_head = word(d->head); seg_row0 = word(d->row0); seg_p0 = word(d->p0); seg_nt = word(d->nt); seg_t0 = word(d->t);
-            wave_active = wave_token < seg_nt;
-            reset_state();
-            if (it > 0) {
-                QueryRows q;
-                fetch_q(q);
-                put_q(q);
-            }
-        }
         Iter I = begin_iteration(it);
-        if (!wave_active) continue;
-        if (!I.whole) {
+        if (!wave_active) {
+        } else if (!I.whole) {
             tile_plain(stage_of(it), I.t_flags, I.t_valid, word(desc_of(it)->t));
         } else {
             // A run of whole tiles.  All but its last tile are pipelined, in a loop of their own.
             scores(stage_of(it));
+            if (I.t_flags & kTileFresh) static_for<2>([&](auto rc) { set_reference(rc, false); });
             begin_run();
             while (I.pipelined) {
                 if (I.copy_inside) {
@@ -753,7 +752,7 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
                         ++it;
                         blk = word(d_blk);
                         const int c_valid = word(d_cpy.x), c_flags = word(d_cpy.y);
-                        if (it >= end || (whole & 1u) == 0 || !is_whole(c_valid, c_flags)) break;
+                        if (it >= end || (whole & 1u) == 0 || !goes_on(c_valid, c_flags)) break;
                         whole = (whole >> 1) | 2u;
                         wait_vmcnt<kCopiesPerTile>();
                         __syncthreads();        // tiles it and it + 1 are complete in LDS; every wavefront is done with tile it - 1
@@ -772,7 +771,21 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
             weights_of_key_block(1);
             products(stage_of(it));
         }
-        if (I.t_flags & kTileEnds) finish_segment(I.t_flags, word(desc_of(it)->t) + 1, word(desc_of(it)->b));
+        if (I.t_flags & kTileEnds) {
+            // the next segment's query rows are on their way while this one's outputs are written
+            const PromptTile *d = desc_of(it), *d2 = desc_of(it + 1);
+            const int head = word(d2->head), row0 = word(d2->row0), p0 = word(d2->p0), nt = word(d2->nt), t0 = word(d2->t);
+            QueryRows q;
+            if (D == 64 && !I.last_iter) fetch_q(q, head, row0, nt);
+            if (wave_active) finish_segment(I.t_flags, word(d->t) + 1, word(d->b));
+            if (!I.last_iter) {
+                seg_head = head; seg_row0 = row0; seg_p0 = p0; seg_nt = nt; seg_t0 = t0;
+                wave_active = wave_token < seg_nt;
+                if (D == 128) fetch_q(q, head, row0, nt);
+                reset_state();
+                put_q(q);
+            }
+        }
     }
     if (p.status && bad) atomicOr(p.status, bad);
 }
