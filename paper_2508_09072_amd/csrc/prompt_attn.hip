@@ -242,6 +242,8 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
 #pragma unroll
         for (int j = 0; j < 4; ++j) page[j] = j * 16 < n_valid ? row[j] : 0;     // (position < keys <= 16 max_pages)
 #pragma unroll
+        for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(page[j]));   // (a load that is not waited for here is waited for in the main loop, with all copies)
+#pragma unroll
         for (int j = 0; j < 4; ++j) {
             slot->blk[j] = -1;
             if (j * 16 >= n_valid) continue;
