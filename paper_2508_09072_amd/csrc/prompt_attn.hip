@@ -242,7 +242,7 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
 #pragma unroll
         for (int j = 0; j < 4; ++j) page[j] = j * 16 < n_valid ? row[j] : 0;     // (position < keys <= 16 max_pages)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(page[j]));   // (a load that is not waited for here is waited for in the main loop, with all copies)
+        for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(page[j]));
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             slot->blk[j] = -1;
@@ -357,6 +357,35 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
         lsum[r][1] += p1;
         pk[kb][r][i >> 3][(i >> 1) & 3] = pack_bf16x2(p0, p1);
     };
+    // Which keys of a tile row block r sees: a bit for each (word 0 and 1: key blocks 0 and 1), the lane's 4 h taken off.
+    // Score i of a key block has bit key_bit(i); a bit is spread over a register to choose between the score and minus infinity,
+    // two instructions and no scalar register, of which comparisons would take two each.
+    struct Sees { uint32_t w[2][2]; };   // [key block][row block]
+    auto key_bit = [](int i) { return (i >> 2) * 8 + (i & 3); };
+    auto sees_of = [&](int n_valid, int t) {
+        Sees o;
+        static_for<2>([&](auto rc) {
+            constexpr int r = decltype(rc)::value;
+            const int tok = token_of(rc), lim = (tok < seg_nt ? min(n_valid, seg_p0 + tok + 1 - t * kTile) : 0) - 4 * h;
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                const int n = min(max(lim - kb * 32, 0), 32);
+                o.w[kb][r] = n == 32 ? ~0u : (1u << n) - 1u;
+                asm volatile("" : "+v"(o.w[kb][r]));
+            }
+        });
+        return o;
+    };
+    auto seen = [](uint32_t word, int bit, float x) {
+        const uint32_t m = (uint32_t)__builtin_amdgcn_sbfe((int)word, bit, 1);
+        return __uint_as_float((m & __float_as_uint(x)) | (~m & 0xff800000u));
+    };
+    auto mask = [&](int kb, const Sees &o) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[kb][r][i] = seen(o.w[kb][r], key_bit(i), s[kb][r][i]);
+    };
     // The weights of pipelined tiles are a pipeline of their own, one per matrix instruction: slot e takes the exponential of
     // the argument made in slot e - 1, makes the argument of weight e + 1, adds weight e - 1 to its row's sum and, when e is even,
     // packs weights e - 2 and e - 1, so that no instruction of a slot waits for another of it.  All of it is written out, so
@@ -368,12 +397,14 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
         asm volatile("v_fma_f32 %0, %1, %2, -%3" : "=v"(x) : "v"(score), "v"(c2), "v"(ref));
         return x;
     };
-    auto weight_slot = [&](auto wkbc, auto ec) {
+    // masked: o[0] and o[1] say what of the current and of the next tile is seen
+    auto weight_slot = [&](auto wkbc, auto ec, auto masked, const Sees (&o)[2]) {
         constexpr int wkb = decltype(wkbc)::value, e = decltype(ec)::value;
         float p_cur;
         asm volatile("v_exp_f32 %0, %1" : "=v"(p_cur) : "v"(w_x));
         constexpr int nb = e == 31 ? 1 - wkb : wkb, ne = (e + 1) & 31;
         w_x = weight_arg(s[nb][ne / 16][ne % 16], mc[ne / 16]);
+        if constexpr (decltype(masked)::value) w_x = seen(o[wkb == 1 && e < 31 ? 0 : 1].w[nb][ne / 16], key_bit(ne % 16), w_x);
         constexpr int pe = (e + 31) & 31;
         asm volatile("v_add_f32 %0, %0, %1" : "+v"(lsum[pe / 16][pe & 1]) : "v"(w_p1));
         if constexpr ((e & 1) == 0) {
@@ -455,8 +486,9 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
     //   O += V(t, kb)^T.P(t, kb)^T  with the weights made in the half step before;
     //   weights of the other key block: of (t, 1) in half step 0, of (t+1, 0) in half step 1, one score per matrix instruction.
     // Operand fragments are read from LDS two groups of four matrix instructions ahead.  with_copy: the copies of a whole tile
-    // (base addresses kbase / vbase, LDS address copy_stage_lds) are issued on the way, spread over the tile.
-    auto tile_pipelined = [&](auto with_copy, const char *stage, const char *next_stage, const char *kbase, const char *vbase,
+    // (base addresses kbase / vbase, LDS address copy_stage_lds) are issued on the way, spread over the tile.  masked: rows do not see
+    // some keys of the tile or of the next one.
+    auto tile_pipelined = [&](auto with_copy, auto masked, const Sees (&sees)[2], const char *stage, const char *next_stage, const char *kbase, const char *vbase,
                               unsigned copy_stage_lds) {
         constexpr int kK = G::kKSteps, kOB = G::kOBlocks;
         static_assert(kK == 2 * kOB, "a half step has as many score as product instructions");
@@ -505,7 +537,7 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
                 }
                 // weights of the other key block (of the next tile in half step 1), 32 scores over 4 kK slots
                 constexpr int lo = j * 32 / (4 * kK), hi = (j + 1) * 32 / (4 * kK);
-                static_for<hi - lo>([&](auto ic) { weight_slot(std::integral_constant<int, 1 - kb>{}, std::integral_constant<int, lo + decltype(ic)::value>{}); });
+                static_for<hi - lo>([&](auto ic) { weight_slot(std::integral_constant<int, 1 - kb>{}, std::integral_constant<int, lo + decltype(ic)::value>{}, masked, sees); });
                 __builtin_amdgcn_sched_barrier(0);
             });
         });
@@ -527,43 +559,22 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
         mc[r] = ref == -INFINITY ? 0.f : ref * c2;
     };
 
-    // Any tile, one step after the other: scores, masks, (first tile of a segment) row maxima, weights, products.
+    // A tile with keys behind page ids that do not exist, one step after the other.
     auto tile_plain = [&](const char *stage, int flags, int n_valid, int t) {
-        const bool first = (flags & kTileFresh) != 0;
         const int holes = (flags >> 8) & 15;
         scores(stage);
-        // keep(kb, r, i): does score i of block (kb, r) belong to a key this row attends to
-        auto softmax = [&](auto &&keep) {
-            static_for<2>([&](auto rc) {
-                constexpr int r = decltype(rc)::value;
+        const Sees o = sees_of(n_valid, t);
+        mask(0, o);
+        mask(1, o);
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[kb][r][i] = keep(kb, r, i) ? s[kb][r][i] : -INFINITY;
-                if (first) set_reference(rc, holes != 0);
+            for (int r = 0; r < 2; ++r)
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int i = 0; i < 16; i += 2) weight_pair(kb, r, i);
-            });
-        };
-        if (flags & (kTileMasked | kTileHoles)) {
-            // score i of block kb is key kb * 32 + (i / 4) * 8 + 4 h + i % 4 of the tile; the lane's part of the comparison is made
-            // here, out of the compiler's sight, or 64 key numbers would wait in registers through the whole main loop
-            int lim[2];
-            static_for<2>([&](auto rc) {
-                constexpr int r = decltype(rc)::value;
-                const int tok = token_of(rc);
-                lim[r] = (tok < seg_nt ? min(n_valid, seg_p0 + tok + 1 - t * kTile) : 0) - 4 * h;
-                asm volatile("" : "+v"(lim[r]));
-            });
-            softmax([&](int kb, int r, int i) {
-                return kb * 32 + (i >> 2) * 8 + (i & 3) < lim[r] && !((holes >> (kb * 2 + (i >> 3))) & 1);
-            });
-        } else {
-            softmax([](int, int, int) { return true; });
-        }
-        asm volatile("s_nop 3");   // (weights written by the vector ALU are matrix operands next)
+                for (int i = 0; i < 16; ++i) s[kb][r][i] = (holes >> (kb * 2 + (i >> 3))) & 1 ? -INFINITY : s[kb][r][i];
+        if (flags & kTileFresh) static_for<2>([&](auto rc) { set_reference(rc, true); });
+        weights_of_key_block(0);
+        weights_of_key_block(1);
         products(stage);
     };
 
@@ -678,14 +689,15 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
     int2 d_nxt = *reinterpret_cast<const int2 *>(&desc_of(1)->n_valid);
     int2 d_cpy = *reinterpret_cast<const int2 *>(&desc_of(kS - 1)->n_valid);
     int d_blk = desc_of(kS - 1)->blk[cw];
-    auto is_whole = [](int valid, int flags) { return ((valid ^ kTile) | (flags & (kTileMasked | kTileHoles))) == 0; };
+    auto is_masked = [](int valid, int flags) { return ((valid ^ kTile) | (flags & kTileMasked)) != 0; };
     auto goes_on = [](int valid, int flags) { return ((valid ^ kTile) | (flags & (kTileFresh | kTileMasked | kTileHoles))) == 0; };
 
     struct Iter {
         int t_valid, t_flags;          // the tile to compute
         int c_blk;                     // first page block of the tile to copy (this wavefront's rows), or -1
         unsigned copy_stage_lds;
-        bool last_iter, whole, pipelined, copy_inside;
+        bool last_iter, runs, masked;  // runs: tiles without holes
+        bool pipelined, closing, copy_inside;   // the next tile of the run is whole; it, or this one, is masked
     };
     auto begin_iteration = [&](int it) {
         Iter I;
@@ -710,8 +722,11 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
         // Tile it + kS - 1 goes into the stage that tile it - 1 has left.
         const bool copy_next = it + kS - 1 < n_iter;
         I.copy_stage_lds = ring_lds + ((unsigned)(it + kS - 1) % kS) * G::kStageBytes;
-        I.whole = is_whole(I.t_valid, I.t_flags);
-        I.pipelined = wave_active && I.whole && !I.last_iter && goes_on(n_valid, n_flags);
+        I.runs = (I.t_flags & kTileHoles) == 0;
+        I.masked = is_masked(I.t_valid, I.t_flags);
+        const bool more = wave_active && I.runs && !I.last_iter && (n_flags & (kTileFresh | kTileHoles)) == 0;
+        I.pipelined = more && !I.masked && goes_on(n_valid, n_flags);
+        I.closing = more && !I.pipelined;
         const bool whole_next = I.c_blk >= 0 && (cw + 1) * G::kRowsPerWave <= c_valid;
         I.copy_inside = copy_next && I.pipelined && whole_next;
         if (copy_next && !I.copy_inside) issue_tile(I.c_blk, c_valid, I.copy_stage_lds);
@@ -730,17 +745,23 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
     seg_p0 = word(desc_of(0)->p0); seg_t0 = word(desc_of(0)->t);
     wave_active = wave_token < seg_nt;
     reset_state();
+    const Sees kNone[2] = {};
     for (int it = 0; it < n_iter; ++it) {
         Iter I = begin_iteration(it);
         if (!wave_active) {
-        } else if (!I.whole) {
+        } else if (!I.runs) {
             tile_plain(stage_of(it), I.t_flags, I.t_valid, word(desc_of(it)->t));
         } else {
-            // A run of whole tiles.  All but its last tile are pipelined, in a loop of their own.
+            // A run of tiles.  All but its last tile are pipelined, whole ones in a loop of their own.
             scores(stage_of(it));
+            if (I.masked) {
+                const Sees o = sees_of(I.t_valid, word(desc_of(it)->t));
+                mask(0, o);
+                mask(1, o);
+            }
             if (I.t_flags & kTileFresh) static_for<2>([&](auto rc) { set_reference(rc, false); });
             begin_run();
-            while (I.pipelined) {
+            while (I.pipelined || I.closing) {
                 if (I.copy_inside) {
                     // The middle of a run: as long as the tile after next and the tile to copy are whole too, a loop with one path
                     // through it and nothing between two tiles but the wait, the barrier and the words of the next tile to copy.
@@ -749,7 +770,7 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
                     const int end = min(n_iter - kS + 1, (it | (kPromptSlots / 2 - 1)) + 1);         // (the list is extended by the general head)
                     for (;;) {
                         const size_t boff = (size_t)(unsigned)blk * (16 * G::kRowBytes);
-                        tile_pipelined(std::true_type{}, stage_of(it), stage_of(it + 1), reinterpret_cast<const char *>(p.k_cache) + boff,
+                        tile_pipelined(std::true_type{}, std::false_type{}, kNone, stage_of(it), stage_of(it + 1), reinterpret_cast<const char *>(p.k_cache) + boff,
                                        reinterpret_cast<const char *>(p.v_cache) + boff, ring_lds + ((unsigned)(it + kS - 1) % kS) * G::kStageBytes);
                         ++it;
                         blk = word(d_blk);
@@ -763,13 +784,21 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
                     }
                     d_cur = *reinterpret_cast<const int2 *>(&desc_of(it)->n_valid);
                     d_nxt = *reinterpret_cast<const int2 *>(&desc_of(it + 1)->n_valid);
+                } else if (I.pipelined) {
+                    tile_pipelined(std::false_type{}, std::false_type{}, kNone, stage_of(it), stage_of(it + 1), nullptr, nullptr, 0u);
+                    ++it;
                 } else {
-                    tile_pipelined(std::false_type{}, stage_of(it), stage_of(it + 1), nullptr, nullptr, 0u);
+                    const PromptTile *d = desc_of(it), *d2 = desc_of(it + 1);
+                    const Sees sees[2] = {sees_of(I.t_valid, word(d->t)), sees_of(word(d2->n_valid), word(d2->t))};
+                    tile_pipelined(std::false_type{}, std::true_type{}, sees, stage_of(it), stage_of(it + 1), nullptr, nullptr, 0u);
                     ++it;
                 }
                 I = begin_iteration(it);    // (a whole tile that starts no segment: nothing else to prepare)
             }
             end_run();
+            if (I.masked) {
+                mask(1, sees_of(I.t_valid, word(desc_of(it)->t)));
+            }
             weights_of_key_block(1);
             products(stage_of(it));
         }
