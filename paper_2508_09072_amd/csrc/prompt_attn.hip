@@ -107,11 +107,7 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
                 c = Block::sequence_cost(seqs.length(b), nn, tb);
                 if (len < 0 || lo < 0 || hi < lo || hi > p.N || (long long)len + nn > p.max_seq_len) bad |= READER_STATUS_BAD_LENGTH;
             }
-#pragma unroll
-            for (int off = 1; off < 64; off <<= 1) {
-                const long long v = __shfl_up(c, off);
-                if (lane >= off) c += v;
-            }
+            c = scan64(c);
             if (lane == 63) s_wave[wave_s] = c;
             __syncthreads();
             long long before = carry;
@@ -154,10 +150,10 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
         o.load(seqs);
         return o.locate(r - s_pref[lo], seqs, p.B, tb);
     };
-    Block from, to;
-    const int t_from = locate(axis.begin(range), from), t_to = locate(axis.begin(range + 1), to);
-    const PromptRange<Block> rg(from, t_from, to, t_to, p.Hkv);
-    const RangeNote note = rg.note(seqs, p.B, tb);
+    Block place;
+    const int t_place = locate(axis.begin(range + h), place);
+    const PromptRange<Block> rg(place, t_place, p.Hkv);
+    const RangeNote note = rg.note(seqs, p.B, tb, lane);
     if (tid == 0) notes[range] = note;
     const int n_iter = __builtin_amdgcn_readfirstlane(note.tiles);
     if (n_iter == 0) return;
@@ -263,7 +259,7 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
             walk_item += to - from;
             walk_first = false;
             walk.next(seqs, p.B, tb);
-            walk.make_uniform();
+            walk = walk.of_lane(0);
         }
     };
     __syncthreads();   // the list is written

@@ -15,15 +15,6 @@ using Block = PromptBlock<kStep, 2 * kStep, 4 * kStep>;
 // Wavefronts of a compute unit that run at once: as many as their stages fit the LDS.
 constexpr int few_wavefronts(int D) { return D == 128 ? 4 : 8; }
 
-__device__ __forceinline__ long long scan64(long long c, int lane) {
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const long long v = __shfl_up(c, off);
-        if (lane >= off) c += v;
-    }
-    return c;
-}
-
 constexpr int kWaves = 4;
 
 // kBlocks: blocks of 16 query rows
@@ -45,7 +36,7 @@ __global__ __launch_bounds__(64 * kWaves) void prompt_few_kernel(PromptParams p)
 
     // ---- this workgroup's range of the axis (every wavefront finds it for itself)
     long long per_head = 0;
-    for (int base = 0; base < p.B; base += 64) {
+    auto cost_up_to = [&](int base) {                    // of sequences `base` .. base + lane, and what they have wrong
         const int b = base + lane;
         long long c = 0;
         if (b < p.B) {
@@ -53,8 +44,11 @@ __global__ __launch_bounds__(64 * kWaves) void prompt_few_kernel(PromptParams p)
             c = Block::sequence_cost(seqs.length(b), nn, tb);
             if (len < 0 || lo < 0 || hi < lo || hi > p.N || (long long)len + nn > p.max_seq_len) bad |= READER_STATUS_BAD_LENGTH;
         }
-        per_head += __shfl(scan64(c, lane), 63);
-    }
+        return scan64(c);
+    };
+    const long long upto0 = cost_up_to(0);
+    per_head = lane64(upto0, 63);
+    for (int base = 64; base < p.B; base += 64) per_head += lane64(cost_up_to(base), 63);
     if (bad && blockIdx.x == 0 && p.status) atomicOr(p.status, bad);
     bad = 0;
     const long long total = per_head * p.Hkv;
@@ -66,33 +60,37 @@ __global__ __launch_bounds__(64 * kWaves) void prompt_few_kernel(PromptParams p)
         return;
     }
     const PromptAxis axis(per_head, p.Hkv, (int)n_ranges);
-    auto locate = [&](long long x, Block &o) {
-        if (x >= total) {
-            o = Block{p.Hkv, 0, 0, 0, 0, 0};
-            return 0;
-        }
-        long long r;
-        o.head = axis.head(x, r);
-        long long carry = 0;
-        for (int base = 0;; base += 64) {
-            const int b = base + lane;
-            const long long upto = carry + scan64(b < p.B ? Block::sequence_cost(seqs.length(b), seqs.tokens(b), tb) : 0, lane);
-            const long long all = __shfl(upto, 63);
-            if (r < all) {                               // (the last of these 64 at the latest: r is below per_head)
-                const int i = (int)__popcll(__ballot(upto <= r));
-                o.b = base + i;
-                carry = i > 0 ? __shfl(upto, i - 1) : carry;
-                break;
+    // the places where the range begins and, in lanes 32..63, where the next one does: head, sequence, then the tile
+    Block place = {p.Hkv, 0, 0, 0, 0, 0};
+    int t_place = 0;
+    {
+        const long long x = axis.begin(range + (lane >> 5));
+        long long r = 0;
+        if (x < total) place.head = axis.head(x, r);
+        long long before = 0;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const long long r_half = lane64(r, 32 * half);
+            long long carry = 0, upto = upto0;
+            for (int base = 0;; base += 64) {
+                if (base > 0) upto = cost_up_to(base);
+                const long long all = carry + lane64(upto, 63);
+                if (r_half < all) {                      // (the last of these 64 at the latest: r is below per_head)
+                    const int i = (int)__popcll(__ballot(carry + upto <= r_half));
+                    if (i > 0) carry += lane64(upto, i - 1);
+                    if ((lane >> 5) == half) place.b = base + i, before = carry;
+                    break;
+                }
+                carry = all;
             }
-            carry = all;
         }
-        o.load(seqs);
-        return o.locate(r - carry, seqs, p.B, tb);
-    };
-    Block from, to;
-    const int t_from = locate(axis.begin(range), from), t_to = locate(axis.begin(range + 1), to);
-    const PromptRange<Block> rg(from, t_from, to, t_to, p.Hkv);
-    const RangeNote note = rg.note(seqs, p.B, tb);
+        if (x < total) {
+            place.load(seqs);
+            t_place = place.locate(r - before, seqs, p.B, tb);
+        } else place.b = 0;
+    }
+    const PromptRange<Block> rg(place, t_place, p.Hkv);
+    const RangeNote note = rg.note(seqs, p.B, tb, lane);
     if (threadIdx.x == 0) notes[range] = note;
 
     const Page page(lane);
@@ -211,7 +209,7 @@ __global__ __launch_bounds__(64 * kWaves) void prompt_few_kernel(PromptParams p)
         }
         if (last_block) break;
         o.next(seqs, p.B, tb);
-        o.make_uniform();
+        o = o.of_lane(0);
     }
     if (p.status && bad) atomicOr(p.status, bad);
 }

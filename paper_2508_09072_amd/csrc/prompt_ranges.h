@@ -19,6 +19,25 @@ struct RangeNote {
 constexpr int kMaxRanges = kNumCU * 8;
 constexpr size_t kNotesBytes = (size_t)kMaxRanges * sizeof(RangeNote);   // in front of the records, two a range
 
+// Sums of the lanes up to each.
+template <int kControl, int kRows>
+__device__ __forceinline__ long long add_from(long long v) {
+    const int lo = __builtin_amdgcn_update_dpp(0, (int)v, kControl, kRows, 0xf, kRows == 0xf);
+    const int hi = __builtin_amdgcn_update_dpp(0, (int)(v >> 32), kControl, kRows, 0xf, kRows == 0xf);
+    return v + (((long long)hi << 32) | (unsigned)lo);
+}
+__device__ __forceinline__ long long scan64(long long v) {
+    v = add_from<0x111, 0xf>(v);             // row_shr:1, 2, 4, 8
+    v = add_from<0x112, 0xf>(v);
+    v = add_from<0x114, 0xf>(v);
+    v = add_from<0x118, 0xf>(v);
+    v = add_from<0x142, 0xa>(v);             // row_bcast:15 into rows 1 and 3
+    return add_from<0x143, 0xc>(v);          // row_bcast:31 into rows 2 and 3
+}
+__device__ __forceinline__ long long lane64(long long v, int lane) {
+    return ((long long)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32) | (unsigned)__builtin_amdgcn_readlane((int)v, lane);
+}
+
 // Lengths and bounds of the sequences, from LDS or from memory.
 struct Sequences {
     const int32_t *lens, *cu;
@@ -77,10 +96,10 @@ struct PromptBlock {
         next(s, B, tb);                      // (may step behind the last head: the end)
         return 0;
     }
-    // every lane of the wavefront has the same
-    __device__ __forceinline__ void make_uniform() {
-        head = __builtin_amdgcn_readfirstlane(head); b = __builtin_amdgcn_readfirstlane(b); k = __builtin_amdgcn_readfirstlane(k);
-        L = __builtin_amdgcn_readfirstlane(L); n = __builtin_amdgcn_readfirstlane(n); c0 = __builtin_amdgcn_readfirstlane(c0);
+    // the place that a lane has found, for all of them
+    __device__ __forceinline__ PromptBlock of_lane(int lane) const {
+        return PromptBlock{__builtin_amdgcn_readlane(head, lane), __builtin_amdgcn_readlane(b, lane), __builtin_amdgcn_readlane(k, lane),
+                           __builtin_amdgcn_readlane(L, lane), __builtin_amdgcn_readlane(n, lane), __builtin_amdgcn_readlane(c0, lane)};
     }
 };
 
@@ -109,10 +128,11 @@ template <class Block>
 struct PromptRange {
     Block at;
     int t_lo, t_hi, stop_head, stop_b, stop_k, heads;
-    __device__ __forceinline__ PromptRange(const Block &from, int t_from, const Block &to, int t_to, int Hkv) : at(from), heads(Hkv) {
-        at.make_uniform();
-        t_lo = __builtin_amdgcn_readfirstlane(t_from); t_hi = __builtin_amdgcn_readfirstlane(t_to);
-        stop_head = __builtin_amdgcn_readfirstlane(to.head); stop_b = __builtin_amdgcn_readfirstlane(to.b); stop_k = __builtin_amdgcn_readfirstlane(to.k);
+    // `o` and `t`: lanes 0..31 have found the first tile, the others the one behind the last.  (Side by side: a search costs as much
+    // for one place as for two, a microsecond and a half.)
+    __device__ __forceinline__ PromptRange(const Block &o, int t, int Hkv) : at(o.of_lane(0)), heads(Hkv) {
+        t_lo = __builtin_amdgcn_readlane(t, 0); t_hi = __builtin_amdgcn_readlane(t, 32);
+        stop_head = __builtin_amdgcn_readlane(o.head, 32); stop_b = __builtin_amdgcn_readlane(o.b, 32); stop_k = __builtin_amdgcn_readlane(o.k, 32);
     }
     __device__ __forceinline__ bool is_stop(const Block &o) const { return o.head == stop_head && (o.head == heads || (o.b == stop_b && o.k == stop_k)); }
     __device__ __forceinline__ bool behind(const Block &o) const { return o.head >= heads || (is_stop(o) && t_hi == 0); }
@@ -121,25 +141,35 @@ struct PromptRange {
         from = first ? t_lo : 0;
         to = is_stop(o) ? t_hi : o.tiles(tb, max_len);
     }
-    // its tiles, and what it leaves to the merge
-    __device__ __forceinline__ RangeNote note(const Sequences &s, int B, int tb) const {
+    // its tiles, and what it leaves to the merge: blocks of a sequence 64 at a time, a lane each
+    __device__ __forceinline__ RangeNote note(const Sequences &s, int B, int tb, int lane) const {
         RangeNote r = {};
+        if (behind(at)) return r;
+        const int from0 = t_lo, all0 = at.tiles(tb, s.max_len), to0 = is_stop(at) ? t_hi : all0;
+        if (from0 > 0 && to0 > from0 && to0 == all0) r.ends = 1;
+        int tiles = 0;
         Block o = at;
         for (bool first = true; !behind(o); first = false) {
-            int from, to;
-            share(o, first, tb, s.max_len, from, to);
-            const int all = o.tiles(tb, s.max_len);
-            if (to > from) {
-                r.tiles += to - from;
-                if (from > 0 && to == all) r.ends = 1;
-                if (from == 0 && to < all) {
+            const bool here = o.head == stop_head && o.b == stop_b;         // (the range's last sequence)
+            const int last = here ? stop_k : (o.n + tb - 1) / tb - 1;
+            for (int k = o.k + lane; k <= last; k += 64) {
+                Block c = o;
+                c.k = k;
+                const int from = first && k == o.k ? t_lo : 0, to = here && k == last ? t_hi : c.tiles(tb, s.max_len);
+                tiles += max(to - from, 0);
+            }
+            const int begun = first && last == o.k ? t_lo : 0;              // of its last block there
+            o.k = last;
+            if (here) {
+                if (begun == 0 && t_hi > 0 && t_hi < o.tiles(tb, s.max_len)) {
                     r.open = 1;
                     r.head = o.head; r.row0 = o.c0 + o.k * tb; r.nt = o.tokens(tb);
                 }
+                break;
             }
-            if (is_stop(o)) break;
             o.next(s, B, tb);
         }
+        r.tiles = (int)lane64(scan64(tiles), 63);
         return r;
     }
 };
