@@ -46,7 +46,7 @@ static bool cache_ok(const reader_dims *dims, const void *k_cache, const void *v
 // Query rows a workgroup takes (reader_prompt_rows).
 //
 // Up to 16 rows that a sequence has for each kv head, on average (the host knows no more): the kernel that streams keys for few
-// rows.  Measured against the 256-row kernel: 16 single tokens on 1 to 16 K positions 98 against 122 us.
+// rows.  Measured against the 256-row kernel: 16 single tokens on 1 to 16 K positions 97 against 122 us.
 //
 // Beyond that the shortest of five estimates, in us:
 //   16, 32 rows: start and merge, and steps of 32 keys, which all blocks share out evenly (four wavefronts a compute unit); keys of
@@ -55,10 +55,10 @@ static bool cache_ok(const reader_dims *dims, const void *k_cache, const void *v
 //     full length), or what all blocks' steps take the compute units;
 //   256 rows: start, merge and imbalance, and per block what its tiles of 64 keys and its ends take, shared out evenly.
 // The constants are fitted to 168 shapes (7 head layouts; 1 to 64 sequences of 12 to 3000 tokens, chunks on up to 30 K positions).
-// Some of them, 16, 32, 64, 128 and 256 rows (32 query and 8 kv heads, D 128): one prompt of 100 tokens -, -, 6.5, 8.1, 19.5; of 800
-// -, -, 24.0, 28.2, 39.6; of 3000 -, -, 137, 106, 106; 16 of 300 -, -, 48.8, 42.3, 48.9; 64 tokens on 8 K positions 61, 42, 188, 229,
-// 79; 32 sequences of 12 on 8 K 476, 327, 216, 278, 196.  The estimates pick the fastest of the five on 138 of the 168 and are 1.6 %
-// behind it on average, 62 % at most (1500 tokens, 6 query heads and 1 kv head: 59 against 37 us).
+// Some of them, 16, 32, 64, 128 and 256 rows (32 query and 8 kv heads, D 128): one prompt of 100 tokens 16.1, 19.6, 6.6, 8.2, 18.9; of
+// 1500 220, 148, 43.2, 49.5, 50.6; of 3000 698, 440, 141, 101, 99; 16 of 300 216, 152, 50.6, 43.6, 42.9; 64 tokens on 8 K positions
+// 58, 40, 187, 230, 75; 32 sequences of 12 on 8 K 471, 322, 216, 278, 170.  The estimates pick the fastest of the five on 145 of the
+// 168 and are 1.2 % behind it on average, 33 % at most (256 tokens on 1000 positions, 64 query heads: 45 against 34 us).
 static int prompt_rows(const reader_dims &d, int32_t N, int32_t max_seq_len) {
     if (d.variant == 1) return 0;
     const int forced = tuning(READER_TUNE_PROMPT_ROWS), G = d.Hq / d.Hkv;
@@ -78,18 +78,18 @@ static int prompt_rows(const reader_dims &d, int32_t N, int32_t max_seq_len) {
         const double chain = (busy ? step_busy : step) * (longest / 32 + 0.5), all = all_steps * blocks(rows) * (average / 32 + 4) / kNumCU;
         return 5.5 + (chain > all ? chain : all);
     };
-    const double parts = blocks(256) < kNumCU / 4 ? (large ? 20.0 : 10.0) : 0.0;     // (every range leaves records, nothing else)
-    double best = 30.0 + parts + blocks(256) / kNumCU * (large ? 11.0 + 1.65 * (average / 64 + 0.5) : 8.0 + 0.9 * (average / 64 + 0.5));
+    const double parts = blocks(256) < kNumCU / 4 ? (large ? 20.0 : 12.0) : 0.0;     // (every range leaves records, nothing else)
+    double best = (large ? 26.0 : 24.0) + parts + blocks(256) / kNumCU * (large ? 7.0 + 1.6 * (average / 64 + 0.5) : 4.0 + 0.95 * (average / 64 + 0.5));
     int rows = 256;
     auto offer = [&](int r, double us) {
         if (us < best) { best = us; rows = r; }
     };
-    offer(16, large ? few(16, 17.0, 0.33) : few(16, 16.5, 0.155));
-    offer(32, large ? few(32, 18.0, 0.42) : few(32, 17.0, 0.24));
+    offer(16, large ? few(16, 13.7, 0.335) : few(16, 14.0, 0.156));
+    offer(32, large ? few(32, 16.3, 0.515) : few(32, 15.7, 0.22));
     // (block numbers of the uncut kernels are counted with the threads of a launch)
     if (((long long)N / (64 / G) + d.B) * d.Hkv < (1 << 23)) {
-        offer(128, large ? uncut(128, 0.93, 1.2, 0.72) : uncut(128, 0.64, 0.8, 0.43));
-        offer(64, large ? uncut(64, 0.76, 0.76, 0.50) : uncut(64, 0.50, 0.50, 0.27));
+        offer(128, large ? uncut(128, 0.93, 1.2, 0.57) : uncut(128, 0.64, 0.8, 0.43));
+        offer(64, large ? uncut(64, 0.75, 0.75, 0.45) : uncut(64, 0.50, 0.50, 0.29));
     }
     return rows;
 }
