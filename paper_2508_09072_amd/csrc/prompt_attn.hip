@@ -9,8 +9,12 @@
 // sequence, block, key) axis is cut evenly into one range per compute unit, whatever the lengths; a block that is cut leaves
 // partial records (fp32: outputs normalised by their own sum, reference, sum) that a second launch folds together.  Positions on
 // the axis are keys, not tiles: blocks of one sequence then add up to a closed form, and nobody has to count them.
-// Tiles travel HBM/L2 -> LDS through a ring of four, asked for three tiles ahead.  Whole tiles run as a software pipeline over
-// two tiles (see tile_pipelined): scores of the next tile, products of the current one and softmax weights alternate.
+// Tiles travel HBM/L2 -> LDS through a ring of four, asked for three tiles ahead.  Tiles run as a software pipeline over two of
+// them (see tile_pipelined): scores of the next tile, products of the current one and softmax weights alternate.
+// Bound by power where prompts are long: 16384 tokens, 32 query and 8 kv heads of 128, 2.03 to 2.11 ms, 1.04 to 1.08 PFLOP/s, at 1.5
+// GHz and 2750 cycles a tile, 2048 of them matrix work; heads of 64 2300, exponentials first.  Beyond its tiles a workgroup spends
+// 8 us before the first one and 5 to 8 us a block (measured with a clock in a copy of this file: masked tile, first tile's maxima,
+// outputs, query rows).
 //
 // A row's softmax reference is its maximum in the first tile of its range and is never moved: a lower reference makes all weights
 // larger by one factor, which fp32 sums and bf16 weights hold up to 2^100.  Rows that this cannot hold, and rows with an output

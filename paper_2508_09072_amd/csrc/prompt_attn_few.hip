@@ -4,7 +4,8 @@
 // (prompt_ranges.h; a block is 16 or 32 rows here) and its four wavefronts take the steps of 32 keys in turn, each through two stages
 // of its own in LDS, waiting for nobody; at the end of a segment they add up their rows.  (Wavefronts with ranges of their own
 // cut the blocks into four times as many parts: one token on 32 K positions 53 us instead of 37, 16 on 1 to 16 K 104 instead of
-// 99.)  Blocks that are cut leave fp32 records for a second launch.
+// 99.)  Blocks that are cut leave fp32 records for a second launch.  16 single tokens on 1 to 16 K positions, 32 query and 8 kv
+// heads of 128: 97 us, 5.9 TB/s, 87 of them this launch.
 #include "prompt_rows.h"
 
 namespace reader {
