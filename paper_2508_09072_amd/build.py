@@ -8,9 +8,11 @@ source tree; nothing is installed anywhere else.
 """
 from __future__ import annotations
 
+import concurrent.futures
 import os
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -24,6 +26,8 @@ NATIVE = os.path.join(HERE, "_reader_torch.so")
 SOURCES = ["reader_api.hip", "trie_drafter.cpp", "tree_shape.cpp", "accept_compact.hip", "kv_compact_layers.hip", "kv_rearrange.hip", "target_argmax.hip", "target_sample.hip", "tree_attn_scalar.hip", "tree_attn_mfma.hip", "tree_attn_wide.hip", "tree_attn_short.hip", "peak_probes.hip",
            "prompt_api.hip", "qkv_prepare.hip", "prompt_attn.hip", "prompt_attn_mid.hip", "prompt_attn_few.hip", "prompt_merge.hip",
            "prompt_attn_scalar.hip", "key_weights.hip", "kv_evict.hip"]
+# sources compiled at a time
+JOBS = 6
 # kernels that manage the accumulation registers by hand
 HAND_MANAGED = ["tree_attn_wide.hip", "prompt_attn.hip"]
 FLAGS = [
@@ -134,14 +138,26 @@ def build_library(verbose: bool = False, stamps: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     lib = STAMPS_LIB if stamps else LIB
     tmp = lib + ".tmp.%d" % os.getpid()
-    cmd = [hipcc] + FLAGS + (["-DREADER_WG_STAMPS"] if stamps else []) + ["-I" + os.path.join(ROOT, "include"), "-I" + CSRC]
-    cmd += [os.path.join(CSRC, s) for s in SOURCES] + ["-o", tmp]
+    cmd = [hipcc] + [f for f in FLAGS if f != "-shared"] + (["-DREADER_WG_STAMPS"] if stamps else [])
+    cmd += ["-c", "-I" + os.path.join(ROOT, "include"), "-I" + CSRC]
     if verbose:
-        print(" ".join(cmd))
-    res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    spilled = spilled_kernels(res.stdout)
+        print(" ".join(cmd + [os.path.join(CSRC, s) for s in SOURCES]))
+    with tempfile.TemporaryDirectory() as objects, concurrent.futures.ThreadPoolExecutor(JOBS) as pool:
+        checks = [pool.submit(check_wide_kernel, hipcc, verbose, source) for source in HAND_MANAGED]
+        names = [os.path.join(objects, s + ".o") for s in SOURCES]
+
+        def compile_one(source, name):
+            return subprocess.run(cmd + [os.path.join(CSRC, source), "-o", name], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+
+        compiled = list(pool.map(compile_one, SOURCES, names))
+        output, failed = "".join(r.stdout for r in compiled), any(r.returncode != 0 for r in compiled)
+        if not failed:
+            res = subprocess.run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC"] + names + ["-o", tmp], stdout=subprocess.PIPE,
+                                 stderr=subprocess.STDOUT, text=True)
+            output, failed = output + res.stdout, res.returncode != 0
+    spilled = spilled_kernels(output)
     kept, after_remark = [], False
-    for l in res.stdout.splitlines():
+    for l in output.splitlines():
         if "remark:" in l:
             after_remark = True
             continue
@@ -151,7 +167,7 @@ def build_library(verbose: bool = False, stamps: bool = False) -> str:
         if "not a recognized feature" not in l:
             kept.append(l)
     out = "\n".join(kept)
-    if res.returncode != 0 or spilled:
+    if failed or spilled:
         if os.path.exists(tmp):
             os.remove(tmp)
         if spilled:
@@ -160,8 +176,8 @@ def build_library(verbose: bool = False, stamps: bool = False) -> str:
     if verbose and out.strip():
         print(out)
     try:
-        for source in HAND_MANAGED:
-            check_wide_kernel(hipcc, verbose, source)
+        for check in checks:
+            check.result()
     except Exception:
         os.remove(tmp)
         raise
