@@ -11,8 +11,8 @@
 // the axis are keys, not tiles: blocks of one sequence then add up to a closed form, and nobody has to count them.
 // Tiles travel HBM/L2 -> LDS through a ring of four, asked for three tiles ahead.  Tiles run as a software pipeline over two of
 // them (see tile_pipelined): scores of the next tile, products of the current one and softmax weights alternate.
-// Bound by power where prompts are long: 16384 tokens, 32 query and 8 kv heads of 128, 2.03 to 2.11 ms, 1.04 to 1.08 PFLOP/s, at 1.5
-// GHz and 2750 cycles a tile, 2048 of them matrix work; heads of 64 2300, exponentials first.  Beyond its tiles a workgroup spends
+// Bound by power where prompts are long: 16384 tokens, 32 query and 8 kv heads of 128, 2.03 to 2.18 ms, 1.01 to 1.08 PFLOP/s, at 1.5
+// GHz and 2750 cycles a tile, 2048 of them matrix work; heads of 64 2230, exponentials first.  Beyond its tiles a workgroup spends
 // 8 us before the first one and 5 to 8 us a block (measured with a clock in a copy of this file: masked tile, first tile's maxima,
 // outputs, query rows).
 //
@@ -417,6 +417,26 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
         w_p1 = p_cur;
     };
 
+    // Slots e (even) and e + 1 in one piece, for tiles with two weights a matrix instruction (in pieces the compiler puts a wait state
+    // between some of them: 16384 tokens with heads of 64 1392 -> 1349 us)
+    auto weight_slots = [&](auto wkbc, auto ec) {
+        constexpr int wkb = decltype(wkbc)::value, e = decltype(ec)::value;
+        static_assert((e & 1) == 0, "a pair starts at an even slot");
+        constexpr int nb = e + 1 == 31 ? 1 - wkb : wkb, ne = (e + 2) & 31;      // the argument of weight e + 2
+        constexpr int pe = (e + 31) & 31, pb = e == 0 ? 1 - wkb : wkb, p2 = (e + 30) & 31, r = p2 / 16, i = p2 % 16;
+        float p0, p1, x1, x2;
+        uint32_t both;
+        asm volatile("v_exp_f32 %0, %7\n\tv_fma_f32 %2, %8, %12, -%13\n\tv_add_f32 %5, %5, %10\n\tv_cvt_pk_bf16_f32 %4, %11, %10\n\t"
+                     "v_exp_f32 %1, %2\n\tv_fma_f32 %3, %9, %12, -%14\n\tv_add_f32 %6, %6, %0"
+                     : "=&v"(p0), "=&v"(p1), "=&v"(x1), "=&v"(x2), "=&v"(both), "+v"(lsum[pe / 16][pe & 1]), "+v"(lsum[e / 16][e & 1])
+                     : "v"(w_x), "v"(s[wkb][(e + 1) / 16][(e + 1) % 16]), "v"(s[nb][ne / 16][ne % 16]), "v"(w_p1), "v"(w_p2), "v"(c2),
+                       "v"(mc[(e + 1) / 16]), "v"(mc[ne / 16]));
+        pk[pb][r][i >> 3][(i >> 1) & 3] = both;
+        w_x = x2;
+        w_p2 = p0;
+        w_p1 = p1;
+    };
+
     // S = K.Q^T of a tile
     auto scores = [&](const char *stage) {
         constexpr int kK = G::kKSteps;
@@ -537,7 +557,8 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
                 }
                 // weights of the other key block (of the next tile in half step 1), 32 scores over 4 kK slots
                 constexpr int lo = j * 32 / (4 * kK), hi = (j + 1) * 32 / (4 * kK);
-                static_for<hi - lo>([&](auto ic) { weight_slot(std::integral_constant<int, 1 - kb>{}, std::integral_constant<int, lo + decltype(ic)::value>{}, masked, sees); });
+                if constexpr (hi - lo == 2 && !decltype(masked)::value) weight_slots(std::integral_constant<int, 1 - kb>{}, std::integral_constant<int, lo>{});
+                else static_for<hi - lo>([&](auto ic) { weight_slot(std::integral_constant<int, 1 - kb>{}, std::integral_constant<int, lo + decltype(ic)::value>{}, masked, sees); });
                 __builtin_amdgcn_sched_barrier(0);
             });
         });
