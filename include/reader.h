@@ -542,7 +542,8 @@ int reader_measure_peaks(const void *src, size_t src_bytes, void *scratch, size_
  *                               wait for (n - 1) / 100 us at most (1: whoever finds another one missing leaves at once; never more
  *                               than 10 ms), the one that appends four times as long
  *   READER_TUNE_JOIN_SPREAD     1 = the shares of a pair run on different XCDs there (0 or cleared: on one)
- *   READER_TUNE_PROMPT_ROWS     16, 32, 64, 128 or 256 query rows a workgroup of reader_prompt_attn (other values: planner decides)
+ *   READER_TUNE_PROMPT_ROWS     one of the values of reader_prompt_rows: 16, 32, READER_PROMPT_ROWS_32_UNCUT, 64, 128 or 256 (other
+ *                               values: planner decides)
  * Returns READER_OK, or READER_EINVAL for an unknown `which`.
  */
 enum {
@@ -649,9 +650,11 @@ int reader_prompt_qkv(const reader_dims *dims, int32_t N, const void *qkv, const
  * row, no workspace).  dims->T and max_path have to be valid and are not used.
  */
 size_t reader_prompt_workspace_bytes(const reader_dims *dims, int32_t N, int32_t max_seq_len);
-/* Query rows of a kv head that a workgroup of reader_prompt_attn takes for these sizes: 16 or 32 (few rows; keys cut into
- * ranges), 64 or 128 (blocks of rows that are never cut), 256 (keys cut into ranges), by an estimate of their times; 0 for
- * dims->variant = 1; or the error that reader_prompt_attn would return for the sizes.  Pure host function; honours reader_tuning_override. */
+/* Query rows of a kv head that a workgroup of reader_prompt_attn takes for these sizes, by an estimate of the kernels' times: 16 or
+ * 32 (few rows; keys cut into ranges), READER_PROMPT_ROWS_32_UNCUT, 64 or 128 (blocks of rows that are never cut), 256 (keys cut into
+ * ranges); 0 for dims->variant = 1; or the error that reader_prompt_attn would return for the sizes.  Pure host function;
+ * honours reader_tuning_override. */
+enum { READER_PROMPT_ROWS_32_UNCUT = 33 };
 int reader_prompt_rows(const reader_dims *dims, int32_t N, int32_t max_seq_len);
 int reader_prompt_attn(const reader_dims *dims, int32_t N, const void *q, const void *k_cache, const void *v_cache,
                        const int32_t *page_table, const int32_t *cu_tokens, const int32_t *seq_lens,

@@ -30,6 +30,7 @@ STATUS_BAD_PATH = 4
 STATUS_BAD_LENGTH = 8
 TUNE_ATTN_ROWS, TUNE_ATTN_RANGES, TUNE_ATTN_PAIR_COST, TUNE_ATTN_AXIS64, TUNE_ATTN_WIDE, TUNE_ATTN_PAIR_FRONT, TUNE_ATTN_SHORT, TUNE_JOIN, TUNE_JOIN_SPREAD = 0, 1, 2, 3, 4, 5, 6, 7, 8
 TUNE_PROMPT_ROWS = 9
+PROMPT_ROWS_32_UNCUT = 33   # of reader_prompt_rows
 
 EXPORTS = (
     "reader_version", "reader_strerror", "reader_last_error_detail", "reader_validate_tree", "reader_workspace_bytes",

@@ -43,53 +43,53 @@ static bool cache_ok(const reader_dims *dims, const void *k_cache, const void *v
     return k_cache && v_cache && page_table && dims->num_pages >= 1 && dims->max_pages_per_seq >= 1 && aligned(k_cache, v_cache);
 }
 
-// Query rows a workgroup takes (reader_prompt_rows).
-//
-// Up to 16 rows that a sequence has for each kv head, on average (the host knows no more): the kernel that streams keys for few
-// rows.  Measured against the 256-row kernel: 16 single tokens on 1 to 16 K positions 97 against 122 us.
-//
-// Beyond that the shortest of five estimates, in us:
+// Query rows a workgroup takes (reader_prompt_rows): the shortest of six estimates, in us, of what the host knows (sequences of one
+// length, the longest one's last tokens):
 //   16, 32 rows: start and merge, and steps of 32 keys, which all blocks share out evenly (four wavefronts a compute unit); keys of
 //     a call that do not stay in the caches come from memory for every block;
-//   64, 128 rows, blocks never cut: the longest block's steps, one after the other (slower where every compute unit has one of
-//     full length), or what all blocks' steps take the compute units;
+//   32, 64, 128 rows, blocks never cut: the longest block's steps, one after the other (with 32 rows two at a time; slower where every
+//     compute unit has one of full length), or what all blocks' steps take the compute units;
 //   256 rows: start, merge and imbalance, and per block what its tiles of 64 keys and its ends take, shared out evenly.
-// The constants are fitted to 168 shapes (7 head layouts; 1 to 64 sequences of 12 to 3000 tokens, chunks on up to 30 K positions).
-// Some of them, 16, 32, 64, 128 and 256 rows (32 query and 8 kv heads, D 128): one prompt of 100 tokens 16.1, 19.6, 6.6, 8.2, 18.9; of
-// 1500 220, 148, 43.2, 49.5, 50.6; of 3000 698, 440, 141, 101, 99; 16 of 300 216, 152, 50.6, 43.6, 42.9; 64 tokens on 8 K positions
-// 58, 40, 187, 230, 75; 32 sequences of 12 on 8 K 471, 322, 216, 278, 170.  The estimates pick the fastest of the five on 145 of the
-// 168 and are 1.2 % behind it on average, 33 % at most (256 tokens on 1000 positions, 64 query heads: 45 against 34 us).
+// The constants are fitted to 252 shapes (7 head layouts; 1 to 64 sequences of 1 to 3000 tokens on up to 30 K positions).  Some of them,
+// 16, 32, 32 uncut, 64, 128 and 256 rows (32 query and 8 kv heads, D 128):
+// one prompt of 100 tokens 16.2, 19.5, 6.2, 6.6, 8.4, 19.0; of 1500 220, 149, 58.6, 45.9, 51.4, 51.1; of 3000 696, 441, 194, 144,
+// 100, 99.0; 16 of 300 214, 150, 75.9, 52.4, 43.7, 42.0; 256 tokens on 1000 positions 48.4, 37.5, 26.0, 35.4, 41.4, 31.4; 64 on 8
+// K 58.6, 40.9, 136, 200, 230, 74.6; 32 sequences of 12 on 8 K 474, 324, 213, 239, 283, 173; 16 single tokens on 500 16.2, 18.8,
+// 14.4, 16.8, 20.0, 25.4; on 2000 30.7, 32.5, 41.9, 52.4, 62.1, 39.9.  The estimates pick the fastest of the six on 226 of the 252
+// and are 0.7 % behind it on average, 29 % at most.
 static int prompt_rows(const reader_dims &d, int32_t N, int32_t max_seq_len) {
     if (d.variant == 1) return 0;
     const int forced = tuning(READER_TUNE_PROMPT_ROWS), G = d.Hq / d.Hkv;
-    if (forced == 16 || forced == 32 || forced == 64 || forced == 128 || forced == 256) return forced;
-    if (d.B == 0 || (long long)N * G <= 16LL * d.B) return 16;
+    if (forced == 16 || forced == 32 || forced == kUncut32 || forced == 64 || forced == 128 || forced == 256) return forced;
+    if (d.B == 0 || N == 0) return 16;
     const double tokens = (double)N / d.B;                        // of a sequence
     const double longest = max_seq_len > tokens ? max_seq_len : tokens, average = longest - 0.5 * tokens;   // keys of a block
     const bool large = d.D == 128;
     auto blocks = [&](int rows) { return (double)d.Hkv * d.B * ceil(tokens / (rows / G)); };
     auto few = [&](int rows, double start, double step) {
         const bool far = (double)d.Hkv * d.B * longest * d.D * 4 > 64e6;
-        const double from_memory = large ? 0.62 : 0.33;
+        const double from_memory = large ? 0.59 : 0.29;
         return start + (far && step < from_memory ? from_memory : step) * blocks(rows) * (average / 32 + 14) / kNumCU;
     };
     auto uncut = [&](int rows, double step, double step_busy, double all_steps) {
         const bool busy = blocks(rows) * average >= 0.8 * kNumCU * longest;
-        const double chain = (busy ? step_busy : step) * (longest / 32 + 0.5), all = all_steps * blocks(rows) * (average / 32 + 4) / kNumCU;
+        const double chain = (busy ? step_busy : step) * (longest / (rows == 32 ? 64 : 32) + 0.5);
+        const double all = all_steps * blocks(rows) * (average / 32 + (rows == 32 ? 6 : 4)) / kNumCU;
         return 5.5 + (chain > all ? chain : all);
     };
     const double parts = blocks(256) < kNumCU / 4 ? (large ? 20.0 : 12.0) : 0.0;     // (every range leaves records, nothing else)
-    double best = (large ? 26.0 : 24.0) + parts + blocks(256) / kNumCU * (large ? 7.0 + 1.6 * (average / 64 + 0.5) : 4.0 + 0.95 * (average / 64 + 0.5));
+    double best = (large ? 26.0 : 25.0) + parts + blocks(256) / kNumCU * (large ? 7.0 + 1.6 * (average / 64 + 0.5) : 4.0 + 0.763 * (average / 64 + 0.5));
     int rows = 256;
     auto offer = [&](int r, double us) {
         if (us < best) { best = us; rows = r; }
     };
-    offer(16, large ? few(16, 13.7, 0.335) : few(16, 14.0, 0.156));
-    offer(32, large ? few(32, 16.3, 0.515) : few(32, 15.7, 0.22));
+    offer(16, large ? few(16, 13.7, 0.303) : few(16, 13.6, 0.156));
+    offer(32, large ? few(32, 16.3, 0.457) : few(32, 15.3, 0.22));
     // (block numbers of the uncut kernels are counted with the threads of a launch)
-    if (((long long)N / (64 / G) + d.B) * d.Hkv < (1 << 23)) {
+    if (((long long)N / (32 / G) + d.B) * d.Hkv < (1 << 23)) {
+        offer(kUncut32, large ? uncut(32, 0.98, 1.09, 0.33) : uncut(32, 0.70, 0.91, 0.22));
         offer(128, large ? uncut(128, 0.93, 1.2, 0.57) : uncut(128, 0.64, 0.8, 0.43));
-        offer(64, large ? uncut(64, 0.75, 0.75, 0.45) : uncut(64, 0.50, 0.50, 0.29));
+        offer(64, large ? uncut(64, 0.85, 0.83, 0.45) : uncut(64, 0.56, 0.64, 0.29));
     }
     return rows;
 }
@@ -98,7 +98,7 @@ static hipError_t launch_prompt(const PromptParams &p, int rows, hipStream_t str
     switch (rows) {
         case 0: return launch_prompt_attn_scalar(p, stream);
         case 16: case 32: return launch_prompt_few(p, rows, stream);
-        case 64: case 128: return launch_prompt_mid(p, rows, stream);
+        case kUncut32: case 64: case 128: return launch_prompt_mid(p, rows, stream);
         default: return launch_prompt_wide(p, stream);
     }
 }

@@ -1,11 +1,14 @@
-// Causal attention of packed prompts over the paged cache, blocks of 64 or 128 query rows that are never cut: short prompts, batches
-// of them.  One launch and no records: where the blocks of a call are about as many as the chip runs at a time, cutting them evenly
+// Causal attention of packed prompts over the paged cache, blocks of 32, 64 or 128 query rows that are never cut: short prompts,
+// batches of them.  One launch and no records: where the blocks of a call are about as many as the chip runs at a time, cutting them evenly
 // costs more than it gains (what is written and read again for a row is as much as 2 tiles of keys, and a second launch).
 //
 // A workgroup is 4 wavefronts of 32 rows (prompt_rows.h) that share the keys, 32 at a time, in a ring of four stages in LDS; two
 // workgroups run on a compute unit and fill each other's waits.  Each wavefront copies one of the four pages of a step.
-// (64 rows: of 16 each.)  Bound by the longest block's steps: one prompt of 800 tokens, 32 query and 8 kv heads of 128, 22 to 23 us,
-// 25 steps of 0.75 us; by all blocks' steps in batches: 16 prompts of 300 43 us.
+// (64 rows: of 16 each; 32: two of them take the even steps and two the odd ones, half as many one after the other.)  Bound by the
+// longest block's steps, 0.75 us each with 64 rows and 1 for two with 32: one prompt of 400 tokens, 32 query and 8 kv heads of 128, 14.7
+// us with 64 rows, 12 with 32, 256 tokens on 1000 positions 35 and 25; by all blocks' steps in batches: 16 prompts of 300 43 us with
+// 128 rows.  (64 rows, of 32 each, the steps shared out like that: 1500 tokens 41.5 instead of 47, one shape in fourteen that the
+// other three do not do better.)
 #include "prompt_rows.h"
 
 namespace reader {
@@ -14,8 +17,9 @@ namespace {
 
 constexpr int kMidThreads = 256, kMidStages = 4;
 
-// kBlocks: blocks of 16 query rows that a wavefront carries
-template <int D, int kBlocks>
+// kBlocks: blocks of 16 query rows that a wavefront carries.  kSplit: 1, every wavefront has rows of its own and takes all steps, or
+// 2, wavefronts 2 and 3 have the rows of 0 and 1 and take the other half of the steps.
+template <int D, int kBlocks, int kSplit>
 __global__ __launch_bounds__(kMidThreads, 2) void prompt_mid_kernel(PromptParams p) {
     using Rows = PromptRows<D, kBlocks>;
     using Page = PageLayout<D>;
@@ -71,30 +75,64 @@ __global__ __launch_bounds__(kMidThreads, 2) void prompt_mid_kernel(PromptParams
     };
     ids.load(0, lane);
     Rows rows;
-    const int first = wave * 16 * kBlocks;
+    constexpr int kGroups = 4 / kSplit;
+    const int first = wave % kGroups * 16 * kBlocks, turn = wave / kGroups;
     rows.load(p, head, row0, p0, nt, first, i16, quad);
     const int first_tok = (int)(((float)first + 0.5f) * p.g_rcp);
     const bool active = first_tok < nt;
     wait_vmcnt<0>();                                     // the first page ids are there
     asm volatile("" ::: "memory");
     ids.begin(lane);
-    for (int i = 0; i < min(kMidStages - 1, steps); ++i) issue(i, 0);
+    constexpr int kAhead = kSplit == 1 ? kMidStages - 1 : 2;             // steps asked for in front of the first
+    for (int i = 0; i < min(kAhead, steps); ++i) issue(i, 0);
     const int all_see = (int)min(p0 + first_tok + 1, (long long)p.max_seq_len);   // keys that every row of this wavefront sees
-    for (int i = 0; i < steps; ++i) {
-        ids.advance<1>(i, steps, lane);
-        // this wavefront's page of step i has landed once at most those of the next two steps are on their way
-        if (i + 2 < steps) wait_vmcnt<2 * Page::kCopies>();
+    for (int i0 = 0; i0 < steps; i0 += kSplit) {
+        ids.advance<kSplit>(i0, steps, lane);
+        // this wavefront's pages of the steps have landed once at most those of the next two steps are on their way
+        if (kSplit == 1 && i0 + 2 < steps) wait_vmcnt<2 * Page::kCopies>();
         else wait_vmcnt<0>();
-        __syncthreads();                                 // ... and everybody's; nobody reads step i - 1 any more
-        if (i + kMidStages - 1 < steps) issue(i + kMidStages - 1, i);
-        const int j0 = i * kStep;
-        const bool hole0 = j0 < keys && ids.get(i * kStepPages, i, keys, p.num_pages) < 0;
-        const bool hole1 = j0 + READER_PAGE_SIZE < keys && ids.get(i * kStepPages + 1, i, keys, p.num_pages) < 0;
+        __syncthreads();                                 // ... and everybody's; nobody reads the steps in front any more
+#pragma unroll
+        for (int c = 0; c < kSplit; ++c)
+            if (i0 + kAhead + c < steps) issue(i0 + kAhead + c, i0);
+        const int i = i0 + turn, j0 = i * kStep;
+        if (kSplit > 1 && i >= steps) break;
+        const bool hole0 = j0 < keys && ids.get(i * kStepPages, i0, keys, p.num_pages) < 0;
+        const bool hole1 = j0 + READER_PAGE_SIZE < keys && ids.get(i * kStepPages + 1, i0, keys, p.num_pages) < 0;
         if (hole0 || hole1) bad |= READER_STATUS_BAD_PAGE;
         const char *stage = s_stage[i & (kMidStages - 1)];
         rows.scores(stage, i16, quad);
-        rows.weights(j0, i == 0, j0 + kStep > all_see || hole0 || hole1, hole0, hole1, p.scale_log2, quad);
+        rows.weights(j0, i == turn, j0 + kStep > all_see || hole0 || hole1, hole0, hole1, p.scale_log2, quad);
         rows.template products<false>(stage + kStepPages * Page::kPageBytes, i16, quad, [] {});
+    }
+    if constexpr (kSplit > 1) {
+        // the second half's rows come to the first through the stages, lane by lane
+        f32x4 *theirs = reinterpret_cast<f32x4 *>(&s_stage[0][0]) + (size_t)(wave % kGroups) * (kBlocks * Rows::kOut + 1) * 64 + lane;
+        static_assert(kGroups * (kBlocks * Rows::kOut + 1) * 64 * 16 <= kMidStages * kStageBytes && kBlocks <= 2, "they fit");
+        __syncthreads();                                 // everybody is done with the keys
+        if (turn > 0) {
+#pragma unroll
+            for (int r = 0; r < kBlocks; ++r)
+#pragma unroll
+                for (int db = 0; db < Rows::kOut; ++db) theirs[(r * Rows::kOut + db) * 64] = rows.acc[r][db];
+            theirs[kBlocks * Rows::kOut * 64] = f32x4{rows.m[0], rows.l[0], rows.m[kBlocks - 1], rows.l[kBlocks - 1]};
+        }
+        __syncthreads();
+        if (turn > 0) {
+            if (p.status && bad) atomicOr(p.status, bad);
+            return;
+        }
+        const f32x4 sums = theirs[kBlocks * Rows::kOut * 64];
+#pragma unroll
+        for (int r = 0; r < kBlocks; ++r) {
+            // (a half that has seen nothing has a reference below all others and a sum of zero)
+            const float m2 = sums[2 * r], l2 = sums[2 * r + 1], top = fmaxf(rows.m[r], m2);
+            const float f1 = __builtin_amdgcn_exp2f(rows.m[r] - top), f2 = __builtin_amdgcn_exp2f(m2 - top);
+            rows.l[r] = rows.l[r] * f1 + l2 * f2;
+            rows.m[r] = top;
+#pragma unroll
+            for (int db = 0; db < Rows::kOut; ++db) rows.acc[r][db] = rows.acc[r][db] * f1 + theirs[(r * Rows::kOut + db) * 64] * f2;
+        }
     }
     if (active) {
         rows.finish_sums();
@@ -105,19 +143,20 @@ __global__ __launch_bounds__(kMidThreads, 2) void prompt_mid_kernel(PromptParams
 }
 
 
-template <int D, int kBlocks>
+template <int D, int kBlocks, int kSplit>
 hipError_t launch_mid(PromptParams p, hipStream_t stream) {
-    p.tokens_per_block = 64 * kBlocks / p.G;
+    p.tokens_per_block = 64 * kBlocks / kSplit / p.G;
     p.n_ranges = p.N / p.tokens_per_block + p.B;         // (block numbers of a kv head)
-    hipLaunchKernelGGL((prompt_mid_kernel<D, kBlocks>), dim3((unsigned)p.n_ranges * p.Hkv), dim3(kMidThreads), 0, stream, p);
+    hipLaunchKernelGGL((prompt_mid_kernel<D, kBlocks, kSplit>), dim3((unsigned)p.n_ranges * p.Hkv), dim3(kMidThreads), 0, stream, p);
     return note_hip_error("launch prompt_mid_kernel", hipGetLastError());
 }
 
 }  // namespace
 
 hipError_t launch_prompt_mid(const PromptParams &p, int rows, hipStream_t stream) {
-    if (rows == 64) return p.D == 64 ? launch_mid<64, 1>(p, stream) : launch_mid<128, 1>(p, stream);
-    return p.D == 64 ? launch_mid<64, 2>(p, stream) : launch_mid<128, 2>(p, stream);
+    if (rows == kUncut32) return p.D == 64 ? launch_mid<64, 1, 2>(p, stream) : launch_mid<128, 1, 2>(p, stream);
+    if (rows == 64) return p.D == 64 ? launch_mid<64, 1, 1>(p, stream) : launch_mid<128, 1, 1>(p, stream);
+    return p.D == 64 ? launch_mid<64, 2, 1>(p, stream) : launch_mid<128, 2, 1>(p, stream);
 }
 
 }  // namespace reader

@@ -51,10 +51,11 @@ struct PromptParams {
     int32_t tokens_per_block;      // (matrix kernels) tokens whose heads fill a block of query rows
     int32_t n_ranges;              // ... and workgroups of the launch
 };
-// 256 rows a workgroup (prompt_attn.hip), 64 or 128 and blocks that are never cut (prompt_attn_mid.hip), 16 or 32
+// 256 rows a workgroup (prompt_attn.hip), 32, 64 or 128 and blocks that are never cut (prompt_attn_mid.hip), 16 or 32
 // (prompt_attn_few.hip); what the first and the last leave of cut blocks is folded by a second launch (prompt_merge.hip)
 size_t prompt_wide_workspace_bytes(int D);
 hipError_t launch_prompt_wide(const PromptParams &p, hipStream_t stream);
+constexpr int kUncut32 = READER_PROMPT_ROWS_32_UNCUT;
 hipError_t launch_prompt_mid(const PromptParams &p, int rows, hipStream_t stream);
 size_t prompt_few_workspace_bytes(int D);
 hipError_t launch_prompt_few(const PromptParams &p, int rows, hipStream_t stream);

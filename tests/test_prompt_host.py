@@ -180,12 +180,13 @@ def test_rows_of_a_prompt(R):
         return R.reader_prompt_rows(dims(R, B=B, Hq=32, Hkv=8, max_pages_per_seq=4096, **kw), N, bound)
     assert rows(16, 16, 16384) == 16                     # single tokens
     assert rows(8, 64, 9000) == 32                       # chunks of eight
-    assert rows(1, 100, 100) == 64 and rows(1, 800, 800) == 64
+    assert rows(1, 100, 100) == R.PROMPT_ROWS_32_UNCUT and rows(1, 400, 400) == R.PROMPT_ROWS_32_UNCUT and rows(16, 16, 300) == R.PROMPT_ROWS_32_UNCUT
+    assert rows(1, 1500, 1500) == 64
     assert rows(16, 16 * 300, 300) == 128
     assert rows(1, 16384, 16384) == 256 and rows(1, 256, 8000) == 256
     assert rows(1, 0, 0) == 16 and rows(0, 0, 0) == 16
     assert rows(1, 16384, 16384, variant=1) == 0
-    for forced in (16, 32, 64, 128, 256):
+    for forced in (16, 32, 33, 64, 128, 256):
         R.reader_tuning_override(R.TUNE_PROMPT_ROWS, forced)
         try:
             assert rows(1, 100, 100) == forced
