@@ -197,6 +197,35 @@ def test_many_sequences(R, rows, Hq, Hkv, D):
     p.check(*p.run(R, rows))
 
 
+def test_the_largest_batch(R, rows):
+    """More sequences than any table in LDS holds."""
+    gen = torch.Generator().manual_seed(16)
+    B = 4096
+    new, L = torch.randint(0, 4, (B,), generator=gen).tolist(), torch.randint(0, 40, (B,), generator=gen).tolist()
+    p = Problem(new, L, 4, 2, 64, seed=17)
+    out, lse = p.run(R, rows)
+    for b in list(range(0, 60)) + list(range(60, B - 40, 97)) + list(range(B - 40, B)):
+        if new[b]:
+            lo, hi = int(p.cu[b]), int(p.cu[b + 1])
+            S = L[b] + new[b]
+            want, want_lse, bound, bound_lse = P.attention(p.q[lo:hi], p.cache.rows(p.cache.k, b, S), p.cache.rows(p.cache.v, b, S), L[b])
+            P.check(out[lo:hi], want, bound, "out of sequence %d" % b)
+            P.check(lse[lo:hi], want_lse, bound_lse, "lse of sequence %d" % b)
+
+
+def test_more_blocks_of_a_sequence_in_a_range_than_lanes(R, rows):
+    if rows == 0:
+        pytest.skip("the plain kernel has no ranges, and is too slow")
+    n = 40000
+    p = Problem([n], [5], 16, 1, 64, seed=18)
+    out, lse = p.run(R, rows)
+    k, v = p.cache.rows(p.cache.k, 0, n + 5), p.cache.rows(p.cache.v, 0, n + 5)
+    for t in [0, 1, 63, 64, 1000, 7777, 20001, n - 65, n - 2, n - 1]:
+        want, want_lse, bound, bound_lse = P.attention(p.q[t:t + 1], k[:, :t + 6], v[:, :t + 6], t + 5)
+        P.check(out[t:t + 1], want, bound, "out of token %d" % t)
+        P.check(lse[t:t + 1], want_lse, bound_lse, "lse of token %d" % t)
+
+
 def test_no_positions_at_all(R, rows):
     p = Problem([5, 3], [0, 0], 4, 2, 64, seed=14)
     out, lse = p.run(R, rows, bound=0, status_want=R.STATUS_BAD_LENGTH)
