@@ -39,6 +39,7 @@ constexpr int kPromptSeqsInLds = 2048;               // batches up to this size 
 constexpr int kBlockFront = 4 * kTile, kBlockCost = 8 * kTile;
 constexpr int kMinRange = 4 * kTile;                 // no range is shorter than this: a range costs as much before its first tile
 using Block = PromptBlock<kTile, kBlockFront, kBlockCost>;
+constexpr int kMaxDevices = 64;                      // whose LDS limit is remembered
 
 // One tile of a workgroup's list.
 struct PromptTile {
@@ -849,13 +850,15 @@ static hipError_t launch_prompt(const PromptParams &p, hipStream_t stream) {
                        (p.B <= kPromptSeqsInLds ? (2 * (size_t)p.B + 1) * sizeof(int) : 0);
     {
         static std::mutex guard;             // host threads may call in at the same time
-        static size_t lds_allowed = 0;
+        static size_t lds_allowed[kMaxDevices] = {};
+        int device = 0;
+        hipError_t e = hipGetDevice(&device);
         std::lock_guard<std::mutex> lock(guard);
-        if (lds > lds_allowed) {
-            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&prompt_attn_kernel<D>),
-                                                     hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        size_t *const allowed = e == hipSuccess && device < kMaxDevices ? &lds_allowed[device] : nullptr;
+        if (!allowed || lds > *allowed) {
+            e = hipFuncSetAttribute(reinterpret_cast<const void *>(&prompt_attn_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
             if (e != hipSuccess) { (void)hipGetLastError(); return note_hip_error("hipFuncSetAttribute(prompt attention LDS size)", e); }
-            lds_allowed = lds;
+            if (allowed) *allowed = lds;
         }
     }
     hipLaunchKernelGGL((prompt_attn_kernel<D>), dim3(p.n_ranges), dim3(kPromptThreads), lds, stream, p, p.page_table);
