@@ -624,35 +624,61 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
             const int row = wave_s * 64 + r * 32 + n, tok = token_of(rc);
             const bool real = tok < seg_nt;
             const float l_mine = lsum[r][0] + lsum[r][1];
-            const float l = l_mine + __shfl_xor(l_mine, 32);
-            const float inv = l == 0.f ? 0.f : 1.f / l;                 // (a row may see no key of a part)
+            const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_mine), __float_as_uint(l_mine), false, false);
+            const float l = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+            const float inv = l == 0.f ? 0.f : __builtin_amdgcn_rcpf(l);    // (a row may see no key of a part; off by 2^-23 at most)
             const float ref = __uint_as_float(acc_read_u32<Acc::m_ref(r)>()) * c2;
             float check[4] = {l < kTooLarge ? 0.f : __builtin_nanf(""), 0.f, 0.f, 0.f};
-            uint16_t *orow = p.out + (((size_t)seg_row0 + tok) * p.Hq + (size_t)seg_head * p.G + group_of(rc)) * D;
-            // A lane holds, per 8-wide chunk of the output row, 4 values and its partner lane (lane ^ 32) the other 4.
-            static_for<G::kOBlocks * 2>([&](auto cc) {
-                constexpr int db = decltype(cc)::value / 2, i4 = (decltype(cc)::value % 2) * 2;
-                float v[8];
+            // values 4 i4 + 4 h .. + 3 and + 8 of them of block db: a lane holds, of two 8-wide chunks of the output row side by side,
+            // 4 values of each, its partner lane (lane ^ 32) the others
+            auto values = [&](auto dbc, auto i4c, float (&v)[8]) {
                 static_for<8>([&](auto ec) {
                     constexpr int e = decltype(ec)::value;
-                    v[e] = acc_read<Acc::o(r, db) + 4 * i4 + e>() * inv;
+                    v[e] = acc_read<Acc::o(r, decltype(dbc)::value) + 4 * decltype(i4c)::value + e>() * inv;
                     check[e % 4] = __builtin_fmaf(v[e], 0.f, check[e % 4]);   // (not a number once any value is none)
                 });
-                if (whole) {
-                    const uint32_t a0 = pack_bf16x2(v[0], v[1]), a1 = pack_bf16x2(v[2], v[3]);
-                    const uint32_t b0 = pack_bf16x2(v[4], v[5]), b1 = pack_bf16x2(v[6], v[7]);
-                    const auto s0 = __builtin_amdgcn_permlane32_swap(a0, b0, false, false);
-                    const auto s1 = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
-                    u32x4 w;
-                    w.x = s0[0]; w.y = s1[0]; w.z = s0[1]; w.w = s1[1];
-                    if (real) *reinterpret_cast<u32x4 *>(orow + db * 32 + (i4 + h) * 8) = w;
-                } else {
-                    // [D / 4 chunks][rows][4 values], then the rows' references, then their sums
+            };
+            if (whole) {
+                // Four chunks of rows 0..15 and of 16..31 of the block change places, so that a store writes 64 bytes of a row in one go
+                // (packed prompts with heads of 64 212 -> 207 us, more than to have the next query rows on their way meanwhile).
+                auto place = [&](int at, bool &is) {
+                    const int t = (int)(((float)at + 0.5f) * p.g_rcp);
+                    is = at < tb * p.G && t < seg_nt;
+                    return p.out + (((size_t)seg_row0 + t) * p.Hq + (size_t)seg_head * p.G + (at - t * p.G)) * D + (((lane >> 4) & 1) * 2 + h) * 8;
+                };
+                bool real_lo, real_hi;
+                uint16_t *const to_lo = place(wave_s * 64 + r * 32 + (lane & 15), real_lo), *const to_hi = place(wave_s * 64 + r * 32 + 16 + (lane & 15), real_hi);
+                static_for<G::kOBlocks>([&](auto dbc) {
+                    constexpr int db = decltype(dbc)::value;
+                    uint32_t w[2][4];
+                    static_for<2>([&](auto ic) {
+                        constexpr int i = decltype(ic)::value;
+                        float v[8];
+                        values(dbc, std::integral_constant<int, 2 * i>{}, v);
+                        const auto s0 = __builtin_amdgcn_permlane32_swap(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[4], v[5]), false, false);
+                        const auto s1 = __builtin_amdgcn_permlane32_swap(pack_bf16x2(v[2], v[3]), pack_bf16x2(v[6], v[7]), false, false);
+                        w[i][0] = s0[0]; w[i][1] = s1[0]; w[i][2] = s0[1]; w[i][3] = s1[1];
+                    });
+                    u32x4 lo, hi;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const auto sw = __builtin_amdgcn_permlane16_swap(w[0][j], w[1][j], false, false);
+                        lo[j] = sw[0]; hi[j] = sw[1];
+                    }
+                    if (real_lo) *reinterpret_cast<u32x4 *>(to_lo + db * 32) = lo;
+                    if (real_hi) *reinterpret_cast<u32x4 *>(to_hi + db * 32) = hi;
+                });
+            } else {
+                // [D / 4 chunks][rows][4 values], then the rows' references, then their sums
+                static_for<G::kOBlocks * 2>([&](auto cc) {
+                    constexpr int db = decltype(cc)::value / 2, i4 = (decltype(cc)::value % 2) * 2;
+                    float v[8];
+                    values(std::integral_constant<int, db>{}, std::integral_constant<int, i4>{}, v);
                     float4 *to = reinterpret_cast<float4 *>(rec) + (size_t)(db * 8 + 2 * i4 + h) * kPromptRows + row;
                     to[0] = make_float4(v[0], v[1], v[2], v[3]);
                     to[2 * kPromptRows] = make_float4(v[4], v[5], v[6], v[7]);
-                }
-            });
+                });
+            }
             if (h == 0) {
                 if (!whole) {
                     float *ml = rec + (size_t)kPromptRows * D;
@@ -825,16 +851,14 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
             products(stage_of(it));
         }
         if (I.t_flags & kTileEnds) {
-            // the next segment's query rows are on their way while this one's outputs are written
             const PromptTile *d = desc_of(it), *d2 = desc_of(it + 1);
             const int head = word(d2->head), row0 = word(d2->row0), p0 = word(d2->p0), nt = word(d2->nt), t0 = word(d2->t);
-            QueryRows q;
-            if (D == 64 && !I.last_iter) fetch_q(q, head, row0, nt);
             if (wave_active) finish_segment(I.t_flags, word(d->t) + 1, word(d->b));
             if (!I.last_iter) {
                 seg_head = head; seg_row0 = row0; seg_p0 = p0; seg_nt = nt; seg_t0 = t0;
                 wave_active = wave_token < seg_nt;
-                if (D == 128) fetch_q(q, head, row0, nt);
+                QueryRows q;
+                fetch_q(q, head, row0, nt);
                 reset_state();
                 put_q(q);
             }
