@@ -13,7 +13,7 @@
 // them (see tile_pipelined): scores of the next tile, products of the current one and softmax weights alternate.
 // Bound by power where prompts are long: 16384 tokens, 32 query and 8 kv heads of 128, 2.03 to 2.18 ms, 1.01 to 1.08 PFLOP/s, at 1.5
 // GHz and 2750 cycles a tile, 2048 of them matrix work; heads of 64 2230, exponentials first.  Beyond its tiles a workgroup spends
-// 8 us before the first one and 5 to 8 us a block (measured with a clock in a copy of this file: masked tile, first tile's maxima,
+// 7 to 10 us before the first one and 5 to 8 us a block (measured with a clock in a copy of this file: masked tile, first tile's maxima,
 // outputs, query rows).
 //
 // A row's softmax reference is its maximum in the first tile of its range and is never moved: a lower reference makes all weights
