@@ -165,18 +165,18 @@ __global__ __launch_bounds__(64 * kWaves) void prompt_few_kernel(PromptParams p)
             for (int r = 0; r < kBlocks; ++r) {
                 const int row = r * 16 + i16;
                 const size_t at = Rows::out_row(p, o.head, row0, nt, 0, r, i16);
-                float top = kNoReference, sum = 0.f, f[kWaves];
+                float top = kNoReference, sum = 0.f, f[kWaves], check = 0.f;   // (check: not a number once any value is none)
 #pragma unroll
                 for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_sum[w][0][row]);
 #pragma unroll
                 for (int w = 0; w < kWaves; ++w) {
                     // (a wavefront whose rows saw nothing has no say, whatever its reference; a sum that is not a number shows)
                     const float lw = s_sum[w][1][row];
+                    check = lw < kTooLarge ? check : __builtin_nanf("");
                     f[w] = lw == 0.f ? 0.f : __builtin_amdgcn_exp2f(s_sum[w][0][row] - top);
                     sum += lw * f[w];
                 }
                 const float inv = sum == 0.f ? 0.f : 1.f / sum;
-                float check = sum * 0.f;
                 // a wavefront takes D / 4 / kWaves chunks of the columns, a lane those of its quarter of them
                 constexpr int kMine = D / 16 / kWaves;
                 f32x4 v[kMine];

@@ -128,7 +128,7 @@ __global__ __launch_bounds__(kMidThreads, 2) void prompt_mid_kernel(PromptParams
             // (a half that has seen nothing has a reference below all others and a sum of zero)
             const float m2 = sums[2 * r], l2 = sums[2 * r + 1], top = fmaxf(rows.m[r], m2);
             const float f1 = __builtin_amdgcn_exp2f(rows.m[r] - top), f2 = __builtin_amdgcn_exp2f(m2 - top);
-            rows.l[r] = rows.l[r] * f1 + l2 * f2;
+            rows.l[r] = fmaxf(rows.l[r], l2) < kTooLarge ? rows.l[r] * f1 + l2 * f2 : __builtin_nanf("");   // (NaN: computed again)
             rows.m[r] = top;
 #pragma unroll
             for (int db = 0; db < Rows::kOut; ++db) rows.acc[r][db] = rows.acc[r][db] * f1 + theirs[(r * Rows::kOut + db) * 64] * f2;

@@ -12,6 +12,7 @@ namespace {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr int kStep = 32, kStepPages = kStep / READER_PAGE_SIZE;
 constexpr float kNoReference = -1e30f;               // of a row that has seen no key
+constexpr float kTooLarge = 0x1p100f;                // of a sum that is not folded with others any more
 
 // How a page of 16 K or V rows is copied to LDS and read back as an operand: whole, 1 KB a copy instruction; the 16-byte chunks of
 // a row are swizzled by the row, so that the reads of an operand touch every bank once (K: 16 rows, one chunk; V: 8 rows, two
@@ -80,8 +81,9 @@ struct PageIds {
 // kBlocks blocks of 16 rows.  S^T = K.Q^T in blocks of 16 keys x 16 rows leaves lane (quad, i16) with four scores of row i16 of a
 // block for each page, keys 4 quad .. + 3: as they stand, the operand of O^T += V^T.P^T, if key 8 quad' + j of that product is key
 // 4 quad + j % 4 of page j / 4 in both operands.  A row's reference is its maximum over the first 32 keys and is never moved: a lower
-// one makes all weights of the row larger by one factor, which fp32 sums and bf16 weights hold up to 2^127 (a row that they do not
-// hold comes out as not a number and is computed again).  With a maximum that moves, were it only once in a thousand steps, the
+// one makes all weights of the row larger by one factor, which fp32 sums and bf16 weights hold.  A row whose sum reaches kTooLarge is
+// computed again: up to there hundreds of its parts add up without an overflow, and a part is below 2^-24 of the row where its factor,
+// 2 to the difference of two references, becomes zero.  With a maximum that moves, were it only once in a thousand steps, the
 // compiler copies all accumulators three times a step where the paths meet.
 template <int D, int kBlocks>
 struct PromptRows {
@@ -205,7 +207,7 @@ struct PromptRows {
 #pragma unroll
         for (int r = 0; r < kBlocks; ++r) {
             const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
-            float check = l[r] * 0.f;                        // (not a number once any value is none)
+            float check = l[r] < kTooLarge ? 0.f : __builtin_nanf("");   // (not a number once any value is none)
             const size_t at = out_row(p, head, row0, nt, first, r, i16);
 #pragma unroll
             for (int db = 0; db < kOut; ++db) {
