@@ -565,10 +565,11 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
         });
     };
 
-    // The reference of row block r: the maximum of the scores in the registers.  (A row that sees no key of the segment's first tile
-    // sees none of a later one either, by its place; behind pages that do not exist it may: its weights then are too large for the
-    // reference, and it is computed again.)
-    auto set_reference = [&](auto rc, bool holes) {
+    // The reference of row block r: the maximum of the scores in the registers, or kNoReference.  (A row that sees no key of the
+    // segment's first tile sees none of a later one either, by its place; behind pages that do not exist, or keys that score minus
+    // infinity, it may: its weights then are too large for the reference, and it is computed again.)
+    constexpr float kNoReference = -1e30f;
+    auto set_reference = [&](auto rc) {
         constexpr int r = decltype(rc)::value;
         float mx = fmaxf(s[0][r][0], s[1][r][0]);
 #pragma unroll
@@ -576,9 +577,9 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
         // the other half of the row's keys sits in lane ^ 32
         const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
         mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
-        const float ref = holes ? fmaxf(mx, -1e30f) : mx;
+        const float ref = fmaxf(mx, kNoReference);
         acc_write<Acc::m_ref(r)>(__float_as_uint(ref));
-        mc[r] = ref == -INFINITY ? 0.f : ref * c2;
+        mc[r] = ref * c2;
     };
 
     // A tile with keys behind page ids that do not exist, one step after the other.
@@ -594,7 +595,7 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
             for (int r = 0; r < 2; ++r)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[kb][r][i] = (holes >> (kb * 2 + (i >> 3))) & 1 ? -INFINITY : s[kb][r][i];
-        if (flags & kTileFresh) static_for<2>([&](auto rc) { set_reference(rc, true); });
+        if (flags & kTileFresh) static_for<2>([&](auto rc) { set_reference(rc); });
         weights_of_key_block(0);
         weights_of_key_block(1);
         products(stage);
@@ -807,7 +808,7 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
                 mask(0, o);
                 mask(1, o);
             }
-            if (I.t_flags & kTileFresh) static_for<2>([&](auto rc) { set_reference(rc, false); });
+            if (I.t_flags & kTileFresh) static_for<2>([&](auto rc) { set_reference(rc); });
             begin_run();
             while (I.pipelined || I.closing) {
                 if (I.copy_inside) {

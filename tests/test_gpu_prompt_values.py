@@ -1,5 +1,5 @@
 """reader_prompt_attn where a row's softmax reference, its maximum over the first keys that a wavefront sees, says little about its
-later keys: scores up to 2^127 times as heavy."""
+later keys: scores up to 2^127 times as heavy, scores of minus infinity by their own value."""
 import math
 
 import pytest
@@ -57,3 +57,30 @@ def test_heavy_keys_in_every_range(R, rows, D, height, n, L, period, at, each):
     want, want_lse, bound, bound_lse = P.attention(q, cache.rows(cache.k, 0, L + n), cache.rows(cache.v, 0, L + n), L)
     P.check(out, want, bound, "out")
     P.check(lse, want_lse, bound_lse, "lse")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("value", [-math.inf, -3e38])
+@pytest.mark.parametrize("n,L", [(1, 9000), (5, 3000), (150, 2300), (700, 0)])
+@pytest.mark.parametrize("period,part", [(3, 1), (12, 9)])
+def test_scores_of_minus_infinity(R, rows, D, value, n, L, period, part):
+    """Of every `period` tiles of 64 keys the first `part` score minus infinity (by an infinite key, or by a sum that overflows): they
+    weigh nothing, also where they are all that the first tile of a range holds."""
+    gen = torch.Generator().manual_seed(n)
+    cache = P.Cache(gen, [L + n], 1, D)
+    cache.fill(gen, 0, L + n)
+    q = (torch.randn((n, 2, D), generator=gen).abs() + 0.1).bfloat16()
+    none = (torch.arange(L + n) // 64) % period < part
+    if L:
+        none[L - 5:] = False                                      # (the rows' own keys, and a few in front, are as ever)
+    page, slot = cache.place(0, L + n)
+    cache.k[page[none], 0, slot[none]] = value
+    out, lse = run(R, rows, cache, q, L)
+    k, v = cache.rows(cache.k, 0, L + n), cache.rows(cache.v, 0, L + n)
+    for i in sorted({0, n // 2, n - 1, 64, 100}):
+        keep = ~none & (torch.arange(L + n) <= L + i)
+        if i >= n or not bool(keep.any()):                        # (a row that sees nothing else is not looked at)
+            continue
+        o, s, bo, bs = P.attention(q[i:i + 1], k[:, keep], v[:, keep], int(keep.sum()) - 1)
+        P.check(out[i:i + 1], o, bo, "row %d" % i)
+        P.check(lse[i:i + 1], s, bs, "lse of row %d" % i)
