@@ -15,19 +15,17 @@ __global__ __launch_bounds__(256) void prompt_attn_scalar_kernel(PromptParams p)
     const int b = sequence_of_row(p.cu_tokens, p.B, t, lane);
     if (b >= p.B) return;
     int bad = 0;
-    const int row = t - p.cu_tokens[b], L = p.seq_lens[b];
-    if (row < 0 || p.cu_tokens[b + 1] > p.N || L < 0 || (long long)L + row >= p.max_seq_len) bad |= READER_STATUS_BAD_LENGTH;
-    if (row >= 0) {
-        const long long last = (long long)max(L, 0) + row + 1;
-        const int keys = (int)(last < p.max_seq_len ? last : p.max_seq_len);
-        const ScalarRow<D> s = prompt_row_scalar<D>(p, p.q + ((size_t)t * p.Hq + hq) * D, p.page_table + (size_t)b * p.max_pages,
-                                                    hq / p.G, 0, keys, lane, bad);
-        const float inv = s.l == 0.f ? 0.f : 1.f / s.l;         // (a row that sees no key: zeros)
+    const int row = t - clamp_row(p.cu_tokens[b], p.N), L = p.seq_lens[b];
+    if (p.cu_tokens[b] < 0 || p.cu_tokens[b + 1] > p.N || L < 0 || (long long)L + row >= p.max_seq_len) bad |= READER_STATUS_BAD_LENGTH;
+    const long long last = (long long)max(L, 0) + row + 1;
+    const int keys = (int)(last < p.max_seq_len ? last : p.max_seq_len);
+    const ScalarRow<D> s = prompt_row_scalar<D>(p, p.q + ((size_t)t * p.Hq + hq) * D, p.page_table + (size_t)b * p.max_pages,
+                                                hq / p.G, 0, keys, lane, bad);
+    const float inv = s.l == 0.f ? 0.f : 1.f / s.l;             // (a row that sees no key: zeros)
 #pragma unroll
-        for (int e = 0; e < D / 64; ++e)
-            p.out[((size_t)t * p.Hq + hq) * D + lane * (D / 64) + e] = (uint16_t)pack_bf16x2(s.o[e] * inv, 0.f);
-        if (p.lse && lane == 0) p.lse[(size_t)t * p.Hq + hq] = s.l == 0.f ? -INFINITY : (s.m + __builtin_amdgcn_logf(s.l)) * kLn2;
-    }
+    for (int e = 0; e < D / 64; ++e)
+        p.out[((size_t)t * p.Hq + hq) * D + lane * (D / 64) + e] = (uint16_t)pack_bf16x2(s.o[e] * inv, 0.f);
+    if (p.lse && lane == 0) p.lse[(size_t)t * p.Hq + hq] = s.l == 0.f ? -INFINITY : (s.m + __builtin_amdgcn_logf(s.l)) * kLn2;
     if (bad && p.status) atomicOr(p.status, bad);
 }
 

@@ -5,11 +5,12 @@
 
 namespace reader {
 
-// Rows of a packed batch: sequence b owns rows cu_tokens[b] .. cu_tokens[b + 1] - 1 of N.  Nothing in a table that does
-// not hold that (a bound outside [0, N], or one below the bound in front of it) leads an access out of the tensors.
+// Rows of a packed batch: sequence b owns rows cu_tokens[b] .. cu_tokens[b + 1] - 1 of N.  Bounds outside [0, N] count as the
+// nearest one inside, so nothing in a table leads an access out of the tensors.
 __device__ inline int clamp_row(int row, int N) { return row < 0 ? 0 : (row > N ? N : row); }
 
-// Sequence of row t, found by a whole wavefront together: 64 bounds are compared at a time.  B: behind the last sequence.
+// Sequence that owns row t, found by a whole wavefront together: 64 bounds are compared at a time.  B: nobody's.  (Several, where
+// bounds go back: the first of them.)
 __device__ inline int sequence_of_row(const int32_t *__restrict__ cu_tokens, int B, int t, int lane) {
     int lo = 0, len = B;
     while (len > 64) {
@@ -18,10 +19,17 @@ __device__ inline int sequence_of_row(const int32_t *__restrict__ cu_tokens, int
         const int n = __popcll(__ballot(behind));
         lo += n * step;
         len = min(step, len - n * step);
-        if (len <= 0) return lo;
+        if (len <= 0) return B;
     }
-    const bool behind = lane < len && cu_tokens[lo + lane + 1] <= t;
-    return __builtin_amdgcn_readfirstlane(lo + __popcll(__ballot(behind)));
+    const bool owns = lane < len && cu_tokens[lo + lane] <= t && t < cu_tokens[lo + lane + 1];
+    const unsigned long long owners = __ballot(owns);
+    return __builtin_amdgcn_readfirstlane(owners ? lo + (int)__builtin_ctzll(owners) : B);
+}
+
+// What is wrong with sequence b's own bounds or its length: READER_STATUS_BAD_LENGTH or 0.
+__device__ inline int bad_sequence(const int32_t *__restrict__ cu_tokens, const int32_t *__restrict__ seq_lens, int N, int b) {
+    const int lo = cu_tokens[b], hi = cu_tokens[b + 1];
+    return seq_lens[b] < 0 || lo < 0 || hi < lo || hi > N ? READER_STATUS_BAD_LENGTH : 0;
 }
 
 struct QkvParams {

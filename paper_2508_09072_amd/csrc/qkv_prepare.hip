@@ -31,6 +31,12 @@ __global__ __launch_bounds__(kQkvThreads) void qkv_kernel(QkvParams p, int parts
     const int lane = threadIdx.x & 63;
     const long long unit = (long long)blockIdx.x * (kQkvThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int token = (int)(unit / parts), part = (int)(unit - (long long)token * parts);
+    // (one workgroup looks the table over, whether or not it owns a row of what is wrong)
+    if (p.cu_tokens && blockIdx.x == 0) {
+        int wrong = 0;
+        for (int i = threadIdx.x; i < p.B; i += kQkvThreads) wrong |= bad_sequence(p.cu_tokens, p.seq_lens, p.N, i);
+        if (wrong && p.status) atomicOr(p.status, wrong);
+    }
     if (token >= p.N) return;
 
     // the token's sequence, its row there, how far behind the sequence's first new position it stands
@@ -38,11 +44,9 @@ __global__ __launch_bounds__(kQkvThreads) void qkv_kernel(QkvParams p, int parts
     bool skip = false;
     if (p.cu_tokens) {
         b = sequence_of_row(p.cu_tokens, p.B, token, lane);
-        if (b >= p.B) return;                            // behind the last sequence: padding, left as it is
-        row = token - p.cu_tokens[b];
+        if (b >= p.B) return;                            // in front of the first or behind the last sequence: left as it is
+        row = token - clamp_row(p.cu_tokens[b], p.N);
         ahead = row;
-        if (row < 0 || p.cu_tokens[b + 1] > p.N) bad |= READER_STATUS_BAD_LENGTH;
-        skip = row < 0;
     } else {
         b = token / p.T;
         row = token - b * p.T;
