@@ -108,9 +108,8 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_attn_kernel(PromptParam
                     s_seq[p.B + b] = lo;
                     if (b == p.B - 1) s_seq[2 * p.B] = hi;
                 }
-                const int nn = seqs.tokens(b);
-                c = Block::sequence_cost(seqs.length(b), nn, tb);
-                if (len < 0 || lo < 0 || hi < lo || hi > p.N || (long long)len + nn > p.max_seq_len) bad |= READER_STATUS_BAD_LENGTH;
+                c = Block::sequence_cost(seqs.length(b), seqs.tokens(b), tb);
+                bad |= bad_sequence(p, b);
             }
             c = scan64(c);
             if (lane == 63) s_wave[wave_s] = c;

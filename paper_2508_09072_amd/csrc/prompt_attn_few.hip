@@ -41,9 +41,8 @@ __global__ __launch_bounds__(64 * kWaves) void prompt_few_kernel(PromptParams p)
         const int b = base + lane;
         long long c = 0;
         if (b < p.B) {
-            const int nn = seqs.tokens(b), len = p.seq_lens[b], lo = p.cu_tokens[b], hi = p.cu_tokens[b + 1];
-            c = Block::sequence_cost(seqs.length(b), nn, tb);
-            if (len < 0 || lo < 0 || hi < lo || hi > p.N || (long long)len + nn > p.max_seq_len) bad |= READER_STATUS_BAD_LENGTH;
+            c = Block::sequence_cost(seqs.length(b), seqs.tokens(b), tb);
+            bad |= bad_sequence(p, b);
         }
         return scan64(c);
     };

@@ -29,6 +29,7 @@ __global__ __launch_bounds__(kMidThreads, 2) void prompt_mid_kernel(PromptParams
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i16 = lane & 15, quad = lane >> 4, tb = p.tokens_per_block;
     int bad = 0;
+    report_bad_sequences(p, gridDim.x - 1, kMidThreads);     // (it has one of the shortest blocks, or none)
 
     // Block number j of a kv head, the last ones first (they are the longest).  Sequence b's are numbers cu[b] / tb + b and on: no two
     // the same, some nobody's.  With two workgroups a compute unit at once, the second round runs the other way, so that a long
@@ -51,11 +52,9 @@ __global__ __launch_bounds__(kMidThreads, 2) void prompt_mid_kernel(PromptParams
         len = min(step, len - n * step);
     }
     b = __builtin_amdgcn_readfirstlane(b);
-    const int lo = p.cu_tokens[b], hi = p.cu_tokens[b + 1], cached = p.seq_lens[b];
-    const int c0 = clamp_row(lo, p.N), n = max(clamp_row(hi, p.N) - c0, 0), L = min(max(cached, 0), p.max_seq_len);
+    const int c0 = clamp_row(p.cu_tokens[b], p.N), n = max(clamp_row(p.cu_tokens[b + 1], p.N) - c0, 0), L = min(max(p.seq_lens[b], 0), p.max_seq_len);
     const int k = id - (c0 / tb + b);
     if (k < 0 || (long long)k * tb >= n) return;
-    if (k == 0 && (cached < 0 || lo < 0 || hi < lo || hi > p.N || (long long)cached + n > p.max_seq_len)) bad |= READER_STATUS_BAD_LENGTH;
     const int nt = min(tb, n - k * tb), row0 = c0 + k * tb;
     const long long p0 = (long long)L + k * tb;
     const int keys = (int)min(p0 + nt, (long long)p.max_seq_len), steps = max(1, (keys + kStep - 1) / kStep);

@@ -11,12 +11,12 @@ __global__ __launch_bounds__(256) void prompt_attn_scalar_kernel(PromptParams p)
     const int lane = threadIdx.x & 63;
     const long long unit = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int t = (int)(unit / p.Hq), hq = (int)(unit - (long long)t * p.Hq);
+    int bad = 0;
+    report_bad_sequences(p, 0, 256);
     if (t >= p.N) return;
     const int b = sequence_of_row(p.cu_tokens, p.B, t, lane);
     if (b >= p.B) return;
-    int bad = 0;
     const int row = t - clamp_row(p.cu_tokens[b], p.N), L = p.seq_lens[b];
-    if (p.cu_tokens[b] < 0 || p.cu_tokens[b + 1] > p.N || L < 0 || (long long)L + row >= p.max_seq_len) bad |= READER_STATUS_BAD_LENGTH;
     const long long last = (long long)max(L, 0) + row + 1;
     const int keys = (int)(last < p.max_seq_len ? last : p.max_seq_len);
     const ScalarRow<D> s = prompt_row_scalar<D>(p, p.q + ((size_t)t * p.Hq + hq) * D, p.page_table + (size_t)b * p.max_pages,

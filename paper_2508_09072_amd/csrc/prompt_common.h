@@ -59,6 +59,18 @@ struct PromptParams {
     int32_t tokens_per_block;      // (matrix kernels) tokens whose heads fill a block of query rows
     int32_t n_ranges;              // ... and workgroups of the launch
 };
+// What the attention finds wrong with sequence b, whichever kernel runs: its bounds, its length, or keys beyond the bound on them.
+__device__ inline int bad_sequence(const PromptParams &p, int b) {
+    const long long tokens = (long long)p.cu_tokens[b + 1] - p.cu_tokens[b];
+    return p.seq_lens[b] + tokens > p.max_seq_len ? READER_STATUS_BAD_LENGTH : bad_sequence(p.cu_tokens, p.seq_lens, p.N, b);
+}
+// ... and with any of them, for kernels whose workgroups do not look at them all: workgroup `who` does.
+__device__ inline void report_bad_sequences(const PromptParams &p, unsigned who, int threads) {
+    if (blockIdx.x != who) return;
+    int bad = 0;
+    for (int b = threadIdx.x; b < p.B; b += threads) bad |= bad_sequence(p, b);
+    if (bad && p.status) atomicOr(p.status, bad);
+}
 // 256 rows a workgroup (prompt_attn.hip), 32, 64 or 128 and blocks that are never cut (prompt_attn_mid.hip), 16 or 32
 // (prompt_attn_few.hip); what the first and the last leave of cut blocks is folded by a second launch (prompt_merge.hip)
 size_t prompt_wide_workspace_bytes(int D);

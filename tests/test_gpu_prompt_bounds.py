@@ -1,5 +1,7 @@
-"""Packed bounds and lengths that are out of order, out of range or start behind row 0: the status, the rows of sequences that
-are as they should be, and nothing else written."""
+"""Packed bounds and lengths that are out of order, out of range or start behind row 0: the same status whatever kernel runs,
+the rows of sequences that are as they should be, and nothing else written."""
+import math
+
 import pytest
 import torch
 
@@ -14,6 +16,13 @@ def R():
     from paper_2508_09072_amd import binding
     binding.load()
     return binding
+
+
+@pytest.fixture(params=[0, 16, 32, 33, 64, 128, 256])
+def rows(R, request):
+    R.reader_tuning_override(R.TUNE_PROMPT_ROWS, request.param or -1)
+    yield request.param
+    R.reader_tuning_override(R.TUNE_PROMPT_ROWS, -1)
 
 
 def i32(x):
@@ -52,6 +61,73 @@ TABLES = [
     ([9, 7, 5, 2, -7], True, []),
 ]
 TOUCHED = {3: range(0, 18)}                                       # (a row that two sequences claim may be either's)
+
+
+@pytest.mark.parametrize("case", range(len(TABLES)))
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention(R, rows, case, D):
+    cu, wrong, owned = TABLES[case]
+    gen = torch.Generator().manual_seed(20 + case)
+    Hq, Hkv, L = 4, 2, [20, 0, 3, 40]
+    cache = P.Cache(gen, [l + N for l in L], Hkv, D)
+    for b in range(4):
+        cache.fill(gen, b, L[b] + N)
+    q = torch.randn((N, Hq, D), generator=gen).bfloat16()
+    dims = R.make_dims(4, 1, Hq, Hkv, D, cache.max_pages, 1, cache.num_pages, variant=1 if rows == 0 else 0)
+    bound = cache.max_pages * 16
+    ws = torch.full((max(256, R.reader_prompt_workspace_bytes(dims, N, bound)),), 0xff, dtype=torch.uint8, device="cuda")
+    out, lse, status = Guarded((N, Hq, D), torch.bfloat16), Guarded((N, Hq), torch.float32), i32([0])
+    R.reader_prompt_attn(dims, q.cuda(), cache.k.cuda(), cache.v.cuda(), cache.table.cuda(), i32(cu), i32(L), out.t, lse.t, bound, ws, status)
+    assert int(status) == (R.STATUS_BAD_LENGTH if wrong else 0)
+    touched = TOUCHED.get(case, [t for _, _, r in owned for t in r])
+    out.unchanged(touched)
+    lse.unchanged(touched)
+    for b, first, mine in owned:
+        end = max(mine) + 1
+        S = L[b] + end - first
+        o, s, bo, bs = P.attention(q[first:end], cache.rows(cache.k, b, S), cache.rows(cache.v, b, S), L[b])
+        for t in mine:
+            P.check(out.t[t], o[t - first], bo[t - first], "row %d" % t)
+            P.check(lse.t[t], s[t - first], bs[t - first], "lse of row %d" % t)
+
+
+@pytest.mark.parametrize("lens,bound", [([5, -3, 9, 2], 100), ([5, 101, 9, 2], 100), ([5, -2 ** 31, 9, 2 ** 31 - 1], 100)])
+def test_lengths_of_sequences_without_tokens(R, rows, lens, bound):
+    """Nobody reads their keys, but the table is wrong all the same."""
+    gen = torch.Generator().manual_seed(30)
+    Hq, Hkv, D, new = 4, 2, 64, [6, 0, 7, 0]
+    cache = P.Cache(gen, [112] * 4, Hkv, D)
+    for b in (0, 2):
+        cache.fill(gen, b, lens[b] + new[b])
+    q = torch.randn((13, Hq, D), generator=gen).bfloat16()
+    dims = R.make_dims(4, 1, Hq, Hkv, D, cache.max_pages, 1, cache.num_pages, variant=1 if rows == 0 else 0)
+    ws = torch.full((max(256, R.reader_prompt_workspace_bytes(dims, 13, bound)),), 0xff, dtype=torch.uint8, device="cuda")
+    out, status = torch.zeros((13, Hq, D), dtype=torch.bfloat16, device="cuda"), i32([0])
+    R.reader_prompt_attn(dims, q.cuda(), cache.k.cuda(), cache.v.cuda(), cache.table.cuda(), i32([0, 6, 6, 13, 13]), i32(lens), out, None, bound,
+                         ws, status)
+    assert int(status) == R.STATUS_BAD_LENGTH
+    for b, lo, hi in ((0, 0, 6), (2, 6, 13)):
+        S = lens[b] + hi - lo
+        o, _, bo, _ = P.attention(q[lo:hi], cache.rows(cache.k, b, S), cache.rows(cache.v, b, S), lens[b])
+        P.check(out[lo:hi], o, bo, "sequence %d" % b)
+
+
+@pytest.mark.parametrize("B", [100, 300, 4096])
+def test_one_bad_bound_among_many(R, rows, B):
+    gen = torch.Generator().manual_seed(B)
+    Hq, Hkv, D, n = 2, 1, 64, B + 20
+    cu = torch.arange(B + 1)
+    cu[B // 2] = 1                                                # goes back
+    cache = P.Cache(gen, [16] * B, Hkv, D)
+    q = torch.randn((n, Hq, D), generator=gen).bfloat16()
+    cache.k.zero_(), cache.v.zero_()
+    dims = R.make_dims(B, 1, Hq, Hkv, D, 1, 1, cache.num_pages, variant=1 if rows == 0 else 0)
+    ws = torch.full((max(256, R.reader_prompt_workspace_bytes(dims, n, 16)),), 0xff, dtype=torch.uint8, device="cuda")
+    out, status = Guarded((n, Hq, D), torch.bfloat16), i32([0])
+    # (the sequence behind the bad bound runs to its own end over all rows in front: its keys then pass the bound on lengths)
+    R.reader_prompt_attn(dims, q.cuda(), cache.k.cuda(), cache.v.cuda(), cache.table.cuda(), i32(cu), i32([0] * B), out.t, None, 16, ws, status)
+    assert int(status) == R.STATUS_BAD_LENGTH
+    out.unchanged(range(B))
 
 
 @pytest.mark.parametrize("case", range(len(TABLES)))
@@ -110,3 +186,34 @@ def test_projections_of_lengths_that_are_none(R, B):
     q.unchanged(range(B))
     kc.unchanged(range(B))
     vc.unchanged(range(B))
+
+
+@pytest.mark.parametrize("case", range(len(TABLES)))
+@pytest.mark.parametrize("decay", [0.0, 0.5])
+def test_key_weights(R, case, decay):
+    cu, wrong, _ = TABLES[case]
+    gen = torch.Generator().manual_seed(60 + case)
+    Hq, Hkv, D, L, window = 4, 2, 64, [20, 0, 3, 40], 7
+    cache = P.Cache(gen, [l + N for l in L], Hkv, D)
+    for b in range(4):
+        cache.fill(gen, b, L[b] + N)
+    q, lse = torch.randn((N, Hq, D), generator=gen).bfloat16(), 3 + torch.randn((N, Hq), generator=gen)
+    W = cache.max_pages * 16
+    old = torch.rand((4, Hkv, W), generator=gen)
+    w, status = Guarded((4, Hkv, W), torch.float32, inside=old), i32([0])
+    dims = R.make_dims(4, 1, Hq, Hkv, D, cache.max_pages, 1, cache.num_pages)
+    R.reader_prompt_key_weights(dims, q.cuda(), lse.cuda(), i32(cu), window, cache.k.cuda(), cache.table.cuda(), i32(L), decay, w.t, W, status)
+    assert int(status) == (R.STATUS_BAD_LENGTH if wrong else 0)
+    good = [b for b in range(4) if 0 <= cu[b] <= cu[b + 1] <= N]
+    w.unchanged(good)
+    for b in good:
+        n, S, end = min(window, cu[b + 1] - cu[b]), L[b] + cu[b + 1] - cu[b], cu[b + 1]
+        want = old[b].double() if decay else torch.zeros(Hkv, W, dtype=torch.float64)
+        want[:, :S] *= decay
+        error = torch.zeros_like(want)
+        if n:
+            x, bx = P.key_weights(q[end - n:end], lse[end - n:end], cache.rows(cache.k, b, S), S - n)
+            want[:, :S] += x
+            error[:, :S] = bx
+        error[:, :S] += 3 * P.F32 * want[:, :S]
+        P.check(w.t[b], want, error, "weights of sequence %d" % b)
