@@ -164,7 +164,7 @@ public:
     const int32_t *i32(bool optional = false) { return static_cast<const int32_t *>(ptr(kI32, optional)); }
     int32_t *i32_out(bool optional = false) { return static_cast<int32_t *>(ptr(kI32, optional)); }
     float *f32(bool optional = false) { return static_cast<float *>(ptr(kF32, optional)); }
-    // anything Python's int() takes
+    // anything Python's int() takes, if 32 bits hold it (their last 32 would be another number)
     int32_t integer() {
         if (!ok_) return 0;
         PyObject *o = raw();
@@ -173,7 +173,11 @@ public:
         const long long v = PyLong_AsLongLong(as_long);
         Py_DECREF(as_long);
         if (v == -1 && PyErr_Occurred()) ok_ = false;
-        return (int32_t)v;
+        else if (v < INT32_MIN || v > INT32_MAX) {
+            PyErr_Format(PyExc_ValueError, "%lld is more than 32 bits hold", v);
+            ok_ = false;
+        }
+        return ok_ ? (int32_t)v : 0;
     }
     // anything Python's float() takes
     double number() {

@@ -196,3 +196,13 @@ def test_rows_of_a_prompt(R):
         rows(1, -1, 10)
     with pytest.raises(R.ReaderError):
         rows(1, 10, 10, variant=3)
+
+
+@pytest.mark.parametrize("big", [1 << 32, (1 << 32) + 5, 1 << 31, -(1 << 31) - 1, 1 << 62])
+def test_numbers_that_32_bits_do_not_hold_are_refused(R, big):
+    """... and not taken for their last 32 bits: 2^32 + 5 kept rows are not five."""
+    bf, i, f = torch.zeros(1, 1, 1, dtype=torch.bfloat16), torch.zeros(1, dtype=torch.int32), torch.zeros(1)
+    d = dims(R)
+    for args in ((big, 0), (50, big)):
+        with pytest.raises(ValueError, match="32 bits"):
+            R.reader_kv_evict(d, *args, bf, bf, i, i, f, None)
