@@ -340,8 +340,8 @@ hipError_t launch_rows(const KeyWeightsParams &p, int span, hipStream_t stream) 
 }  // namespace
 
 hipError_t launch_key_weights(const KeyWeightsParams &p, hipStream_t stream) {
-    const int span = p.decay == 0.f ? p.max_positions : min(p.max_seq_len, p.max_positions);   // (a fresh start clears the whole row)
-    if (span <= 0) return hipSuccess;
+    // (a fresh start clears the whole row; where no position is allowed, lengths are still looked at)
+    const int span = max(p.decay == 0.f ? p.max_positions : min(p.max_seq_len, p.max_positions), 1);
     return p.D == 64 ? launch_rows<64>(p, span, stream) : launch_rows<128>(p, span, stream);
 }
 

@@ -217,3 +217,19 @@ def test_key_weights(R, case, decay):
             error[:, :S] = bx
         error[:, :S] += 3 * P.F32 * want[:, :S]
         P.check(w.t[b], want, error, "weights of sequence %d" % b)
+
+
+def test_key_weights_without_any_position(R):
+    """No position is allowed: lengths that have some do not fit, and are said to."""
+    gen = torch.Generator().manual_seed(70)
+    cache = P.Cache(gen, [20], 1, 64)
+    cache.fill(gen, 0, 20)
+    q, lse = torch.randn((2, 2, 64), generator=gen).bfloat16().cuda(), torch.zeros((2, 2), device="cuda")
+    dims = R.make_dims(1, 1, 2, 1, 64, cache.max_pages, 1, cache.num_pages)
+    for decay in (0.0, 1.0):
+        w, status = torch.full((1, 1, 32), 2.0, device="cuda"), i32([0])
+        R.reader_prompt_key_weights(dims, q, lse, i32([0, 2]), 2, cache.k.cuda(), cache.table.cuda(), i32([5]), decay, w, 0, status)
+        assert int(status) == R.STATUS_BAD_LENGTH and bool((w == 2.0).all())
+        status.zero_()
+        R.reader_prompt_key_weights(dims, q, lse, i32([0, 0]), 2, cache.k.cuda(), cache.table.cuda(), i32([0]), decay, w, 0, status)
+        assert int(status) == 0 and bool((w == (2.0 if decay else 0.0)).all())
