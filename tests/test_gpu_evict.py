@@ -107,3 +107,16 @@ def test_sequences_that_do_not_fit_are_left_as_they_are(R):
     assert got[2] == [bad[0], 60, keep, -4]
     for g, x in zip((got[0], got[1], got[3]), (want[0], want[1], want[3])):
         assert torch.equal(bits(g), bits(x))
+
+
+@pytest.mark.parametrize("kind", ["normal", "ties"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("NL,L,Hkv,keep,recent", [
+    (4, [700, 90], 4, 333, 20), (3, [300, 20, 150], 4, 100, 0), (11, [40], 3, 17, 17), (5, [1500, 900, 1200], 4, 1100, 90),
+    (17, [129, 64], 1, 64, 1), (9, [600, 1, 0, 599], 1, 513, 100),
+])
+def test_many_layers_and_heads(R, kind, D, NL, L, Hkv, keep, recent):
+    """32 (layer, sequence, kv head) triples and more, whose rows move in wider slices; several passes of 512 rows, not whole ones."""
+    gen = torch.Generator().manual_seed(keep + D + NL)
+    cache, w = make(gen, NL, L, Hkv, D, kind)
+    same(run(R, cache, L, w, keep, recent), expect(cache, L, w, keep, recent))
