@@ -891,12 +891,15 @@ static hipError_t launch_prompt(const PromptParams &p, hipStream_t stream) {
     return launch_prompt_merge(p, kPromptRows, stream);
 }
 
-size_t prompt_wide_workspace_bytes(int D) { return kNotesBytes + (size_t)2 * kNumCU * prompt_record_floats(D) * sizeof(float); }
+constexpr int kWideRanges = kNumCU;                  // workgroups of the launch: one a compute unit
+static_assert(kWideRanges <= kMaxRanges, "the workspace has a note for each");
+
+size_t prompt_wide_workspace_bytes(int D) { return ranges_workspace_bytes(kWideRanges, kPromptRows, D); }
 
 hipError_t launch_prompt_wide(const PromptParams &params, hipStream_t stream) {
     PromptParams p = params;
     p.tokens_per_block = kPromptRows / p.G;
-    p.n_ranges = kNumCU;
+    p.n_ranges = kWideRanges;
     return p.D == 64 ? launch_prompt<64>(p, stream) : launch_prompt<128>(p, stream);
 }
 

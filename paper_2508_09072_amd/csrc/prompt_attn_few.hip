@@ -13,10 +13,10 @@ namespace reader {
 namespace {
 
 using Block = PromptBlock<kStep, 2 * kStep, 4 * kStep>;
-// Wavefronts of a compute unit that run at once: as many as their stages fit the LDS.
-constexpr int few_wavefronts(int D) { return D == 128 ? 4 : 8; }
-
 constexpr int kWaves = 4;
+// Workgroups of the launch, a range each: as many as run at once, by their stages in the LDS.
+constexpr int few_ranges(int D) { return kNumCU * (D == 128 ? 1 : 2); }
+static_assert(few_ranges(64) <= kMaxRanges && few_ranges(128) <= kMaxRanges, "the workspace has a note for each");
 
 // kBlocks: blocks of 16 query rows
 template <int D, int kBlocks>
@@ -216,7 +216,7 @@ __global__ __launch_bounds__(64 * kWaves) void prompt_few_kernel(PromptParams p)
 
 template <int D, int kBlocks>
 hipError_t launch_few(PromptParams p, hipStream_t stream) {
-    p.n_ranges = kNumCU * few_wavefronts(D) / kWaves;
+    p.n_ranges = few_ranges(D);
     hipLaunchKernelGGL((prompt_few_kernel<D, kBlocks>), dim3(p.n_ranges), dim3(64 * kWaves), 0, stream, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return note_hip_error("launch prompt_few_kernel", e);
@@ -232,6 +232,6 @@ hipError_t launch_prompt_few(const PromptParams &params, int rows, hipStream_t s
     return p.D == 64 ? launch_few<64, 2>(p, stream) : launch_few<128, 2>(p, stream);
 }
 
-size_t prompt_few_workspace_bytes(int D) { return kNotesBytes + (size_t)2 * kNumCU * few_wavefronts(D) * 32 * (D + 2) * sizeof(float); }
+size_t prompt_few_workspace_bytes(int D) { return ranges_workspace_bytes(few_ranges(D), 32, D); }
 
 }  // namespace reader

@@ -16,8 +16,11 @@ struct RangeNote {
     int head, row0, nt;   // ... this one: kv head, first packed row, tokens
     int pad[2];
 };
-constexpr int kMaxRanges = kNumCU * 8;
+constexpr int kMaxRanges = kNumCU * 2;               // of any launch
 constexpr size_t kNotesBytes = (size_t)kMaxRanges * sizeof(RangeNote);   // in front of the records, two a range
+constexpr size_t ranges_workspace_bytes(int n_ranges, int record_rows, int D) {
+    return kNotesBytes + (size_t)2 * n_ranges * record_rows * (D + 2) * sizeof(float);
+}
 
 // Sums of the lanes up to each.
 template <int kControl, int kRows>

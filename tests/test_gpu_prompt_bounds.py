@@ -233,3 +233,26 @@ def test_key_weights_without_any_position(R):
         status.zero_()
         R.reader_prompt_key_weights(dims, q, lse, i32([0, 0]), 2, cache.k.cuda(), cache.table.cuda(), i32([0]), decay, w, 0, status)
         assert int(status) == 0 and bool((w == (2.0 if decay else 0.0)).all())
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n,L", [(1, 40000), (9, 20000), (130, 9000)])
+def test_nothing_behind_the_workspace(R, rows, D, n, L):
+    """Every range of a launch leaves records, and the workspace is no larger than it has to be."""
+    gen = torch.Generator().manual_seed(80)
+    Hq, Hkv = 16, 8
+    cache = P.Cache(gen, [L + n], Hkv, D)
+    cache.fill(gen, 0, L + n)
+    q = torch.randn((n, Hq, D), generator=gen).bfloat16()
+    dims = R.make_dims(1, 1, Hq, Hkv, D, cache.max_pages, 1, cache.num_pages, variant=1 if rows == 0 else 0)
+    need = R.reader_prompt_workspace_bytes(dims, n, L + n)
+    ws = torch.full((need + 512,), 0xff, dtype=torch.uint8, device="cuda")
+    out, status = torch.zeros((n, Hq, D), dtype=torch.bfloat16, device="cuda"), i32([0])
+    R.reader_prompt_attn(dims, q.cuda(), cache.k.cuda(), cache.v.cuda(), cache.table.cuda(), i32([0, n]), i32([L]), out, None, L + n,
+                         ws[256:256 + need], status)
+    assert int(status) == 0
+    assert bool((ws[:256] == 0xff).all()) and bool((ws[256 + need:] == 0xff).all())
+    k, v = cache.rows(cache.k, 0, L + n), cache.rows(cache.v, 0, L + n)
+    for t in {0, n - 1}:
+        o, _, bo, _ = P.attention(q[t:t + 1], k[:, :L + t + 1], v[:, :L + t + 1], L + t)
+        P.check(out[t:t + 1], o, bo, "row %d" % t)
