@@ -20,7 +20,7 @@ constexpr int kMidThreads = 256, kMidStages = 4;
 // kBlocks: blocks of 16 query rows that a wavefront carries.  kSplit: 1, every wavefront has rows of its own and takes all steps, or
 // 2, wavefronts 2 and 3 have the rows of 0 and 1 and take the other half of the steps.
 template <int D, int kBlocks, int kSplit>
-__global__ __launch_bounds__(kMidThreads, 2) void prompt_mid_kernel(PromptParams p) {
+__device__ __forceinline__ void prompt_mid_block(const PromptParams &p) {
     using Rows = PromptRows<D, kBlocks>;
     using Page = PageLayout<D>;
     constexpr int kStageBytes = 2 * kStepPages * Page::kPageBytes;
@@ -29,7 +29,6 @@ __global__ __launch_bounds__(kMidThreads, 2) void prompt_mid_kernel(PromptParams
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i16 = lane & 15, quad = lane >> 4, tb = p.tokens_per_block;
     int bad = 0;
-    report_bad_sequences(p, gridDim.x - 1, kMidThreads);     // (it has one of the shortest blocks, or none)
 
     // Block number j of a kv head, the last ones first (they are the longest).  Sequence b's are numbers cu[b] / tb + b and on: no two
     // the same, some nobody's.  With two workgroups a compute unit at once, the second round runs the other way, so that a long
@@ -141,6 +140,12 @@ __global__ __launch_bounds__(kMidThreads, 2) void prompt_mid_kernel(PromptParams
     if (p.status && bad) atomicOr(p.status, bad);
 }
 
+template <int D, int kBlocks, int kSplit>
+__global__ __launch_bounds__(kMidThreads, 2) void prompt_mid_kernel(PromptParams p) {
+    prompt_mid_block<D, kBlocks, kSplit>(p);
+    // (the last workgroup: it has one of the shortest blocks, or none)
+    if (blockIdx.x == gridDim.x - 1) report_bad_sequences(p, kMidThreads);
+}
 
 template <int D, int kBlocks, int kSplit>
 hipError_t launch_mid(PromptParams p, hipStream_t stream) {

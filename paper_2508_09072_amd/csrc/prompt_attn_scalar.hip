@@ -12,11 +12,12 @@ __global__ __launch_bounds__(256) void prompt_attn_scalar_kernel(PromptParams p)
     const long long unit = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int t = (int)(unit / p.Hq), hq = (int)(unit - (long long)t * p.Hq);
     int bad = 0;
-    report_bad_sequences(p, 0, 256);
+    if (blockIdx.x == 0) report_bad_sequences(p, 256);
     if (t >= p.N) return;
-    const int b = sequence_of_row(p.cu_tokens, p.B, t, lane);
+    int first = 0;
+    const int b = sequence_of_row(p.cu_tokens, p.B, t, lane, first);
     if (b >= p.B) return;
-    const int row = t - clamp_row(p.cu_tokens[b], p.N), L = p.seq_lens[b];
+    const int row = t - first, L = p.seq_lens[b];
     const long long last = (long long)max(L, 0) + row + 1;
     const int keys = (int)(last < p.max_seq_len ? last : p.max_seq_len);
     const ScalarRow<D> s = prompt_row_scalar<D>(p, p.q + ((size_t)t * p.Hq + hq) * D, p.page_table + (size_t)b * p.max_pages,

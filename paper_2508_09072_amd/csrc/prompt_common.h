@@ -9,9 +9,9 @@ namespace reader {
 // nearest one inside, so nothing in a table leads an access out of the tensors.
 __device__ inline int clamp_row(int row, int N) { return row < 0 ? 0 : (row > N ? N : row); }
 
-// Sequence that owns row t, found by a whole wavefront together: 64 bounds are compared at a time.  B: nobody's.  (Several, where
-// bounds go back: the first of them.)
-__device__ inline int sequence_of_row(const int32_t *__restrict__ cu_tokens, int B, int t, int lane) {
+// Sequence that owns row t, found by a whole wavefront together: 64 bounds are compared at a time.  first: its first row.  B: nobody's.
+// (Several, where bounds go back: the first of them.)
+__device__ inline int sequence_of_row(const int32_t *__restrict__ cu_tokens, int B, int t, int lane, int &first) {
     int lo = 0, len = B;
     while (len > 64) {
         const int step = (len + 63) >> 6, at = lo + (lane + 1) * step - 1;
@@ -21,9 +21,12 @@ __device__ inline int sequence_of_row(const int32_t *__restrict__ cu_tokens, int
         len = min(step, len - n * step);
         if (len <= 0) return B;
     }
-    const bool owns = lane < len && cu_tokens[lo + lane] <= t && t < cu_tokens[lo + lane + 1];
-    const unsigned long long owners = __ballot(owns);
-    return __builtin_amdgcn_readfirstlane(owners ? lo + (int)__builtin_ctzll(owners) : B);
+    const int at = lo + min(lane, len - 1), from = cu_tokens[at], to = cu_tokens[at + 1];
+    const unsigned long long owners = __ballot(lane < len && from <= t && t < to);
+    if (owners == 0) return B;
+    const int owner = (int)__builtin_ctzll(owners);
+    first = max(__builtin_amdgcn_readlane(from, owner), 0);
+    return __builtin_amdgcn_readfirstlane(lo + owner);
 }
 
 // What is wrong with sequence b's own bounds or its length: READER_STATUS_BAD_LENGTH or 0.
@@ -64,10 +67,10 @@ __device__ inline int bad_sequence(const PromptParams &p, int b) {
     const long long tokens = (long long)p.cu_tokens[b + 1] - p.cu_tokens[b];
     return p.seq_lens[b] + tokens > p.max_seq_len ? READER_STATUS_BAD_LENGTH : bad_sequence(p.cu_tokens, p.seq_lens, p.N, b);
 }
-// ... and with any of them, for kernels whose workgroups do not look at them all: workgroup `who` does.
-__device__ inline void report_bad_sequences(const PromptParams &p, unsigned who, int threads) {
-    if (blockIdx.x != who) return;
+// ... and with any of them, for kernels whose workgroups do not look at them all: one of them does, threads side by side.
+__device__ inline void report_bad_sequences(const PromptParams &p, int threads) {
     int bad = 0;
+#pragma unroll 4
     for (int b = threadIdx.x; b < p.B; b += threads) bad |= bad_sequence(p, b);
     if (bad && p.status) atomicOr(p.status, bad);
 }

@@ -25,27 +25,31 @@ __device__ inline void unpack8(const u32x4 &w, float (&x)[8]) {
 }
 
 // A wavefront takes one token and every `parts`-th group of its head rows.  A row is D / 8 lanes of 8 values.
-template <int D>
-__global__ __launch_bounds__(kQkvThreads) void qkv_kernel(QkvParams p, int parts) {
+// kPacked: rows of packed prompts, else nodes of trees.  (80 registers at most, for six wavefronts a SIMD: five take 10 % longer.)
+template <int D, bool kPacked>
+__global__ __launch_bounds__(kQkvThreads, 6) void qkv_kernel(QkvParams p, int parts) {
     constexpr int kLanes = D / 8, kRows = 64 / kLanes;
     const int lane = threadIdx.x & 63;
-    const long long unit = (long long)blockIdx.x * (kQkvThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int token = (int)(unit / parts), part = (int)(unit - (long long)token * parts);
-    // (one workgroup looks the table over, whether or not it owns a row of what is wrong)
-    if (p.cu_tokens && blockIdx.x == 0) {
+    // (the first workgroup of packed rows looks the table over, whether or not anybody owns a row of what is wrong)
+    if (kPacked && blockIdx.x == 0) {
         int wrong = 0;
-        for (int i = threadIdx.x; i < p.B; i += kQkvThreads) wrong |= bad_sequence(p.cu_tokens, p.seq_lens, p.N, i);
+#pragma unroll 4
+        for (int b = threadIdx.x; b < p.B; b += kQkvThreads) wrong |= bad_sequence(p.cu_tokens, p.seq_lens, p.N, b);
         if (wrong && p.status) atomicOr(p.status, wrong);
+        return;
     }
+    const long long unit = (long long)(blockIdx.x - (kPacked ? 1 : 0)) * (kQkvThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int token = (int)(unit / parts), part = (int)(unit - (long long)token * parts);
     if (token >= p.N) return;
 
     // the token's sequence, its row there, how far behind the sequence's first new position it stands
     int b, row, ahead, bad = 0;
     bool skip = false;
-    if (p.cu_tokens) {
-        b = sequence_of_row(p.cu_tokens, p.B, token, lane);
+    if constexpr (kPacked) {
+        int first = 0;
+        b = sequence_of_row(p.cu_tokens, p.B, token, lane, first);
         if (b >= p.B) return;                            // in front of the first or behind the last sequence: left as it is
-        row = token - clamp_row(p.cu_tokens[b], p.N);
+        row = token - first;
         ahead = row;
     } else {
         b = token / p.T;
@@ -67,7 +71,7 @@ __global__ __launch_bounds__(kQkvThreads) void qkv_kernel(QkvParams p, int parts
     // where the key and value rows go: [Hkv] rows `stride` apart from `at`
     size_t at = 0, stride = D;
     bool store_kv = !skip;
-    if (p.k_tree) {
+    if (!kPacked && p.k_tree) {
         at = (size_t)token * p.Hkv * D;
     } else {
         const long long j = (long long)L + row;
@@ -83,7 +87,7 @@ __global__ __launch_bounds__(kQkvThreads) void qkv_kernel(QkvParams p, int parts
     }
     if (bad && p.status && lane == 0 && part == 0) atomicOr(p.status, bad);
     if (skip) return;
-    uint16_t *const k_out = (p.k_tree ? p.k_tree : p.k_cache) + at, *const v_out = (p.k_tree ? p.v_tree : p.v_cache) + at;
+    uint16_t *const k_out = (!kPacked && p.k_tree ? p.k_tree : p.k_cache) + at, *const v_out = (!kPacked && p.k_tree ? p.v_tree : p.v_cache) + at;
 
     // this lane's values of a head row: 8 c .. 8 c + 7; the angles of its pairs and, of pairs half a rotation apart, the
     // lane that holds the other halves
@@ -168,19 +172,24 @@ __global__ __launch_bounds__(kQkvThreads) void qkv_kernel(QkvParams p, int parts
     }
 }
 
-}  // namespace
-
-hipError_t launch_qkv(const QkvParams &p, hipStream_t stream) {
+template <int D, bool kPacked>
+hipError_t launch(const QkvParams &p, hipStream_t stream) {
     const int rows = 64 / (p.D / 8), groups = (p.Hq + 2 * p.Hkv + rows - 1) / rows;
     // A token's rows go to as many wavefronts as fill the chip once, up to four of them to as many as fill it four times (4096
     // tokens of 80 heads: 45.7 us with one, 43.1 with four; 1000 tokens of 48 heads: 9.6 us with five, 12 with twelve).
     const long long once = (kNumCU * 16LL + p.N - 1) / p.N, often = (kNumCU * 64LL + p.N - 1) / p.N;
     long long parts = once > 4 ? once : often < 4 ? often : 4;
     parts = parts > groups ? groups : parts;
-    const long long blocks = ((long long)p.N * parts + kQkvThreads / 64 - 1) / (kQkvThreads / 64);
-    if (p.D == 64) hipLaunchKernelGGL(qkv_kernel<64>, dim3((unsigned)blocks), dim3(kQkvThreads), 0, stream, p, (int)parts);
-    else hipLaunchKernelGGL(qkv_kernel<128>, dim3((unsigned)blocks), dim3(kQkvThreads), 0, stream, p, (int)parts);
+    const long long blocks = ((long long)p.N * parts + kQkvThreads / 64 - 1) / (kQkvThreads / 64) + (kPacked ? 1 : 0);
+    hipLaunchKernelGGL((qkv_kernel<D, kPacked>), dim3((unsigned)blocks), dim3(kQkvThreads), 0, stream, p, (int)parts);
     return note_hip_error("launch qkv_kernel", hipGetLastError());
+}
+
+}  // namespace
+
+hipError_t launch_qkv(const QkvParams &p, hipStream_t stream) {
+    if (p.cu_tokens) return p.D == 64 ? launch<64, true>(p, stream) : launch<128, true>(p, stream);
+    return p.D == 64 ? launch<64, false>(p, stream) : launch<128, false>(p, stream);
 }
 
 }  // namespace reader
