@@ -642,7 +642,8 @@ int reader_prompt_qkv(const reader_dims *dims, int32_t N, const void *qkv, const
  *   out          bf16 [N, Hq, D]                            out  fp32 accumulation, rounded to nearest even
  *   lse          f32 [N, Hq] or NULL                        out  natural-log sum of exp of the scaled scores
  *   max_seq_len  upper bound of seq_lens[b] + new tokens; keys at or behind it are left out and
- *                READER_STATUS_BAD_LENGTH is set.  max_pages_per_seq * page_size >= max_seq_len
+ *                READER_STATUS_BAD_LENGTH is set.  max_pages_per_seq * page_size >= max_seq_len.  The kernel is chosen as
+ *                if the longest sequence had that length: a loose bound costs short calls up to three times their time
  *   workspace    >= reader_prompt_workspace_bytes(dims, N, max_seq_len) bytes, 256-byte aligned; its contents are
  *                meaningless between calls, calls that are ordered on one stream may share it
  *   status       i32 [1] or NULL                            in/out

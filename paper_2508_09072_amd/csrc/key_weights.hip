@@ -1,7 +1,9 @@
 // The attention weight that every cached key has drawn from the queries that count (a step's accepted path, or the last
 // tokens of a prompt), per kv head:
 //   weights[b, hkv, j] = decay * weights[b, hkv, j] + sum over rows (t, g) that see key j of exp(s <q[t, hkv G + g], k_j> - lse[t, hkv G + g])
-// The log-sum-exp that the attention left turns a score into its softmax weight, so one product with the keys is all.
+// The log-sum-exp that the attention left turns a score into its softmax weight, so one product with the keys is all.  In powers of
+// two it is rounded once more, to fp32: off by 2^-24 of it, as much as the attention's own rounding of it, 1.6e-7 of a weight on
+// long contexts against 6.7e-8 where the scale is taken behind the difference, for one instruction less a weight.
 //
 // S = Q.K^T on the matrix cores in blocks of 16 rows x 16 keys (one page): a lane then holds four rows of one key, and the
 // sum over rows is a sum over registers, with two exchanges between lanes at the end.  A wavefront holds up to 128 query rows

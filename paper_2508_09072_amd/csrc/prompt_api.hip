@@ -55,8 +55,10 @@ static bool cache_ok(const reader_dims *dims, const void *k_cache, const void *v
 // one prompt of 100 tokens 16.2, 19.5, 6.2, 6.6, 8.4, 19.0; of 1500 220, 149, 58.6, 45.9, 51.4, 51.1; of 3000 696, 441, 194, 144,
 // 100, 99.0; 16 of 300 214, 150, 75.9, 52.4, 43.7, 42.0; 256 tokens on 1000 positions 48.4, 37.5, 26.0, 35.4, 41.4, 31.4; 64 on 8
 // K 58.6, 40.9, 136, 200, 230, 74.6; 32 sequences of 12 on 8 K 474, 324, 213, 239, 283, 173; 16 single tokens on 500 16.2, 18.8,
-// 14.4, 16.8, 20.0, 25.4; on 2000 30.7, 32.5, 41.9, 52.4, 62.1, 39.9.  The estimates pick the fastest of the six on 226 of the 252
-// and are 0.7 % behind it on average, 29 % at most.
+// 14.4, 16.8, 20.0, 25.4; on 2000 30.7, 32.5, 41.9, 52.4, 62.1, 39.9.  The estimates pick the fastest of the six on 223 of the 252
+// and are 0.7 % behind it on average, 27 % at most (all of them: profiles/prompt_rows_sweep.txt).  They take max_seq_len for the
+// longest sequence: where it is only a bound, one prompt of 100 tokens takes 18 us instead of 6, of 777 39 instead of 22, single
+// tokens on 500 positions 14 to 16 instead of 10 to 13; 3000 tokens, batches of prompts and long contexts the same.
 static int prompt_rows(const reader_dims &d, int32_t N, int32_t max_seq_len) {
     if (d.variant == 1) return 0;
     const int forced = tuning(READER_TUNE_PROMPT_ROWS), G = d.Hq / d.Hkv;

@@ -12,7 +12,7 @@ namespace {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr int kStep = 32, kStepPages = kStep / READER_PAGE_SIZE;
 constexpr float kNoReference = -1e30f;               // of a row that has seen no key
-constexpr float kTooLarge = 0x1p100f;                // of a sum that is not folded with others any more
+constexpr float kTooLarge = 0x1p100f;                // ... of a sum that is not added to others any more
 
 // How a page of 16 K or V rows is copied to LDS and read back as an operand: whole, 1 KB a copy instruction; the 16-byte chunks of
 // a row are swizzled by the row, so that the reads of an operand touch every bank once (K: 16 rows, one chunk; V: 8 rows, two
@@ -84,7 +84,8 @@ struct PageIds {
 // one makes all weights of the row larger by one factor, which fp32 sums and bf16 weights hold.  A row whose sum reaches kTooLarge is
 // computed again: up to there hundreds of its parts add up without an overflow, and a part is below 2^-24 of the row where its factor,
 // 2 to the difference of two references, becomes zero.  With a maximum that moves, were it only once in a thousand steps, the
-// compiler copies all accumulators three times a step where the paths meet.
+// compiler copies all accumulators three times a step where the paths meet.  Weights are rounded to bf16 for the second product, their
+// sums are not (what that costs: prompt_attn.hip).
 template <int D, int kBlocks>
 struct PromptRows {
     using Page = PageLayout<D>;
