@@ -568,11 +568,14 @@ int reader_tuning_override(int32_t which, int32_t value);
  * Packed prompts: the new tokens of all sequences are rows of one tensor, sequence b's are rows
  * cu_tokens[b] .. cu_tokens[b + 1] - 1 (i32 [B + 1], not decreasing, cu_tokens[0] >= 0, cu_tokens[B] <= N); rows
  * in front of the first and behind the last sequence are padding and stay as they were.  A sequence may have no new
- * tokens.  Bounds out of order or of range set READER_STATUS_BAD_LENGTH.  One out of range counts as the nearest of 0
- * and N, a sequence whose bounds go back has no tokens, and where bounds go back rows may be taken for those of either of two
- * sequences that claim them, or be left as they were; nothing but rows of the batch and of its sequences is written.  (The
- * key weights leave a sequence whose bounds are wrong as it is.)  New keys and values go behind the seq_lens[b] positions that the cache holds (as a draft tree's do in the in-cache layout);
- * every layer's calls see the same seq_lens, and the caller adds the new tokens to it after the last layer.
+ * tokens.  New keys and values go behind the seq_lens[b] positions that the cache holds (as a draft tree's do in the
+ * in-cache layout); every layer's calls see the same seq_lens, and the caller adds the new tokens to it after the last
+ * layer.
+ *
+ * Bounds out of order or of range, and negative lengths, set READER_STATUS_BAD_LENGTH, whoever they are of.  A bound out
+ * of range counts as the nearest of 0 and N.  A sequence whose bounds go back has no tokens, and in such a batch a row
+ * may be taken for that of either of two sequences that claim it, or be left as it was; nothing but rows of the batch
+ * and of its sequences is written.  (The key weights leave a sequence whose bounds are wrong as it is.)
  *
  * bf16 tensors and the rotation table start at a multiple of 16 bytes (READER_EINVAL otherwise).  No output overlaps an
  * input, but for what is named in/out.
