@@ -1,10 +1,10 @@
 """What a serving program asks of a cache held in 4 bits and of the pages of a cache, as a list of timed cases.
 
-  store    K/V rows become 4-bit rows of the paged cache: of a step's draft trees (reader_kv4_store), or of a prompt that was
-           worked on in a bf16 cache (reader_kv4_pack, all layers in one call)
-  attn     attention over that cache: of draft trees (reader_kv4_tree_attn), of packed prompts, chunks and single tokens
-           (reader_kv4_prompt_attn)
-  compact  the accepted path's rows move to where they stay, all layers (reader_kv4_compact_layers)
+  store    K/V rows become 4-bit rows of the paged cache: of a step's draft trees (reader_kvq_store), or of a prompt that was
+           worked on in a bf16 cache (reader_kvq_pack, all layers in one call)
+  attn     attention over that cache: of draft trees (reader_kvq_tree_attn), of packed prompts, chunks and single tokens
+           (reader_kvq_prompt_attn)
+  compact  the accepted path's rows move to where they stay, all layers (reader_kvq_compact_layers)
   reorder  sequences are forked, permuted and dropped by their page tables (reader_pages_reorder)
   reserve  pages for the positions that the next step writes: taken, given back, copied where others hold them too
            (reader_pages_reserve)
@@ -249,19 +249,19 @@ def prepare(case, seed):
     s.cu_tokens = _i32(np.concatenate([[0], np.cumsum(new)]))
     if kind == "store":
         NL = case.get("NL", 1)
-        s.kv4 = torch.zeros((NL, s.num_pages, Hkv, 17 * D), dtype=torch.uint8, device=DEVICE)
+        s.kvq = torch.zeros((NL, s.num_pages, Hkv, 17 * D), dtype=torch.uint8, device=DEVICE)
         if case["form"] == "pages":
             s.from_table = _i32(_table(rng, L, s.num_pages, s.max_pages))
             s.k, s.v = (_normal(gen, NL, s.num_pages, Hkv, PAGE, D) for _ in range(2))
             s.k.mul_(torch.randn((Hkv, 1, D), generator=gen, device=DEVICE).exp_())      # channels of their own size
         else:
-            s.kv4 = s.kv4[0]
+            s.kvq = s.kvq[0]
             shape = (B, case["T"]) if case["form"] == "tree" else (N,)
             s.k, s.v = (_normal(gen, *shape, Hkv, D) for _ in range(2))
             s.k.mul_(torch.randn((Hkv, D), generator=gen, device=DEVICE).exp_())
         return s
     if kind == "compact":
-        s.kv4 = _held(gen, case["NL"], s.num_pages, Hkv, D=D)
+        s.kvq = _held(gen, case["NL"], s.num_pages, Hkv, D=D)
         n = _accepted(case)
         path = np.full((B, case["path"]), -1, dtype=np.int32)
         path[:, 0] = 0
@@ -270,7 +270,7 @@ def prepare(case, seed):
         path[:, 1:] = np.where(np.arange(1, case["path"])[None, :] < n[:, None], pick, -1)
         s.path, s.accept_len = _i32(path), _i32(n - 1)
         return s
-    s.kv4 = _held(gen, s.num_pages, Hkv, D=D)
+    s.kvq = _held(gen, s.num_pages, Hkv, D=D)
     s.parents = None
     if case["form"] == "tree":
         i = np.arange(case["T"])
@@ -330,7 +330,7 @@ def _rows(first, count):
 
 def _plain_store(s):
     case, D = s.case, s.case["D"]
-    kv4 = s.kv4 if s.kv4.dim() == 4 else s.kv4[None]
+    kvq = s.kvq if s.kvq.dim() == 4 else s.kvq[None]
     if case["form"] == "pages":
         seq, at = _rows(torch.zeros_like(s.seq_lens).long(), s.seq_lens.long())
         page, slot = s.from_table.long()[seq, at // PAGE], at % PAGE
@@ -341,10 +341,10 @@ def _plain_store(s):
     kc, ks, kbad = _quantised(k)
     vc, vs, vbad = _quantised(v)
     page, place = s.page_table.long()[seq, at // PAGE], _places(at % PAGE, D)
-    layer, head = torch.arange(kv4.shape[0], device=DEVICE), torch.arange(case["Hkv"], device=DEVICE)
-    kv4[layer[:, None, None], page[:, None, None, None], head[:, None], place[:, None, None, :]] = torch.cat([kc, vc, ks, vs], dim=-1)
+    layer, head = torch.arange(kvq.shape[0], device=DEVICE), torch.arange(case["Hkv"], device=DEVICE)
+    kvq[layer[:, None, None], page[:, None, None, None], head[:, None], place[:, None, None, :]] = torch.cat([kc, vc, ks, vs], dim=-1)
     s.status |= 16 * (kbad | vbad)
-    return {"kv4": s.kv4, "status": s.status}
+    return {"kvq": s.kvq, "status": s.status}
 
 
 def _ancestors(parents):
@@ -365,7 +365,7 @@ def _plain_attn(s):
     pages = int((_lengths(case) + _new(case)).max() + PAGE - 1) // PAGE
     n, S = int(_new(case).max()), pages * PAGE
     # the keys of all sequences, [B, Hkv, S, D], zeros behind the last one
-    block = s.kv4[s.page_table[:, :pages].clamp(min=0).long()]                            # [B, pages, Hkv, 17 D]
+    block = s.kvq[s.page_table[:, :pages].clamp(min=0).long()]                            # [B, pages, Hkv, 17 D]
     rows = block[..., _places(torch.arange(PAGE, device=DEVICE), D)].permute(0, 2, 1, 3, 4).reshape(B, Hkv, S, -1)
     there = torch.arange(S, device=DEVICE) < (L + new)[:, None]
     k = _dequantised(rows[..., : D // 2], rows[..., D:D + D // 32]) * there[:, None, :, None]
@@ -400,9 +400,9 @@ def _plain_compact(s):
     table = s.page_table.long()
     page = lambda at: table[seq, at // PAGE][:, None, None]                               # noqa: E731
     place = lambda at: _places(at % PAGE, case["D"])[:, None, :]                          # noqa: E731
-    s.kv4[:, page(L + j), heads, place(L + j)] = s.kv4[:, page(L + node), heads, place(L + node)]
+    s.kvq[:, page(L + j), heads, place(L + j)] = s.kvq[:, page(L + node), heads, place(L + node)]
     s.seq_lens += s.accept_len + 1
-    return {"kv4": s.kv4, "seq_lens": s.seq_lens, "status": s.status}
+    return {"kvq": s.kvq, "seq_lens": s.seq_lens, "status": s.status}
 
 
 def _changed(refs, table, by):
@@ -471,18 +471,18 @@ def _library(s):
     room = lambda nbytes: torch.empty((max(nbytes, 256),), dtype=torch.uint8, device=DEVICE)     # noqa: E731
     if kind == "store":
         if case["form"] == "pages":
-            return lambda: R.reader_kv4_pack(dims, s.k, s.v, s.from_table, None, s.seq_lens, s.max_seq_len, s.kv4, s.page_table, s.status)
-        return lambda: R.reader_kv4_store(dims, s.k, s.v, None if tree else s.cu_tokens, s.seq_lens, s.kv4, s.page_table, s.status)
+            return lambda: R.reader_kvq_pack(dims, s.k, s.v, s.from_table, None, s.seq_lens, s.max_seq_len, s.kvq, s.page_table, s.status)
+        return lambda: R.reader_kvq_store(dims, s.k, s.v, None if tree else s.cu_tokens, s.seq_lens, s.kvq, s.page_table, s.status)
     if kind == "attn":
         N = s.q.numel() // (case["Hq"] * D)
-        ws = room(R.reader_kv4_workspace_bytes(dims, N, s.max_seq_len))
+        ws = room(R.reader_kvq_workspace_bytes(dims, N, s.max_seq_len))
         if tree:
-            return lambda: R.reader_kv4_tree_attn(dims, s.q, s.kv4, s.page_table, s.seq_lens, s.parents, s.out, s.lse, s.max_seq_len,
+            return lambda: R.reader_kvq_tree_attn(dims, s.q, s.kvq, s.page_table, s.seq_lens, s.parents, s.out, s.lse, s.max_seq_len,
                                                   ws, s.status)
-        return lambda: R.reader_kv4_prompt_attn(dims, s.q, s.kv4, s.page_table, s.cu_tokens, s.seq_lens, s.out, s.lse, s.max_seq_len,
+        return lambda: R.reader_kvq_prompt_attn(dims, s.q, s.kvq, s.page_table, s.cu_tokens, s.seq_lens, s.out, s.lse, s.max_seq_len,
                                                 ws, s.status)
     if kind == "compact":
-        return lambda: R.reader_kv4_compact_layers(dims, s.path, s.accept_len, s.kv4, s.page_table, s.seq_lens, s.status)
+        return lambda: R.reader_kvq_compact_layers(dims, s.path, s.accept_len, s.kvq, s.page_table, s.seq_lens, s.status)
     ws = room(R.reader_pages_workspace_bytes(dims))
     if kind == "reorder":
         return lambda: R.reader_pages_reorder(dims, s.sources, s.page_table, s.seq_lens, s.page_refs, ws, s.status)
@@ -503,11 +503,11 @@ def run(s):
         s.call = _library(s)
     s.call()
     if kind == "store":
-        return {"kv4": s.kv4, "status": s.status}
+        return {"kvq": s.kvq, "status": s.status}
     if kind == "attn":
         return {"out": s.out, "lse": s.lse, "status": s.status}
     if kind == "compact":
-        return {"kv4": s.kv4, "seq_lens": s.seq_lens, "status": s.status}
+        return {"kvq": s.kvq, "seq_lens": s.seq_lens, "status": s.status}
     if kind == "reorder":
         return {"page_table": s.page_table, "seq_lens": s.seq_lens, "page_refs": s.page_refs, "status": s.status}
     return _reserve_outputs(s)
@@ -585,7 +585,7 @@ def exact(case, seed):
                 mine[i, i] = True
             sees[:, L[b]:] = dev(mine)
         for h in range(Hkv):
-            block = s.kv4[page, h]
+            block = s.kvq[page, h]
             k, v = values(block, k_at, ks_at)[:S], values(block, v_at, vs_at)[:S]
             x = q[first:first + n, h * G:(h + 1) * G].transpose(0, 1) @ k.t() / math.sqrt(D)     # [G, n, S]
             x = x.masked_fill(~sees, -math.inf)
