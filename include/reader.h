@@ -73,7 +73,9 @@ enum {
     READER_STATUS_BAD_TREE = 1, /* parents[b][0] != -1 or parents[b][i] not in [0, i) */
     READER_STATUS_BAD_PAGE = 2, /* a page id outside [0, num_pages) was met */
     READER_STATUS_BAD_PATH = 4, /* accept_len/path entry out of range, or path longer than max_path */
-    READER_STATUS_BAD_LENGTH = 8 /* a length, packed bound or position that the tensors, the page table or a table of positions do not hold */
+    READER_STATUS_BAD_LENGTH = 8, /* a length, packed bound or position that the tensors, the page table or a table of positions do not hold */
+    READER_STATUS_BAD_VALUE = 16, /* a value that the cache in 4 bits cannot hold: a NaN or an infinity */
+    READER_STATUS_NO_PAGES = 32   /* the pool has fewer free pages than were asked for */
 };
 
 enum {
@@ -734,6 +736,169 @@ int reader_kv_evict(const reader_dims *dims, int32_t num_layers, int32_t keep, i
                     void *k_cache, void *v_cache, const int32_t *page_table, int32_t *seq_lens,
                     float *weights, int32_t max_positions, void *workspace, size_t workspace_bytes,
                     int32_t *status, void *stream);
+
+/*
+ * ------------------------------------------------------------------ a cache in 4 bits
+ * The paged cache at 17 / 64 of the bytes: K and V of a position in 4 bits a value.  Values 32 g .. 32 g + 31 of a row share a
+ * scale 2^e, -125 <= e <= 125, and each is one of 0, 1/2, 1, 3/2, 2, 3, 4, 6 times it, with a sign: exact in bf16.  With a the
+ * largest magnitude of the group, e = floor(log2(a)) - 2, and one more where a > 7 * 2^e, so that no value moves by more than 2^e (but
+ * where the upper bound on e holds it back, a > 7 * 2^125); values are rounded to nearest even.  A group with a NaN or an infinity
+ * is stored as zeros and READER_STATUS_BAD_VALUE is set.
+ *
+ *   kvq_cache   u8 [num_pages, Hkv, READER_KVQ_BLOCK_BYTES(D)], 16-byte aligned.  A block holds, for the 16 rows s of a page, d even:
+ *     codes of values d, d + 1 of K (the low half of a byte is the even value's; bit 3 of a code is its sign, the others number
+ *       the values above)       at  d / (D/4) * 2 D + s * (D/8) + d % (D/4) / 2
+ *     ... of V                  at  8 D + s / 4 * 2 D + d / (D/16) * (D/8) + s % 4 * (D/32) + d % (D/16) / 2
+ *     the scale of K's group g  at  16 D + 16 g + s            (a byte, e + 127)
+ *     ... of V's                at  16 D + D / 2 + s / 4 * (D/8) + 4 g + s % 4
+ *   (whole-number divisions).  Scale bytes above 252 are of no value: the rows that read them are unspecified.
+ *
+ * The rows of new tokens and of draft trees are stored behind the seq_lens[b] positions that the cache holds before the attention is
+ * called, as in the in-cache layout of reader_tree_attn: plain decoding and the verification of a tree then read the same
+ * values.  dims->variant must be 0; the bf16 tensors start at a multiple of 16 bytes.  A page that rows are stored in
+ * belongs to one sequence (reader_pages_reserve).
+ */
+#define READER_KVQ_BLOCK_BYTES(D) (17 * (D))
+
+/*
+ * K/V rows into the cache: row t of sequence b, its i-th new one, goes to position seq_lens[b] + i.
+ *
+ *   N            rows
+ *   k, v         bf16 [N, Hkv, D]                           in   (k_tree, v_tree of reader_tree_qkv, for one)
+ *   cu_tokens    i32 [B + 1] or NULL                        in   packed rows as above; NULL: draft trees, N = B * T
+ *   seq_lens     i32 [B]                                    in
+ *   kvq_cache    u8 [num_pages, Hkv, 17 D]                  out
+ *   page_table   i32 [B, max_pages_per_seq]                 in
+ *   status       i32 [1] or NULL                            in/out
+ *
+ * A row that the page table does not hold (READER_STATUS_BAD_LENGTH) or whose page id is out of range (BAD_PAGE) is left out.
+ * One launch.
+ */
+int reader_kvq_store(const reader_dims *dims, int32_t N, const void *k, const void *v, const int32_t *cu_tokens,
+                     const int32_t *seq_lens, void *kvq_cache, const int32_t *page_table, int32_t *status, void *stream);
+
+/*
+ * Positions [starts[b], seq_lens[b]) of a bf16 cache into the same positions of the cache in 4 bits, all layers in one call: a
+ * prompt is worked on in bf16 (reader_prompt_qkv, reader_prompt_attn) and kept in 4 bits.
+ *
+ *   k_cache, v_cache  bf16 [num_layers, from_pages, Hkv, page_size, D]   in
+ *   from_table   i32 [B, max_pages_per_seq]                 in   pages of k_cache and v_cache
+ *   starts       i32 [B] or NULL                            in   NULL: zeros
+ *   seq_lens     i32 [B]                                    in   ends, at most max_seq_len
+ *   kvq_cache    u8 [num_layers, num_pages, Hkv, 17 D]      out
+ *   page_table   i32 [B, max_pages_per_seq]                 in   pages of kvq_cache
+ *   status       i32 [1] or NULL                            in/out
+ *
+ * A sequence whose bounds are out of order, or behind max_seq_len or the page table, is left out (READER_STATUS_BAD_LENGTH), as are
+ * the positions of a page whose id is out of range in either table (BAD_PAGE).  One launch.
+ */
+int reader_kvq_pack(const reader_dims *dims, int32_t num_layers, const void *k_cache, const void *v_cache, int64_t from_pages,
+                    const int32_t *from_table, const int32_t *starts, const int32_t *seq_lens, int32_t max_seq_len, void *kvq_cache,
+                    const int32_t *page_table, int32_t *status, void *stream);
+
+/*
+ * reader_kv_compact_layers on the cache in 4 bits: for every b, layer, kv head and j = 1..accept_len[b], position seq_lens[b] + j
+ * receives the row that position seq_lens[b] + path[b][j] held; then seq_lens[b] += accept_len[b] + 1.  The same checks, status
+ * bits and results; num_layers 0: only the lengths.  Calls on several streams do not meet (nothing is kept between calls).
+ *
+ *   kvq_cache    u8 [num_layers, num_pages, Hkv, 17 D]      in/out
+ */
+int reader_kvq_compact_layers(const reader_dims *dims, int32_t num_layers, const int32_t *path, const int32_t *accept_len,
+                              void *kvq_cache, const int32_t *page_table, int32_t *seq_lens, int32_t *status, void *stream);
+
+/*
+ * Tree-masked attention over the cache in 4 bits: reader_tree_attn in its in-cache layout, the row of node n of sequence b at
+ * position seq_lens[b] + n.
+ *
+ *   q            bf16 [B, T, Hq, D]                         in
+ *   kvq_cache    u8 [num_pages, Hkv, 17 D]                  in
+ *   page_table   i32 [B, max_pages_per_seq]                 in   must map pages for [0, seq_lens[b] + T)
+ *   seq_lens     i32 [B]                                    in   tree rows excluded
+ *   parents      i32 [B, T]                                 in
+ *   out          bf16 [B, T, Hq, D]                         out  fp32 accumulation, rounded to nearest even
+ *   lse          f32 [B, Hq, T] or NULL                     out
+ *   max_seq_len  upper bound of seq_lens[b]; max_pages_per_seq * page_size >= max_seq_len + T.  A longer sequence counts as this
+ *                long (READER_STATUS_BAD_LENGTH)
+ *   workspace    >= reader_kvq_workspace_bytes(dims, B * T, max_seq_len) bytes, 256-byte aligned; its contents are meaningless
+ *                between calls, calls that are ordered on one stream may share it
+ *   status       i32 [1] or NULL                            in/out
+ *
+ * A node whose link is wrong counts as a root (BAD_TREE): it sees the prefix and itself.  Keys behind a page id out of range are left
+ * out (BAD_PAGE); a row that sees no key gives zeros and a log-sum-exp of -inf.  What the pages hold behind the last row does
+ * not reach the outputs.  Softmax weights are rounded to bf16 before they multiply V.  dims->max_path is not used.  Two launches.
+ */
+size_t reader_kvq_workspace_bytes(const reader_dims *dims, int32_t N, int32_t max_seq_len);
+int reader_kvq_tree_attn(const reader_dims *dims, const void *q, const void *kvq_cache, const int32_t *page_table,
+                         const int32_t *seq_lens, const int32_t *parents, void *out, float *lse, int32_t max_seq_len,
+                         void *workspace, size_t workspace_bytes, int32_t *status, void *stream);
+
+/*
+ * Causal attention of packed prompts, chunks and single tokens over the cache in 4 bits: arguments, masks, padding and status bits
+ * of reader_prompt_attn, the new tokens' rows stored already.
+ *
+ *   q            bf16 [N, Hq, D]                            in
+ *   out          bf16 [N, Hq, D]                            out
+ *   lse          f32 [N, Hq] or NULL                        out
+ *   max_seq_len  upper bound of seq_lens[b] + new tokens; keys at or behind it are left out (READER_STATUS_BAD_LENGTH)
+ *   workspace    >= reader_kvq_workspace_bytes(dims, N, max_seq_len) bytes, 256-byte aligned
+ */
+int reader_kvq_prompt_attn(const reader_dims *dims, int32_t N, const void *q, const void *kvq_cache, const int32_t *page_table,
+                           const int32_t *cu_tokens, const int32_t *seq_lens, void *out, float *lse, int32_t max_seq_len,
+                           void *workspace, size_t workspace_bytes, int32_t *status, void *stream);
+
+/*
+ * ------------------------------------------------------------------ pages that sequences share
+ * A pool of num_pages pages, of whichever cache: page_refs[p] is the number of entries of page tables that name page p, and a page
+ * nobody names is free.  Sequences may hold pages together (the prefix that they share, a beam and its forks); entries that
+ * hold no page are -1.  The two calls below keep the counts; a page that is held elsewhere too has a count of its own there (the
+ * entries of the table at hand are added and taken away, never counted anew).  Counts that do not match the tables give pages away
+ * that are in use: nothing checks them.
+ *
+ *   page_table   i32 [B, max_pages_per_seq]                 in/out
+ *   page_refs    i32 [num_pages]                            in/out
+ *   workspace    >= reader_pages_workspace_bytes(dims) bytes, 4-byte aligned; its contents are meaningless between calls
+ * Of dims only B, max_pages_per_seq and num_pages are used; the rest has to be valid.  No atomics but of whole numbers: the same
+ * inputs give the same results.
+ */
+size_t reader_pages_workspace_bytes(const reader_dims *dims);
+
+/*
+ * Row b of the batch becomes what row sources[b] was before the call: forks (a source that is named twice), permutations, and
+ * sequences dropped (a row that nobody names).  The new row holds the pages of its positions, all of them shared with the
+ * row's other forks, and nothing behind (pages that were reserved there are given back); seq_lens follows.
+ *
+ *   sources      i32 [B]                                    in   -1: the row becomes empty, of length 0
+ *   seq_lens     i32 [B]                                    in/out
+ *   status       i32 [1] or NULL                            in/out
+ *
+ * A source outside [-1, B) counts as b (READER_STATUS_BAD_PATH).  An entry in front of a sequence's length that names no page
+ * is handed on as it is (BAD_PAGE); a length that the table does not hold takes the whole row (BAD_LENGTH).  Two launches.
+ */
+int reader_pages_reorder(const reader_dims *dims, const int32_t *sources, int32_t *page_table, int32_t *seq_lens, int32_t *page_refs,
+                         void *workspace, size_t workspace_bytes, int32_t *status, void *stream);
+
+/*
+ * Makes positions [seq_lens[b], new_lens[b]) of every sequence ready to be written: on pages that nobody else holds.
+ *   - the page that seq_lens[b] falls into the middle of, if others hold it too: a free page takes its place and its contents, in
+ *     all layers; of the sequences of the call that write into one page and hold it alone together, the last keeps it
+ *   - pages that lie wholly behind seq_lens[b]: entries that hold none, or one that others hold too, get a free page
+ *   - pages behind new_lens[b] are given back; entries there that name no page become -1
+ * Free pages are taken in ascending order, for the sequences in their order and the pages of each from the first; what the call
+ * gives back can be taken by it.  If there are not as many as are wanted, none is taken or given back and READER_STATUS_NO_PAGES is
+ * set.  seq_lens is not changed.
+ *
+ *   num_layers   >= 0 (0: no contents to copy, the caches are not used)
+ *   page_bytes   bytes of a page of one layer, a multiple of 16
+ *   seq_lens, new_lens  i32 [B]                             in   new_lens[b] >= seq_lens[b] (else the sequence is left as it is,
+ *                                                                READER_STATUS_BAD_LENGTH, as where the table does not hold new_lens[b])
+ *   k_cache, v_cache    [num_layers, num_pages, page_bytes] in/out, 16-byte aligned; v_cache may be NULL (one cache: the one in 4 bits)
+ *   status       i32 [1] or NULL                            in/out
+ *
+ * A page id out of range in the middle of which seq_lens[b] falls sets BAD_PAGE and stays.  Two launches.
+ */
+int reader_pages_reserve(const reader_dims *dims, int32_t num_layers, int64_t page_bytes, const int32_t *seq_lens, const int32_t *new_lens,
+                         void *k_cache, void *v_cache, int32_t *page_table, int32_t *page_refs, void *workspace,
+                         size_t workspace_bytes, int32_t *status, void *stream);
 
 #ifdef __cplusplus
 }

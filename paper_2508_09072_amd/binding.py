@@ -28,6 +28,8 @@ STATUS_BAD_TREE = 1
 STATUS_BAD_PAGE = 2
 STATUS_BAD_PATH = 4
 STATUS_BAD_LENGTH = 8
+STATUS_BAD_VALUE = 16
+STATUS_NO_PAGES = 32
 TUNE_ATTN_ROWS, TUNE_ATTN_RANGES, TUNE_ATTN_PAIR_COST, TUNE_ATTN_AXIS64, TUNE_ATTN_WIDE, TUNE_ATTN_PAIR_FRONT, TUNE_ATTN_SHORT, TUNE_JOIN, TUNE_JOIN_SPREAD = 0, 1, 2, 3, 4, 5, 6, 7, 8
 TUNE_PROMPT_ROWS = 9
 PROMPT_ROWS_32_UNCUT = 33   # of reader_prompt_rows
@@ -38,6 +40,8 @@ EXPORTS = (
     "reader_kv_rearrange_scratch_bytes", "reader_kv_rearrange", "reader_target_argmax", "reader_target_sample", "reader_kv_compact_layers",
     "reader_tree_qkv", "reader_prompt_qkv", "reader_prompt_workspace_bytes", "reader_prompt_rows", "reader_prompt_attn", "reader_key_weights",
     "reader_prompt_key_weights", "reader_kv_evict_workspace_bytes", "reader_kv_evict",
+    "reader_kvq_store", "reader_kvq_pack", "reader_kvq_compact_layers", "reader_kvq_workspace_bytes", "reader_kvq_tree_attn",
+    "reader_kvq_prompt_attn", "reader_pages_workspace_bytes", "reader_pages_reorder", "reader_pages_reserve",
     "reader_trie_create", "reader_trie_destroy", "reader_trie_nodes", "reader_trie_insert", "reader_trie_search_path",
     "reader_trie_extract_tree", "reader_tree_attach_path", "reader_self_repetition", "reader_tree_prune_order",
     "reader_tree_select",
@@ -170,6 +174,24 @@ def load():
     lib.reader_kv_evict_workspace_bytes.argtypes = [dp, i32, i32]
     lib.reader_kv_evict.restype = ctypes.c_int
     lib.reader_kv_evict.argtypes = [dp, i32, i32, i32] + [vp] * 5 + [i32, vp, sz, vp, vp]
+    lib.reader_kvq_store.restype = ctypes.c_int
+    lib.reader_kvq_store.argtypes = [dp, i32] + [vp] * 8
+    lib.reader_kvq_pack.restype = ctypes.c_int
+    lib.reader_kvq_pack.argtypes = [dp, i32, vp, vp, i64, vp, vp, vp, i32, vp, vp, vp, vp]
+    lib.reader_kvq_compact_layers.restype = ctypes.c_int
+    lib.reader_kvq_compact_layers.argtypes = [dp, i32] + [vp] * 7
+    lib.reader_kvq_workspace_bytes.restype = sz
+    lib.reader_kvq_workspace_bytes.argtypes = [dp, i32, i32]
+    lib.reader_kvq_tree_attn.restype = ctypes.c_int
+    lib.reader_kvq_tree_attn.argtypes = [dp] + [vp] * 7 + [i32, vp, sz, vp, vp]
+    lib.reader_kvq_prompt_attn.restype = ctypes.c_int
+    lib.reader_kvq_prompt_attn.argtypes = [dp, i32] + [vp] * 7 + [i32, vp, sz, vp, vp]
+    lib.reader_pages_workspace_bytes.restype = sz
+    lib.reader_pages_workspace_bytes.argtypes = [dp]
+    lib.reader_pages_reorder.restype = ctypes.c_int
+    lib.reader_pages_reorder.argtypes = [dp] + [vp] * 5 + [sz, vp, vp]
+    lib.reader_pages_reserve.restype = ctypes.c_int
+    lib.reader_pages_reserve.argtypes = [dp, i32, i64] + [vp] * 7 + [sz, vp, vp]
     lib.reader_profile_enable.restype = ctypes.c_int
     lib.reader_profile_enable.argtypes = [i32]
     lib.reader_profile_collect.restype = ctypes.c_int
@@ -409,6 +431,73 @@ def reader_kv_evict(dims, keep, recent, k_cache, v_cache, page_table, seq_lens, 
                                                 status)
     if code:
         _check(code, "reader_kv_evict")
+
+
+KVQ_BLOCK_BYTES = {64: 17 * 64, 128: 17 * 128}      # of a page of a kv head, by the head dimension
+
+
+def reader_kvq_store(dims, k, v, cu_tokens, seq_lens, kvq_cache, page_table, status=None):
+    """k, v: bf16 [N, Hkv, D], packed by cu_tokens, or [B, T, Hkv, D] with cu_tokens None (draft trees);
+    kvq_cache: uint8 [num_pages, Hkv, 17 D], updated in place."""
+    code = (_native or _load_native()).kvq_store(dims, k, v, cu_tokens, seq_lens, kvq_cache, page_table, status)
+    if code:
+        _check(code, "reader_kvq_store")
+
+
+def reader_kvq_pack(dims, k_cache, v_cache, from_table, starts, seq_lens, max_seq_len, kvq_cache, page_table, status=None):
+    """k_cache, v_cache: bf16 [num_layers, from_pages, Hkv, page_size, D]; starts: int32 [B] or None (zeros);
+    kvq_cache: uint8 [num_layers, num_pages, Hkv, 17 D], updated in place."""
+    code = (_native or _load_native()).kvq_pack(dims, k_cache, v_cache, from_table, starts, seq_lens, max_seq_len, kvq_cache,
+                                                page_table, status)
+    if code:
+        _check(code, "reader_kvq_pack")
+
+
+def reader_kvq_compact_layers(dims, path, accept_len, kvq_cache, page_table, seq_lens, status=None):
+    """kvq_cache: uint8 [num_layers, num_pages, Hkv, 17 D]; it and seq_lens in place."""
+    code = (_native or _load_native()).kvq_compact_layers(dims, path, accept_len, kvq_cache, page_table, seq_lens, status)
+    if code:
+        _check(code, "reader_kvq_compact_layers")
+
+
+def reader_kvq_workspace_bytes(dims: ReaderDims, N: int, max_seq_len: int) -> int:
+    return int(load().reader_kvq_workspace_bytes(ctypes.byref(dims), int(N), int(max_seq_len)))
+
+
+def reader_kvq_tree_attn(dims, q, kvq_cache, page_table, seq_lens, parents, out, lse, max_seq_len, workspace, status=None):
+    """q, out: bf16 [B, T, Hq, D]; kvq_cache: uint8 [num_pages, Hkv, 17 D]; lse: float32 [B, Hq, T] or None."""
+    code = (_native or _load_native()).kvq_tree_attn(dims, q, kvq_cache, page_table, seq_lens, parents, out, lse, max_seq_len,
+                                                     workspace, status)
+    if code:
+        _check(code, "reader_kvq_tree_attn")
+
+
+def reader_kvq_prompt_attn(dims, q, kvq_cache, page_table, cu_tokens, seq_lens, out, lse, max_seq_len, workspace, status=None):
+    """q, out: bf16 [N, Hq, D]; kvq_cache: uint8 [num_pages, Hkv, 17 D]; lse: float32 [N, Hq] or None."""
+    code = (_native or _load_native()).kvq_prompt_attn(dims, q, kvq_cache, page_table, cu_tokens, seq_lens, out, lse, max_seq_len,
+                                                       workspace, status)
+    if code:
+        _check(code, "reader_kvq_prompt_attn")
+
+
+def reader_pages_workspace_bytes(dims: ReaderDims) -> int:
+    return int(load().reader_pages_workspace_bytes(ctypes.byref(dims)))
+
+
+def reader_pages_reorder(dims, sources, page_table, seq_lens, page_refs, workspace, status=None):
+    """sources: int32 [B]; page_table: int32 [B, max_pages_per_seq], seq_lens: int32 [B], page_refs: int32 [num_pages], in place."""
+    code = (_native or _load_native()).pages_reorder(dims, sources, page_table, seq_lens, page_refs, workspace, status)
+    if code:
+        _check(code, "reader_pages_reorder")
+
+
+def reader_pages_reserve(dims, seq_lens, new_lens, k_cache, v_cache, page_table, page_refs, workspace, status=None):
+    """k_cache, v_cache: [num_layers, num_pages, ...] of any type (v_cache None: one cache; both None: no contents), page_table and
+    page_refs in place."""
+    code = (_native or _load_native()).pages_reserve(dims, seq_lens, new_lens, k_cache, v_cache, page_table, page_refs, workspace,
+                                                     status)
+    if code:
+        _check(code, "reader_pages_reserve")
 
 
 def _host_i32(a):

@@ -1,0 +1,496 @@
+// Attention over a cache in 4 bits, of packed prompts, chunks and single tokens (causal) and of draft trees whose rows are in the
+// cache behind their sequence (ancestors only).
+#include "kvq_common.h"
+#include "prompt_ranges.h"
+#include "tree_attn_common.h"
+
+namespace reader {
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+constexpr int kStep = 32, kStepPages = kStep / READER_PAGE_SIZE;
+constexpr float kNoReference = -1e30f;               // of a row that has seen no key
+constexpr float kMostSum = 0x1p16f;                  // ... of a lane's part of a row's sum, before its reference moves
+using Block = PromptBlock<kStep, 2 * kStep, 4 * kStep>;
+
+// Two codes of byte `kByte` of a word, times 2^(scale - 127) in the exponent bits of `scale`: exact.
+template <int kByte>
+__device__ __forceinline__ uint32_t two_values(uint32_t word, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, kByte));
+}
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// One lane's bytes of a page: K of row i16 and quarter `quad`, V of rows 4 quad .. + 3 and chunk i16.
+template <int D>
+struct KvqPage {
+    static constexpr int kWords = D / 32;
+    uint32_t k[kWords], v[kWords], ks, vs;
+    __device__ __forceinline__ void load(const uint8_t *block, int lane, int i16, int quad) {
+        using B = KvqBlock<D>;
+        typedef uint32_t words __attribute__((ext_vector_type(kWords)));
+        const words kw = *reinterpret_cast<const words *>(block + lane * (kWords * 4));
+        const words vw = *reinterpret_cast<const words *>(block + B::kV + lane * (kWords * 4));
+#pragma unroll
+        for (int w = 0; w < kWords; ++w) { k[w] = kw[w]; v[w] = vw[w]; }
+        ks = block[B::kKScales + (D == 128 ? quad : quad >> 1) * 16 + i16];
+        vs = *reinterpret_cast<const uint32_t *>(block + B::kVScales + quad * (D / 8) + (i16 * B::kChunk / 32) * 4);
+    }
+    // takes row e of the lane's four out of V
+    __device__ __forceinline__ void drop(int e) {
+        if constexpr (D == 128) v[e] = 0;
+        else v[e / 2] &= 0xffffu << (e % 2 ? 0 : 16);
+        vs = (vs & ~(255u << (8 * e))) | (127u << (8 * e));
+    }
+};
+
+// kBlocks blocks of 16 query rows, carried through 32 keys at a time.  S^T = K.Q^T leaves lane (quad, i16) with four scores of row
+// i16 for each page, keys 4 quad .. + 3: as they stand, the operand of O^T += V^T.P^T whose other one is the lane's V.
+template <int D, int kBlocks>
+struct KvqRows {
+    static constexpr int kSteps = D / 32, kOut = D / 16;
+    bf16x8 q[kBlocks][kSteps];                                // step s: values (D / 4) quad + 8 s .. + 7 of row i16
+    int lim[kBlocks], node[kBlocks];                          // keys that row i16 sees (trees: at most), its node
+    bool real[kBlocks];
+    f32x4 acc[kBlocks][kOut];                                 // [i][k]: output value (4 quad + k) D / 16 + i of row i16
+    float m[kBlocks], l[kBlocks];                             // reference (exponent of two), this lane's part of the sum
+    f32x4 x[kBlocks][kStepPages];                             // scores
+    u32x4 pk[kBlocks];                                        // weights of 32 keys, an operand
+
+    __device__ static __forceinline__ size_t out_row(const PromptParams &p, int head, int row0, int nt, int row) {
+        const int tok = (int)(((float)row + 0.5f) * p.g_rcp);
+        return ((size_t)row0 + min(tok, nt - 1)) * p.Hq + (size_t)head * p.G + (row - tok * p.G);
+    }
+    __device__ __forceinline__ void load(const PromptParams &p, int head, int row0, long long p0, int node0, int nt, int first, int i16, int quad) {
+#pragma unroll
+        for (int r = 0; r < kBlocks; ++r) {
+            const int row = first + r * 16 + i16, tok = (int)(((float)row + 0.5f) * p.g_rcp);    // row / G
+            real[r] = tok < nt;
+            node[r] = node0 + min(tok, nt - 1);
+            lim[r] = real[r] ? (int)min(p0 + tok + 1, (long long)p.max_seq_len) : 0;
+            const size_t at = out_row(p, head, row0, nt, row);
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) q[r][s] = __builtin_bit_cast(bf16x8, keep_if(real[r], ld16(p.q + at * D + quad * (D / 4) + s * 8)));
+            m[r] = kNoReference;
+            l[r] = 0.f;
+#pragma unroll
+            for (int i = 0; i < kOut; ++i) acc[r][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+    __device__ __forceinline__ void scores(const KvqPage<D> (&pages)[kStepPages]) {
+#pragma unroll
+        for (int pg = 0; pg < kStepPages; ++pg) {
+            const float sc = scale_of(pages[pg].ks);
+#pragma unroll
+            for (int r = 0; r < kBlocks; ++r) x[r][pg] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                const uint32_t w = pages[pg].k[s];
+                const u32x4 k = {two_values<0>(w, sc), two_values<1>(w, sc), two_values<2>(w, sc), two_values<3>(w, sc)};
+#pragma unroll
+                for (int r = 0; r < kBlocks; ++r)
+                    x[r][pg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), q[r][s], x[r][pg], 0, 0, 0);
+            }
+        }
+    }
+    // Weights of the scores, and what the lane's sums become with them: the largest of those.
+    __device__ __forceinline__ float weights(float c2, float (&sum)[kBlocks]) {
+        float most = 0.f;
+#pragma unroll
+        for (int r = 0; r < kBlocks; ++r) {
+            float w[8];
+            sum[r] = l[r];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                w[e] = __builtin_amdgcn_exp2f(x[r][e / 4][e % 4] * c2 - m[r]);
+                sum[r] += w[e];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) pk[r][e] = pack_bf16x2(w[2 * e], w[2 * e + 1]);
+            most = fmaxf(most, sum[r]);
+        }
+        return most;
+    }
+    // Moves the references so that no weight of the scores at hand is above one, nor a row's sum.
+    __device__ __forceinline__ void move_references(float c2) {
+#pragma unroll
+        for (int r = 0; r < kBlocks; ++r) {
+            float mx = fmaxf(fmaxf(x[r][0][0], x[r][0][1]), fmaxf(x[r][0][2], x[r][0][3]));
+            mx = fmaxf(mx, fmaxf(fmaxf(x[r][1][0], x[r][1][1]), fmaxf(x[r][1][2], x[r][1][3]))) * c2;
+            mx = fmaxf(mx, m[r] + __builtin_amdgcn_logf(l[r]));              // (minus infinity where the sum is zero)
+            mx = fmaxf(mx, __shfl_xor(mx, 16));
+            mx = fmaxf(mx, __shfl_xor(mx, 32));
+            const float top = fmaxf(m[r], mx), f = __builtin_amdgcn_exp2f(m[r] - top);
+            l[r] *= f;
+            m[r] = top;
+#pragma unroll
+            for (int i = 0; i < kOut; ++i) acc[r][i] *= f;
+        }
+    }
+    __device__ __forceinline__ void products(const KvqPage<D> (&pages)[kStepPages]) {
+        float sc[kStepPages][4];
+#pragma unroll
+        for (int pg = 0; pg < kStepPages; ++pg)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sc[pg][e] = scale_of((pages[pg].vs >> (8 * e)) & 255u);
+        two_columns<0>(pages, sc);
+        two_columns<1>(pages, sc);
+        if constexpr (D == 128) {
+            two_columns<2>(pages, sc);
+            two_columns<3>(pages, sc);
+        }
+    }
+    // columns 2 kPair and 2 kPair + 1 of every chunk
+    template <int kPair>
+    __device__ __forceinline__ void two_columns(const KvqPage<D> (&pages)[kStepPages], const float (&sc)[kStepPages][4]) {
+        u32x4 even, odd;
+#pragma unroll
+        for (int pg = 0; pg < kStepPages; ++pg) {
+            uint32_t y[4];
+            if constexpr (D == 128) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = two_values<kPair>(pages[pg].v[e], sc[pg][e]);
+            } else {
+                y[0] = two_values<kPair>(pages[pg].v[0], sc[pg][0]);
+                y[1] = two_values<2 + kPair>(pages[pg].v[0], sc[pg][1]);
+                y[2] = two_values<kPair>(pages[pg].v[1], sc[pg][2]);
+                y[3] = two_values<2 + kPair>(pages[pg].v[1], sc[pg][3]);
+            }
+            even[2 * pg] = __builtin_amdgcn_perm(y[1], y[0], 0x05040100);
+            even[2 * pg + 1] = __builtin_amdgcn_perm(y[3], y[2], 0x05040100);
+            odd[2 * pg] = __builtin_amdgcn_perm(y[1], y[0], 0x07060302);
+            odd[2 * pg + 1] = __builtin_amdgcn_perm(y[3], y[2], 0x07060302);
+        }
+#pragma unroll
+        for (int r = 0; r < kBlocks; ++r) {
+            acc[r][2 * kPair] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, even), __builtin_bit_cast(bf16x8, pk[r]), acc[r][2 * kPair], 0, 0, 0);
+            acc[r][2 * kPair + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), __builtin_bit_cast(bf16x8, pk[r]), acc[r][2 * kPair + 1], 0, 0, 0);
+        }
+    }
+    // Four output values of row i16, number n of the lane's kOut / 4 * 4 such pieces, and the piece's place among the row's D / 4.
+    __device__ __forceinline__ f32x4 piece(int r, int n) const {
+        const int k = n / (kOut / 4), h = n % (kOut / 4);
+        return f32x4{acc[r][4 * h][k], acc[r][4 * h + 1][k], acc[r][4 * h + 2][k], acc[r][4 * h + 3][k]};
+    }
+    __device__ static __forceinline__ int piece_at(int n, int quad) { return (4 * quad + n / (kOut / 4)) * (kOut / 4) + n % (kOut / 4); }
+    __device__ __forceinline__ void finish_sums() {
+#pragma unroll
+        for (int r = 0; r < kBlocks; ++r) {
+            l[r] += __shfl_xor(l[r], 16);
+            l[r] += __shfl_xor(l[r], 32);
+        }
+    }
+};
+
+// Which nodes every node of a draft tree sees: itself and its ancestors, a bit each.  By doubling the links, seven times for 128 nodes;
+// a node whose link is wrong is a root.  All threads of the workgroup; barriers at both ends.
+__device__ inline void ancestors(const int32_t *parents, int T, uint32_t (&s_mask)[READER_MAX_T][4], int (&s_up)[READER_MAX_T], int &bad) {
+    const int i = threadIdx.x;
+    uint32_t mine[4] = {};
+    int up = -1;
+    __syncthreads();
+    if (i < T) {
+        up = parents[i];
+        if (i == 0 ? up != -1 : (up < 0 || up >= i)) { up = -1; bad |= READER_STATUS_BAD_TREE; }
+        mine[i >> 5] = 1u << (i & 31);
+    }
+    for (int turn = 0; turn < 8; ++turn) {
+        if (i < T) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) s_mask[i][w] = mine[w];
+            s_up[i] = up;
+        }
+        __syncthreads();
+        if (turn == 7) break;
+        if (up >= 0) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) mine[w] |= s_mask[up][w];
+            up = s_up[up];
+        }
+        __syncthreads();
+    }
+}
+
+// A row of lse
+__device__ __forceinline__ size_t lse_at(const PromptParams &p, size_t out_row) {
+    if (p.nodes == 0) return out_row;
+    const int row = (int)(out_row / p.Hq), hq = (int)(out_row - (size_t)row * p.Hq), b = row / p.nodes;
+    return ((size_t)b * p.Hq + hq) * p.nodes + (row - b * p.nodes);
+}
+
+// A workgroup takes a range of the (head, sequence, block of query rows, key) axis; kRowWaves groups of 16 kBlocks rows, each carried
+// by kKeyWaves wavefronts that take the steps of 32 keys in turn.
+template <int D, int kBlocks, int kRowWaves, int kKeyWaves, bool kTree>
+__global__ __launch_bounds__(64 * kRowWaves * kKeyWaves) void kvq_attn_kernel(KvqAttnParams p) {
+    using Rows = KvqRows<D, kBlocks>;
+    constexpr int kWaveRows = kBlocks * 16, kRows = kWaveRows * kRowWaves, kWaves = kRowWaves * kKeyWaves;
+    constexpr int kMinRange = 2 * kStep * kKeyWaves;
+    constexpr bool kMeet = kKeyWaves > 1;
+    __shared__ __attribute__((aligned(16))) f32x4 s_part[kMeet ? kWaves : 1][kMeet ? kWaveRows * D / 4 : 1];
+    __shared__ float s_sum[kWaves][2][kWaveRows];
+    __shared__ uint32_t s_mask[kTree ? READER_MAX_T : 1][4];
+    __shared__ int s_up[kTree ? READER_MAX_T : 1];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int row_wave = wave / kKeyWaves, key_wave = wave % kKeyWaves;
+    const int i16 = lane & 15, quad = lane >> 4, tb = p.tokens_per_block;
+    RangeNote *const notes = reinterpret_cast<RangeNote *>(p.workspace);
+    const Sequences seqs{p.seq_lens, p.cu_tokens, p.N, p.max_seq_len, kTree ? p.nodes : 0};
+    int bad = 0;
+
+    // ---- this workgroup's range of the axis (every wavefront finds it for itself)
+    long long per_head = 0;
+    auto cost_up_to = [&](int base) {
+        const int b = base + lane;
+        long long c = 0;
+        if (b < p.B) {
+            c = Block::sequence_cost(seqs.length(b), seqs.tokens(b), tb);
+            if constexpr (kTree) {
+                if (p.seq_lens[b] < 0 || p.seq_lens[b] > p.max_seq_len - p.nodes) bad |= READER_STATUS_BAD_LENGTH;
+            } else bad |= bad_sequence(p, b);
+        }
+        return scan64(c);
+    };
+    const long long upto0 = cost_up_to(0);
+    per_head = lane64(upto0, 63);
+    for (int base = 64; base < p.B; base += 64) per_head += lane64(cost_up_to(base), 63);
+    if (bad && blockIdx.x == 0 && p.status) atomicOr(p.status, bad);
+    bad = 0;
+    const long long total = per_head * p.Hkv;
+    long long n_ranges = total / kMinRange;
+    n_ranges = n_ranges > (long long)gridDim.x ? gridDim.x : (n_ranges < 1 ? 1 : n_ranges);
+    const int range = blockIdx.x;
+    if (range >= n_ranges || total == 0) {
+        if (threadIdx.x == 0) notes[range] = RangeNote{};
+        return;
+    }
+    const PromptAxis axis(per_head, p.Hkv, (int)n_ranges);
+    Block place = {p.Hkv, 0, 0, 0, 0, 0};
+    int t_place = 0;
+    {
+        const long long at = axis.begin(range + (lane >> 5));
+        long long r = 0;
+        if (at < total) place.head = axis.head(at, r);
+        long long before = 0;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const long long r_half = lane64(r, 32 * half);
+            long long carry = 0, upto = upto0;
+            for (int base = 0;; base += 64) {
+                if (base > 0) upto = cost_up_to(base);
+                const long long all = carry + lane64(upto, 63);
+                if (r_half < all) {
+                    const int i = (int)__popcll(__ballot(carry + upto <= r_half));
+                    if (i > 0) carry += lane64(upto, i - 1);
+                    if ((lane >> 5) == half) place.b = base + i, before = carry;
+                    break;
+                }
+                carry = all;
+            }
+        }
+        if (at < total) {
+            place.load(seqs);
+            t_place = place.locate(r - before, seqs, p.B, tb);
+        } else place.b = 0;
+    }
+    bad = 0;
+    const PromptRange<Block> rg(place, t_place, p.Hkv);
+    const RangeNote note = rg.note(seqs, p.B, tb, lane);
+    if (threadIdx.x == 0) notes[range] = note;
+
+    Block o = rg.at;
+    for (bool first_block = true; !rg.behind(o); first_block = false) {
+        int t0, t1;
+        rg.share(o, first_block, tb, p.max_seq_len, t0, t1);
+        const int keys = o.keys(tb, p.max_seq_len), nt = o.tokens(tb), row0 = o.c0 + o.k * tb, all = o.tiles(tb, p.max_seq_len);
+        const long long p0 = (long long)o.L + o.k * tb;
+        const bool last_block = rg.is_stop(o);
+        if (t1 > t0) {
+            if constexpr (kTree) {
+                if ((long long)t1 * kStep > o.L) ancestors(p.parents + (size_t)o.b * p.nodes, p.nodes, s_mask, s_up, bad);
+            }
+            const int first = row_wave * kWaveRows;
+            // steps key_wave, key_wave + kKeyWaves, ... of the segment are this wavefront's (none, if it has no rows)
+            const int steps = first < nt * p.G ? (t1 - t0 - key_wave + kKeyWaves - 1) / kKeyWaves : 0;
+            const int32_t *table = p.page_table + (size_t)o.b * p.max_pages;
+            const int unmasked = kTree ? o.L : (int)min(p0 + 1, (long long)p.max_seq_len);     // keys that every row sees
+            // pages of step j: their ids, -1 for one that is not there (nobody sees its keys)
+            auto page_id = [&](int j, int pg) {
+                const int at = (t0 + key_wave + j * kKeyWaves) * kStepPages + pg;
+                const bool there = j < steps && at * READER_PAGE_SIZE < keys;
+                const int id = table[there ? at : 0];
+                return there && id >= 0 && id < p.num_pages ? id : -1;
+            };
+            auto load = [&](KvqPage<D> (&to)[kStepPages], const int (&id)[kStepPages]) {
+#pragma unroll
+                for (int pg = 0; pg < kStepPages; ++pg)
+                    to[pg].load(p.cache + ((size_t)max(id[pg], 0) * p.Hkv + o.head) * KvqBlock<D>::kBytes, lane, i16, quad);
+            };
+            Rows rows;
+            rows.load(p, o.head, row0, p0, o.k * tb, nt, first, i16, quad);
+            if (steps > 0) {
+                int id[kStepPages] = {page_id(0, 0), page_id(0, 1)}, id_next[kStepPages] = {page_id(1, 0), page_id(1, 1)};
+                KvqPage<D> now[kStepPages], next[kStepPages];
+                load(now, id);
+                int j = 0;
+                // (the references are moved outside the loop over the steps: a path around its accumulators inside it is paid for in every step)
+                while (true) {
+                    bool move = false;
+                    for (; j < steps; ++j) {
+                        load(next, id_next);
+                        const int id_then[kStepPages] = {page_id(j + 2, 0), page_id(j + 2, 1)};
+                        const int j0 = (t0 + key_wave + j * kKeyWaves) * kStep;
+                        rows.scores(now);
+                        if (j0 + kStep > unmasked || id[0] < 0 || id[1] < 0) {
+#pragma unroll
+                            for (int pg = 0; pg < kStepPages; ++pg) {
+                                const int jp = j0 + pg * READER_PAGE_SIZE;
+                                if (jp < keys && id[pg] < 0) bad |= READER_STATUS_BAD_PAGE;
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    const int key = jp + quad * 4 + e, n = key - o.L;
+                                    const bool nobody = id[pg] < 0 || key >= keys;
+                                    if (nobody) now[pg].drop(e);
+#pragma unroll
+                                    for (int r = 0; r < kBlocks; ++r) {
+                                        // (no branches: with them the compiler has lost the assignment on one of the ways)
+                                        bool sees = !nobody & (key < rows.lim[r]);
+                                        if constexpr (kTree) sees &= (n < 0) | ((s_mask[rows.node[r]][(n >> 5) & 3] >> (n & 31) & 1u) != 0);
+                                        rows.x[r][pg][e] = sees ? rows.x[r][pg][e] : -INFINITY;
+                                    }
+                                }
+                            }
+                        }
+                        float sum[kBlocks];
+                        if (__any(rows.weights(p.scale_log2, sum) > kMostSum)) {
+                            move = true;
+                            break;
+                        }
+#pragma unroll
+                        for (int r = 0; r < kBlocks; ++r) rows.l[r] = sum[r];
+                        rows.products(now);
+#pragma unroll
+                        for (int pg = 0; pg < kStepPages; ++pg) {
+                            now[pg] = next[pg];
+                            id[pg] = id_next[pg];
+                            id_next[pg] = id_then[pg];
+                        }
+                    }
+                    if (!move) break;
+                    rows.move_references(p.scale_log2);
+                }
+            }
+            rows.finish_sums();
+            // ---- end of the segment: the whole block is normalised and written out, a part of one leaves a record
+            const bool whole = t0 == 0 && t1 == all;
+            float *rec = reinterpret_cast<float *>(reinterpret_cast<char *>(p.workspace) + kNotesBytes) +
+                         (size_t)(2 * range + (t0 == 0 ? 1 : 0)) * ((size_t)kRows * (D + 2));
+            constexpr int kPieces = D / 16;                  // a lane's of a row
+            auto write = [&](int r, int piece, f32x4 v) {
+                const int row = first + r * 16 + i16;
+                if (!whole) reinterpret_cast<f32x4 *>(rec)[piece * kRows + row] = v;
+                else if (rows.real[r])
+                    *reinterpret_cast<uint2 *>(p.out + Rows::out_row(p, o.head, row0, nt, row) * D + piece * 4) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+            };
+            auto write_sums = [&](int r, float top, float sum) {
+                const int row = first + r * 16 + i16;
+                if (!whole) {
+                    rec[(size_t)kRows * D + row] = sum == 0.f ? -INFINITY : top;
+                    rec[(size_t)kRows * (D + 1) + row] = sum;
+                } else if (rows.real[r] && p.lse) {
+                    p.lse[lse_at(p, Rows::out_row(p, o.head, row0, nt, row))] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+                }
+            };
+            if constexpr (!kMeet) {
+#pragma unroll
+                for (int r = 0; r < kBlocks; ++r) {
+                    const float inv = rows.l[r] == 0.f ? 0.f : 1.f / rows.l[r];
+#pragma unroll
+                    for (int n = 0; n < kPieces; ++n) write(r, Rows::piece_at(n, quad), rows.piece(r, n) * inv);
+                    if (quad == 0) write_sums(r, rows.m[r], rows.l[r]);
+                }
+            } else {
+                // the wavefronts that share rows add them up: [D / 4 pieces][rows], a part of the pieces each
+#pragma unroll
+                for (int r = 0; r < kBlocks; ++r) {
+#pragma unroll
+                    for (int n = 0; n < kPieces; ++n) s_part[wave][Rows::piece_at(n, quad) * kWaveRows + r * 16 + i16] = rows.piece(r, n);
+                    if (quad == 0) { s_sum[wave][0][r * 16 + i16] = rows.m[r]; s_sum[wave][1][r * 16 + i16] = rows.l[r]; }
+                }
+                __syncthreads();
+#pragma unroll
+                for (int r = 0; r < kBlocks; ++r) {
+                    const int row = r * 16 + i16, w0 = row_wave * kKeyWaves;
+                    float top = kNoReference, sum = 0.f, f[kKeyWaves];
+#pragma unroll
+                    for (int w = 0; w < kKeyWaves; ++w) top = fmaxf(top, s_sum[w0 + w][0][row]);
+#pragma unroll
+                    for (int w = 0; w < kKeyWaves; ++w) {
+                        // (a wavefront whose rows saw nothing has no say, whatever its reference)
+                        const float lw = s_sum[w0 + w][1][row];
+                        f[w] = lw == 0.f ? 0.f : __builtin_amdgcn_exp2f(s_sum[w0 + w][0][row] - top);
+                        sum += lw * f[w];
+                    }
+                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                    constexpr int kMine = (D / 4 + 4 * kKeyWaves - 1) / (4 * kKeyWaves);
+#pragma unroll
+                    for (int c = 0; c < kMine; ++c) {
+                        const int piece = (key_wave * kMine + c) * 4 + quad;
+                        if (D / 4 % (4 * kKeyWaves) != 0 && piece >= D / 4) break;
+                        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int w = 0; w < kKeyWaves; ++w) v += s_part[w0 + w][piece * kWaveRows + row] * f[w];
+                        write(r, piece, v * inv);
+                    }
+                    if (key_wave == 0 && quad == 0) write_sums(r, top, sum);
+                }
+                __syncthreads();                             // everybody is done with the others' rows
+            }
+        }
+        if (last_block) break;
+        o.next(seqs, p.B, tb);
+        o = o.of_lane(0);
+    }
+    if (p.status && bad) atomicOr(p.status, bad);
+}
+
+template <int D, int kBlocks, int kRowWaves, int kKeyWaves>
+hipError_t launch(KvqAttnParams p, int ranges, hipStream_t stream) {
+    constexpr int kRows = 16 * kBlocks * kRowWaves;
+    p.n_ranges = ranges;
+    p.tokens_per_block = kRows / p.G;
+    const dim3 grid(ranges), block(64 * kRowWaves * kKeyWaves);
+    if (p.nodes > 0) hipLaunchKernelGGL((kvq_attn_kernel<D, kBlocks, kRowWaves, kKeyWaves, true>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((kvq_attn_kernel<D, kBlocks, kRowWaves, kKeyWaves, false>), grid, block, 0, stream, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return note_hip_error("launch kvq_attn_kernel", e);
+    return launch_prompt_merge(p, kRows, stream);
+}
+
+template <int D>
+hipError_t launch_rows(const KvqAttnParams &p, hipStream_t stream) {
+    switch (kvq_attn_rows(p)) {
+        case 16: return launch<D, 1, 1, 4>(p, 2 * kNumCU, stream);
+        case 32: return launch<D, 2, 1, 4>(p, 2 * kNumCU, stream);
+        case 64: return launch<D, 2, 2, 2>(p, kNumCU, stream);
+        default: return launch<D, 2, 4, 1>(p, kNumCU, stream);
+    }
+}
+
+}  // namespace
+
+// Query rows of a kv head that a workgroup takes: as many as a sequence has.
+int kvq_attn_rows(const KvqAttnParams &p) {
+    const int forced = tuning(READER_TUNE_PROMPT_ROWS);
+    if (forced == 16 || forced == 32 || forced == 64 || forced == 128) return forced;
+    const long long rows = ((long long)p.N + p.B - 1) / (p.B > 0 ? p.B : 1) * p.G;
+    return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+}
+
+size_t kvq_attn_workspace_bytes(int D) { return ranges_workspace_bytes(2 * kNumCU, 128, D); }
+
+hipError_t launch_kvq_attn(const KvqAttnParams &p, hipStream_t stream) {
+    return p.D == 64 ? launch_rows<64>(p, stream) : launch_rows<128>(p, stream);
+}
+
+}  // namespace reader

@@ -61,6 +61,7 @@ struct PromptParams {
     float g_rcp;                   // 1 / G
     int32_t tokens_per_block;      // (matrix kernels) tokens whose heads fill a block of query rows
     int32_t n_ranges;              // ... and workgroups of the launch
+    int32_t nodes;                 // > 0: rows are draft trees of as many nodes, lse is [B, Hq, nodes]
 };
 // What the attention finds wrong with sequence b, whichever kernel runs: its bounds, its length, or keys beyond the bound on them.
 __device__ inline int bad_sequence(const PromptParams &p, int b) {

@@ -111,7 +111,14 @@ __global__ __launch_bounds__(64 * kMergeWaves) void prompt_merge_kernel(PromptPa
         *reinterpret_cast<uint4 *>(out + c * 4) =
             make_uint4(pack_bf16x2(acc[c].x * inv, acc[c].y * inv), pack_bf16x2(acc[c].z * inv, acc[c].w * inv),
                        pack_bf16x2(acc[c + 1].x * inv, acc[c + 1].y * inv), pack_bf16x2(acc[c + 1].z * inv, acc[c + 1].w * inv));
-    if (quad == 0 && p.lse) p.lse[out_row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    if (quad == 0 && p.lse) {
+        size_t at = out_row;
+        if (p.nodes > 0) {
+            const int t = mine.row0 + tok, b = t / p.nodes;
+            at = ((size_t)b * p.Hq + mine.head * p.G + g) * p.nodes + (t - b * p.nodes);
+        }
+        p.lse[at] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    }
 }
 
 }  // namespace

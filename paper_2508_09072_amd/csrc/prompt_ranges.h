@@ -45,10 +45,11 @@ __device__ __forceinline__ long long lane64(long long v, int lane) {
 struct Sequences {
     const int32_t *lens, *cu;
     int N, max_len;
+    int nodes = 0;        // > 0: draft trees, each sequence has as many rows (cu is not read), behind which max_len leaves room for them
     // (rows behind the bound on the lengths see what lies in front of it)
-    __device__ __forceinline__ int length(int b) const { return min(max(lens[b], 0), max_len); }
-    __device__ __forceinline__ int first(int b) const { return clamp_row(cu[b], N); }
-    __device__ __forceinline__ int tokens(int b) const { return max(clamp_row(cu[b + 1], N) - first(b), 0); }
+    __device__ __forceinline__ int length(int b) const { return min(max(lens[b], 0), max_len - nodes); }
+    __device__ __forceinline__ int first(int b) const { return nodes > 0 ? b * nodes : clamp_row(cu[b], N); }
+    __device__ __forceinline__ int tokens(int b) const { return nodes > 0 ? nodes : max(clamp_row(cu[b + 1], N) - first(b), 0); }
 };
 
 // A block of query rows: `tb` tokens of a sequence (the last one of it: what is left) with all query heads of a kv head.  On the

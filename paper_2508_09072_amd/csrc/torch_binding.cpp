@@ -37,6 +37,8 @@ struct Api {
     X(reader_kv_rearrange) X(reader_target_argmax) X(reader_target_sample) X(reader_kv_compact_layers)               \
     X(reader_tree_qkv) X(reader_prompt_qkv) X(reader_prompt_attn) X(reader_key_weights) X(reader_prompt_key_weights)  \
     X(reader_kv_evict)                                                                                               \
+    X(reader_kvq_store) X(reader_kvq_pack) X(reader_kvq_compact_layers) X(reader_kvq_tree_attn)                       \
+    X(reader_kvq_prompt_attn) X(reader_pages_reorder) X(reader_pages_reserve)                                         \
     X(reader_trie_insert) X(reader_trie_search_path) X(reader_trie_extract_tree) X(reader_tree_attach_path)
     READER_FNS(READER_FN)
 #undef READER_FN
@@ -560,6 +562,175 @@ PyObject *py_kv_evict(PyObject *const *args, Py_ssize_t n) {
     });
 }
 
+// ------------------------------------------------------------------ the cache in 4 bits, and pages
+
+PyObject *py_kvq_store(PyObject *const *args, Py_ssize_t n) {
+    Args a(args, n, 8);
+    const reader_dims *d = a.dims();
+    const at::Tensor *k = a.tensor(kBf16);
+    if (!a.ok()) return nullptr;
+    const int64_t B = d->B, T = d->T, Hkv = d->Hkv, D = d->D;
+    const bool tree = k->dim() == 4;
+    const int64_t N = tree ? B * T : a.size(k, 0, "k");
+    if (tree ? k->sizes() != at::IntArrayRef({B, T, Hkv, D}) : k->sizes() != at::IntArrayRef({N, Hkv, D}))
+        a.reject(PyExc_ValueError, "k must be [N, Hkv, D] or [B, T, Hkv, D]");
+    const at::Tensor *v = tree ? a.shaped(kBf16, {B, T, Hkv, D}, "v") : a.shaped(kBf16, {N, Hkv, D}, "v");
+    const at::Tensor *cu = a.shaped(kI32, {B + 1}, "cu_tokens", true), *lens = a.shaped(kI32, {B}, "seq_lens");
+    const at::Tensor *cache = a.shaped(kU8, {d->num_pages, Hkv, READER_KVQ_BLOCK_BYTES(D)}, "kvq_cache");
+    const at::Tensor *table = a.shaped(kI32, {B, d->max_pages_per_seq}, "page_table");
+    int32_t *status = a.i32_out(true);
+    a.on_current_device();
+    if (a.ok() && tree != (cu == nullptr)) a.reject(PyExc_ValueError, "rows of draft trees have no cu_tokens, packed rows have");
+    if (a.ok() && N > INT32_MAX) a.reject(PyExc_ValueError, "more rows than 32 bits hold");
+    if (!a.ok()) return nullptr;
+    void *st = stream();
+    return unlocked([&] {
+        return api.reader_kvq_store(d, (int32_t)N, data<void>(k), data<void>(v), data<int32_t>(cu), data<int32_t>(lens), data<void>(cache),
+                                    data<int32_t>(table), status, st);
+    });
+}
+
+PyObject *py_kvq_pack(PyObject *const *args, Py_ssize_t n) {
+    Args a(args, n, 10);
+    const reader_dims *d = a.dims();
+    const at::Tensor *k = a.tensor(kBf16);
+    a.want_dims(k, 5, "k_cache");
+    if (!a.ok()) return nullptr;
+    const int64_t NL = k->size(0), from_pages = k->size(1), B = d->B, Hkv = d->Hkv, D = d->D;
+    if (k->sizes() != at::IntArrayRef({NL, from_pages, Hkv, (int64_t)d->page_size, D}))
+        a.reject(PyExc_ValueError, "k_cache must be [num_layers, from_pages, Hkv, page_size, D]");
+    const at::Tensor *v = a.shaped(kBf16, {NL, from_pages, Hkv, d->page_size, D}, "v_cache");
+    const at::Tensor *from = a.shaped(kI32, {B, d->max_pages_per_seq}, "from_table"), *starts = a.shaped(kI32, {B}, "starts", true);
+    const at::Tensor *lens = a.shaped(kI32, {B}, "seq_lens");
+    const int32_t max_len = a.integer();
+    const at::Tensor *cache = a.shaped(kU8, {NL, d->num_pages, Hkv, READER_KVQ_BLOCK_BYTES(D)}, "kvq_cache");
+    const at::Tensor *table = a.shaped(kI32, {B, d->max_pages_per_seq}, "page_table");
+    int32_t *status = a.i32_out(true);
+    a.on_current_device();
+    const int32_t layers = a.size(k, 0, "k_cache");
+    if (!a.ok()) return nullptr;
+    void *st = stream();
+    return unlocked([&] {
+        return api.reader_kvq_pack(d, layers, data<void>(k), data<void>(v), from_pages, data<int32_t>(from), data<int32_t>(starts),
+                                   data<int32_t>(lens), max_len, data<void>(cache), data<int32_t>(table), status, st);
+    });
+}
+
+PyObject *py_kvq_compact_layers(PyObject *const *args, Py_ssize_t n) {
+    Args a(args, n, 7);
+    const reader_dims *d = a.dims();
+    if (!d) return nullptr;
+    const int64_t B = d->B;
+    const at::Tensor *path = a.shaped(kI32, {B, d->max_path}, "path"), *len = a.shaped(kI32, {B}, "accept_len");
+    const at::Tensor *cache = a.tensor(kU8);
+    a.want_dims(cache, 4, "kvq_cache");
+    if (!a.ok()) return nullptr;
+    if (cache->sizes() != at::IntArrayRef({cache->size(0), d->num_pages, (int64_t)d->Hkv, (int64_t)READER_KVQ_BLOCK_BYTES(d->D)}))
+        a.reject(PyExc_ValueError, "kvq_cache must be [num_layers, num_pages, Hkv, 17 D]");
+    const at::Tensor *table = a.shaped(kI32, {B, d->max_pages_per_seq}, "page_table"), *lens = a.shaped(kI32, {B}, "seq_lens");
+    int32_t *status = a.i32_out(true);
+    a.on_current_device();
+    const int32_t layers = a.size(cache, 0, "kvq_cache");
+    if (!a.ok()) return nullptr;
+    void *st = stream();
+    return unlocked([&] {
+        return api.reader_kvq_compact_layers(d, layers, data<int32_t>(path), data<int32_t>(len), data<void>(cache), data<int32_t>(table),
+                                             data<int32_t>(lens), status, st);
+    });
+}
+
+PyObject *py_kvq_tree_attn(PyObject *const *args, Py_ssize_t n) {
+    Args a(args, n, 11);
+    const reader_dims *d = a.dims();
+    if (!d) return nullptr;
+    const int64_t B = d->B, T = d->T, Hq = d->Hq, D = d->D;
+    const at::Tensor *q = a.shaped(kBf16, {B, T, Hq, D}, "q");
+    const at::Tensor *cache = a.shaped(kU8, {d->num_pages, d->Hkv, READER_KVQ_BLOCK_BYTES(D)}, "kvq_cache");
+    const at::Tensor *table = a.shaped(kI32, {B, d->max_pages_per_seq}, "page_table"), *lens = a.shaped(kI32, {B}, "seq_lens");
+    const at::Tensor *parents = a.shaped(kI32, {B, T}, "parents");
+    const at::Tensor *out = a.shaped(kBf16, {B, T, Hq, D}, "out"), *lse = a.shaped(kF32, {B, Hq, T}, "lse", true);
+    const int32_t max_len = a.integer();
+    const at::Tensor *ws = a.tensor(kAny, true);
+    int32_t *status = a.i32_out(true);
+    a.on_current_device();
+    if (!a.ok()) return nullptr;
+    void *st = stream();
+    const size_t ws_bytes = ws ? ws->nbytes() : 0;
+    return unlocked([&] {
+        return api.reader_kvq_tree_attn(d, data<void>(q), data<void>(cache), data<int32_t>(table), data<int32_t>(lens), data<int32_t>(parents),
+                                        data<void>(out), data<float>(lse), max_len, data<void>(ws), ws_bytes, status, st);
+    });
+}
+
+PyObject *py_kvq_prompt_attn(PyObject *const *args, Py_ssize_t n) {
+    Args a(args, n, 11);
+    const reader_dims *d = a.dims();
+    const at::Tensor *q = a.tensor(kBf16);
+    a.want_dims(q, 3, "q");
+    const int64_t N = a.size(q, 0, "q");
+    if (!a.ok()) return nullptr;
+    const int64_t B = d->B, Hq = d->Hq, D = d->D;
+    if (q->size(1) != Hq || q->size(2) != D) a.reject(PyExc_ValueError, "q must be [N, Hq, D]");
+    const at::Tensor *cache = a.shaped(kU8, {d->num_pages, d->Hkv, READER_KVQ_BLOCK_BYTES(D)}, "kvq_cache");
+    const at::Tensor *table = a.shaped(kI32, {B, d->max_pages_per_seq}, "page_table");
+    const at::Tensor *cu = a.shaped(kI32, {B + 1}, "cu_tokens"), *lens = a.shaped(kI32, {B}, "seq_lens");
+    const at::Tensor *out = a.shaped(kBf16, {N, Hq, D}, "out"), *lse = a.shaped(kF32, {N, Hq}, "lse", true);
+    const int32_t max_len = a.integer();
+    const at::Tensor *ws = a.tensor(kAny, true);
+    int32_t *status = a.i32_out(true);
+    a.on_current_device();
+    if (!a.ok()) return nullptr;
+    void *st = stream();
+    const size_t ws_bytes = ws ? ws->nbytes() : 0;
+    return unlocked([&] {
+        return api.reader_kvq_prompt_attn(d, (int32_t)N, data<void>(q), data<void>(cache), data<int32_t>(table), data<int32_t>(cu),
+                                          data<int32_t>(lens), data<void>(out), data<float>(lse), max_len, data<void>(ws), ws_bytes, status, st);
+    });
+}
+
+PyObject *py_pages_reorder(PyObject *const *args, Py_ssize_t n) {
+    Args a(args, n, 7);
+    const reader_dims *d = a.dims();
+    if (!d) return nullptr;
+    const int64_t B = d->B;
+    const at::Tensor *sources = a.shaped(kI32, {B}, "sources"), *table = a.shaped(kI32, {B, d->max_pages_per_seq}, "page_table");
+    const at::Tensor *lens = a.shaped(kI32, {B}, "seq_lens"), *refs = a.shaped(kI32, {d->num_pages}, "page_refs"), *ws = a.tensor(kAny, true);
+    int32_t *status = a.i32_out(true);
+    a.on_current_device();
+    if (!a.ok()) return nullptr;
+    void *st = stream();
+    const size_t ws_bytes = ws ? ws->nbytes() : 0;
+    return unlocked([&] {
+        return api.reader_pages_reorder(d, data<int32_t>(sources), data<int32_t>(table), data<int32_t>(lens), data<int32_t>(refs), data<void>(ws),
+                                        ws_bytes, status, st);
+    });
+}
+
+PyObject *py_pages_reserve(PyObject *const *args, Py_ssize_t n) {
+    Args a(args, n, 9);
+    const reader_dims *d = a.dims();
+    if (!d) return nullptr;
+    const int64_t B = d->B;
+    const at::Tensor *lens = a.shaped(kI32, {B}, "seq_lens"), *wanted = a.shaped(kI32, {B}, "new_lens");
+    const at::Tensor *k = a.tensor(kAny, true), *v = a.tensor(kAny, true);
+    const at::Tensor *table = a.shaped(kI32, {B, d->max_pages_per_seq}, "page_table");
+    const at::Tensor *refs = a.shaped(kI32, {d->num_pages}, "page_refs"), *ws = a.tensor(kAny, true);
+    int32_t *status = a.i32_out(true);
+    a.on_current_device();
+    if (a.ok() && k && (k->dim() < 2 || k->size(1) != d->num_pages)) a.reject(PyExc_ValueError, "k_cache must be [num_layers, num_pages, ...]");
+    if (a.ok() && v && (!k || v->sizes() != k->sizes() || v->scalar_type() != k->scalar_type()))
+        a.reject(PyExc_ValueError, "v_cache must be like k_cache");
+    const int32_t layers = k ? a.size(k, 0, "k_cache") : 0;
+    if (!a.ok()) return nullptr;
+    const int64_t pages = (int64_t)layers * d->num_pages, page_bytes = pages > 0 ? (int64_t)k->nbytes() / pages : 0;
+    void *st = stream();
+    const size_t ws_bytes = ws ? ws->nbytes() : 0;
+    return unlocked([&] {
+        return api.reader_pages_reserve(d, layers, page_bytes, data<int32_t>(lens), data<int32_t>(wanted), data<void>(k), data<void>(v),
+                                        data<int32_t>(table), data<int32_t>(refs), data<void>(ws), ws_bytes, status, st);
+    });
+}
+
 // ------------------------------------------------------------------ the host-side drafter (numpy arrays)
 
 // Whole numbers as a C-contiguous int32 array: the object itself if it is one, else a converted copy.
@@ -673,7 +844,9 @@ PyMethodDef methods[] = {
     READER_FAST(tree_attn), READER_FAST(tree_attn_noalloc), READER_FAST(accept_path), READER_FAST(kv_compact),
     READER_FAST(verify_step), READER_FAST(kv_rearrange), READER_FAST(target_argmax), READER_FAST(target_sample),
     READER_FAST(kv_compact_layers), READER_FAST(tree_qkv), READER_FAST(prompt_qkv), READER_FAST(prompt_attn),
-    READER_FAST(key_weights), READER_FAST(prompt_key_weights), READER_FAST(kv_evict), READER_FAST(trie_insert), READER_FAST(trie_search_path), READER_FAST(trie_extract_tree),
+    READER_FAST(key_weights), READER_FAST(prompt_key_weights), READER_FAST(kv_evict),
+    READER_FAST(kvq_store), READER_FAST(kvq_pack), READER_FAST(kvq_compact_layers), READER_FAST(kvq_tree_attn), READER_FAST(kvq_prompt_attn),
+    READER_FAST(pages_reorder), READER_FAST(pages_reserve), READER_FAST(trie_insert), READER_FAST(trie_search_path), READER_FAST(trie_extract_tree),
     READER_FAST(tree_attach_path), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_reader_torch", "torch and numpy arguments of the reader C ABI", -1, methods,
