@@ -26,7 +26,7 @@ NATIVE = os.path.join(HERE, "_reader_torch.so")
 SOURCES = ["reader_api.hip", "trie_drafter.cpp", "tree_shape.cpp", "accept_compact.hip", "kv_compact_layers.hip", "kv_rearrange.hip", "target_argmax.hip", "target_sample.hip", "tree_attn_scalar.hip", "tree_attn_mfma.hip", "tree_attn_wide.hip", "tree_attn_short.hip", "peak_probes.hip",
            "prompt_api.hip", "qkv_prepare.hip", "prompt_attn.hip", "prompt_attn_mid.hip", "prompt_attn_few.hip", "prompt_merge.hip",
            "prompt_attn_scalar.hip", "key_weights.hip", "kv_evict.hip", "kvq_api.hip",
-           "kvq_store.hip", "kvq_attn.hip", "pages.hip"]
+           "kvq_store.hip", "kvq_attn.hip", "kvq_attn_wide.hip", "pages.hip"]
 # sources compiled at a time
 JOBS = 6
 # kernels that manage the accumulation registers by hand

@@ -1,0 +1,118 @@
+// What the kernels of the attention over the cache in 4 bits share (kvq_attn.hip, kvq_attn_wide.hip).
+#pragma once
+
+#include "kvq_common.h"
+#include "prompt_rows.h"
+#include "tree_attn_common.h"
+
+namespace reader {
+
+namespace {
+
+constexpr float kMostSum = 0x1p16f;                  // of a lane's part of a row's sum, before its reference moves
+
+// Two codes of byte `kByte` of a word, times 2^(scale - 127) in the exponent bits of `scale`: exact.
+template <int kByte>
+__device__ __forceinline__ uint32_t two_values(uint32_t word, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, kByte));
+}
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Which nodes every node of a draft tree sees: itself and its ancestors, a bit each.  By doubling the links, seven times for 128 nodes;
+// a node whose link is wrong is a root.  All threads of the workgroup; barriers at both ends.
+__device__ inline void ancestors(const int32_t *parents, int T, uint32_t (&s_mask)[READER_MAX_T][4], int (&s_up)[READER_MAX_T], int &bad) {
+    const int i = threadIdx.x;
+    uint32_t mine[4] = {};
+    int up = -1;
+    __syncthreads();
+    if (i < T) {
+        up = parents[i];
+        if (i == 0 ? up != -1 : (up < 0 || up >= i)) { up = -1; bad |= READER_STATUS_BAD_TREE; }
+        mine[i >> 5] = 1u << (i & 31);
+    }
+    for (int turn = 0; turn < 8; ++turn) {
+        if (i < T) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) s_mask[i][w] = mine[w];
+            s_up[i] = up;
+        }
+        __syncthreads();
+        if (turn == 7) break;
+        if (up >= 0) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) mine[w] |= s_mask[up][w];
+            up = s_up[up];
+        }
+        __syncthreads();
+    }
+}
+
+// A row of lse
+__device__ __forceinline__ size_t lse_at(const PromptParams &p, size_t out_row) {
+    if (p.nodes == 0) return out_row;
+    const int row = (int)(out_row / p.Hq), hq = (int)(out_row - (size_t)row * p.Hq), b = row / p.nodes;
+    return ((size_t)b * p.Hq + hq) * p.nodes + (row - b * p.nodes);
+}
+
+// This workgroup's range of the (head, sequence, block, key) axis, found by every wavefront for itself: false if there is none.  Its
+// note is written, and what the first workgroup finds wrong with lengths and bounds.
+template <class Block, int kMinRange, bool kTree>
+__device__ __forceinline__ bool find_range(const KvqAttnParams &p, const Sequences &seqs, int lane, Block &place, int &t_place) {
+    RangeNote *const notes = reinterpret_cast<RangeNote *>(p.workspace);
+    const int tb = p.tokens_per_block;
+    int bad = 0;
+    auto cost_up_to = [&](int base) {                    // of sequences `base` .. base + lane
+        const int b = base + lane;
+        long long c = 0;
+        if (b < p.B) {
+            c = Block::sequence_cost(seqs.length(b), seqs.tokens(b), tb);
+            if constexpr (kTree) {
+                if (p.seq_lens[b] < 0 || p.seq_lens[b] > p.max_seq_len - p.nodes) bad |= READER_STATUS_BAD_LENGTH;
+            } else bad |= bad_sequence(p, b);
+        }
+        return scan64(c);
+    };
+    const long long upto0 = cost_up_to(0);
+    long long per_head = lane64(upto0, 63);
+    for (int base = 64; base < p.B; base += 64) per_head += lane64(cost_up_to(base), 63);
+    if (bad && blockIdx.x == 0 && p.status) atomicOr(p.status, bad);
+    const long long total = per_head * p.Hkv;
+    long long n_ranges = total / kMinRange;
+    n_ranges = n_ranges > (long long)gridDim.x ? gridDim.x : (n_ranges < 1 ? 1 : n_ranges);
+    const int range = blockIdx.x;
+    if (range >= n_ranges || total == 0) {
+        if (threadIdx.x == 0) notes[range] = RangeNote{};
+        return false;
+    }
+    const PromptAxis axis(per_head, p.Hkv, (int)n_ranges);
+    place = Block{p.Hkv, 0, 0, 0, 0, 0};
+    t_place = 0;
+    const long long at = axis.begin(range + (lane >> 5));
+    long long r = 0, before = 0;
+    if (at < total) place.head = axis.head(at, r);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const long long r_half = lane64(r, 32 * half);
+        long long carry = 0, upto = upto0;
+        for (int base = 0;; base += 64) {
+            if (base > 0) upto = cost_up_to(base);
+            const long long all = carry + lane64(upto, 63);
+            if (r_half < all) {                          // (the last of these 64 at the latest: r is below per_head)
+                const int i = (int)__popcll(__ballot(carry + upto <= r_half));
+                if (i > 0) carry += lane64(upto, i - 1);
+                if ((lane >> 5) == half) place.b = base + i, before = carry;
+                break;
+            }
+            carry = all;
+        }
+    }
+    if (at < total) {
+        place.load(seqs);
+        t_place = place.locate(r - before, seqs, p.B, tb);
+    } else place.b = 0;
+    return true;
+}
+
+}  // namespace
+
+}  // namespace reader

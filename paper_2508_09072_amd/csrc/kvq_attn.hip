@@ -1,26 +1,12 @@
 // Attention over a cache in 4 bits, of packed prompts, chunks and single tokens (causal) and of draft trees whose rows are in the
 // cache behind their sequence (ancestors only).
-#include "kvq_common.h"
-#include "prompt_ranges.h"
-#include "tree_attn_common.h"
+#include "kvq_attn.h"
 
 namespace reader {
 
 namespace {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-constexpr int kStep = 32, kStepPages = kStep / READER_PAGE_SIZE;
-constexpr float kNoReference = -1e30f;               // of a row that has seen no key
-constexpr float kMostSum = 0x1p16f;                  // ... of a lane's part of a row's sum, before its reference moves
 using Block = PromptBlock<kStep, 2 * kStep, 4 * kStep>;
-
-// Two codes of byte `kByte` of a word, times 2^(scale - 127) in the exponent bits of `scale`: exact.
-template <int kByte>
-__device__ __forceinline__ uint32_t two_values(uint32_t word, float scale) {
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, kByte));
-}
-__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
 // One lane's bytes of a page: K of row i16 and quarter `quad`, V of rows 4 quad .. + 3 and chunk i16.
 template <int D>
@@ -183,42 +169,6 @@ struct KvqRows {
     }
 };
 
-// Which nodes every node of a draft tree sees: itself and its ancestors, a bit each.  By doubling the links, seven times for 128 nodes;
-// a node whose link is wrong is a root.  All threads of the workgroup; barriers at both ends.
-__device__ inline void ancestors(const int32_t *parents, int T, uint32_t (&s_mask)[READER_MAX_T][4], int (&s_up)[READER_MAX_T], int &bad) {
-    const int i = threadIdx.x;
-    uint32_t mine[4] = {};
-    int up = -1;
-    __syncthreads();
-    if (i < T) {
-        up = parents[i];
-        if (i == 0 ? up != -1 : (up < 0 || up >= i)) { up = -1; bad |= READER_STATUS_BAD_TREE; }
-        mine[i >> 5] = 1u << (i & 31);
-    }
-    for (int turn = 0; turn < 8; ++turn) {
-        if (i < T) {
-#pragma unroll
-            for (int w = 0; w < 4; ++w) s_mask[i][w] = mine[w];
-            s_up[i] = up;
-        }
-        __syncthreads();
-        if (turn == 7) break;
-        if (up >= 0) {
-#pragma unroll
-            for (int w = 0; w < 4; ++w) mine[w] |= s_mask[up][w];
-            up = s_up[up];
-        }
-        __syncthreads();
-    }
-}
-
-// A row of lse
-__device__ __forceinline__ size_t lse_at(const PromptParams &p, size_t out_row) {
-    if (p.nodes == 0) return out_row;
-    const int row = (int)(out_row / p.Hq), hq = (int)(out_row - (size_t)row * p.Hq), b = row / p.nodes;
-    return ((size_t)b * p.Hq + hq) * p.nodes + (row - b * p.nodes);
-}
-
 // A workgroup takes a range of the (head, sequence, block of query rows, key) axis; kRowWaves groups of 16 kBlocks rows, each carried
 // by kKeyWaves wavefronts that take the steps of 32 keys in turn.
 template <int D, int kBlocks, int kRowWaves, int kKeyWaves, bool kTree>
@@ -236,67 +186,14 @@ __global__ __launch_bounds__(64 * kRowWaves * kKeyWaves) void kvq_attn_kernel(Kv
     const int i16 = lane & 15, quad = lane >> 4, tb = p.tokens_per_block;
     RangeNote *const notes = reinterpret_cast<RangeNote *>(p.workspace);
     const Sequences seqs{p.seq_lens, p.cu_tokens, p.N, p.max_seq_len, kTree ? p.nodes : 0};
-    int bad = 0;
-
-    // ---- this workgroup's range of the axis (every wavefront finds it for itself)
-    long long per_head = 0;
-    auto cost_up_to = [&](int base) {
-        const int b = base + lane;
-        long long c = 0;
-        if (b < p.B) {
-            c = Block::sequence_cost(seqs.length(b), seqs.tokens(b), tb);
-            if constexpr (kTree) {
-                if (p.seq_lens[b] < 0 || p.seq_lens[b] > p.max_seq_len - p.nodes) bad |= READER_STATUS_BAD_LENGTH;
-            } else bad |= bad_sequence(p, b);
-        }
-        return scan64(c);
-    };
-    const long long upto0 = cost_up_to(0);
-    per_head = lane64(upto0, 63);
-    for (int base = 64; base < p.B; base += 64) per_head += lane64(cost_up_to(base), 63);
-    if (bad && blockIdx.x == 0 && p.status) atomicOr(p.status, bad);
-    bad = 0;
-    const long long total = per_head * p.Hkv;
-    long long n_ranges = total / kMinRange;
-    n_ranges = n_ranges > (long long)gridDim.x ? gridDim.x : (n_ranges < 1 ? 1 : n_ranges);
     const int range = blockIdx.x;
-    if (range >= n_ranges || total == 0) {
-        if (threadIdx.x == 0) notes[range] = RangeNote{};
-        return;
-    }
-    const PromptAxis axis(per_head, p.Hkv, (int)n_ranges);
-    Block place = {p.Hkv, 0, 0, 0, 0, 0};
-    int t_place = 0;
-    {
-        const long long at = axis.begin(range + (lane >> 5));
-        long long r = 0;
-        if (at < total) place.head = axis.head(at, r);
-        long long before = 0;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const long long r_half = lane64(r, 32 * half);
-            long long carry = 0, upto = upto0;
-            for (int base = 0;; base += 64) {
-                if (base > 0) upto = cost_up_to(base);
-                const long long all = carry + lane64(upto, 63);
-                if (r_half < all) {
-                    const int i = (int)__popcll(__ballot(carry + upto <= r_half));
-                    if (i > 0) carry += lane64(upto, i - 1);
-                    if ((lane >> 5) == half) place.b = base + i, before = carry;
-                    break;
-                }
-                carry = all;
-            }
-        }
-        if (at < total) {
-            place.load(seqs);
-            t_place = place.locate(r - before, seqs, p.B, tb);
-        } else place.b = 0;
-    }
-    bad = 0;
+    Block place;
+    int t_place;
+    if (!find_range<Block, kMinRange, kTree>(p, seqs, lane, place, t_place)) return;
     const PromptRange<Block> rg(place, t_place, p.Hkv);
     const RangeNote note = rg.note(seqs, p.B, tb, lane);
     if (threadIdx.x == 0) notes[range] = note;
+    int bad = 0;
 
     Block o = rg.at;
     for (bool first_block = true; !rg.behind(o); first_block = false) {
@@ -473,7 +370,7 @@ hipError_t launch_rows(const KvqAttnParams &p, hipStream_t stream) {
         case 16: return launch<D, 1, 1, 4>(p, 2 * kNumCU, stream);
         case 32: return launch<D, 2, 1, 4>(p, 2 * kNumCU, stream);
         case 64: return launch<D, 2, 2, 2>(p, kNumCU, stream);
-        default: return launch<D, 2, 4, 1>(p, kNumCU, stream);
+        default: return launch_kvq_attn_wide(p, kvq_attn_rows(p), stream);
     }
 }
 
@@ -482,12 +379,12 @@ hipError_t launch_rows(const KvqAttnParams &p, hipStream_t stream) {
 // Query rows of a kv head that a workgroup takes: as many as a sequence has.
 int kvq_attn_rows(const KvqAttnParams &p) {
     const int forced = tuning(READER_TUNE_PROMPT_ROWS);
-    if (forced == 16 || forced == 32 || forced == 64 || forced == 128) return forced;
+    if (forced == 16 || forced == 32 || forced == 64 || forced == 128 || forced == 256) return forced;
     const long long rows = ((long long)p.N + p.B - 1) / (p.B > 0 ? p.B : 1) * p.G;
-    return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+    return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
 }
 
-size_t kvq_attn_workspace_bytes(int D) { return ranges_workspace_bytes(2 * kNumCU, 128, D); }
+size_t kvq_attn_workspace_bytes(int D) { return ranges_workspace_bytes(kNumCU, 256, D); }
 
 hipError_t launch_kvq_attn(const KvqAttnParams &p, hipStream_t stream) {
     return p.D == 64 ? launch_rows<64>(p, stream) : launch_rows<128>(p, stream);

@@ -58,6 +58,7 @@ struct KvqAttnParams : PromptParams {      // (k_cache and v_cache are not used;
 size_t kvq_attn_workspace_bytes(int D);
 int kvq_attn_rows(const KvqAttnParams &p);
 hipError_t launch_kvq_attn(const KvqAttnParams &p, hipStream_t stream);
+hipError_t launch_kvq_attn_wide(const KvqAttnParams &p, int rows, hipStream_t stream);    // 128 or 256 rows a workgroup
 
 struct PagesParams {
     const int32_t *sources;        // (reorder) [B]
