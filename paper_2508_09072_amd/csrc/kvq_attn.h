@@ -21,7 +21,8 @@ __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_floa
 // Which nodes every node of a draft tree sees: itself and its ancestors, a bit each.  By doubling the links, seven times for 128 nodes;
 // a node whose link is wrong is a root.  All threads of the workgroup; barriers at both ends.
 __device__ inline void ancestors(const int32_t *parents, int T, uint32_t (&s_mask)[READER_MAX_T][4], int (&s_up)[READER_MAX_T], int &bad) {
-    const int i = threadIdx.x;
+    int i = threadIdx.x;
+    asm("" : "+v"(i));                                   // (nothing here is worth a register outside)
     uint32_t mine[4] = {};
     int up = -1;
     __syncthreads();
@@ -30,6 +31,7 @@ __device__ inline void ancestors(const int32_t *parents, int T, uint32_t (&s_mas
         if (i == 0 ? up != -1 : (up < 0 || up >= i)) { up = -1; bad |= READER_STATUS_BAD_TREE; }
         mine[i >> 5] = 1u << (i & 31);
     }
+#pragma unroll 1
     for (int turn = 0; turn < 8; ++turn) {
         if (i < T) {
 #pragma unroll
