@@ -49,11 +49,9 @@ __device__ inline void ancestors(const int32_t *parents, int T, uint32_t (&s_mas
     }
 }
 
-// A row of lse
-__device__ __forceinline__ size_t lse_at(const PromptParams &p, size_t out_row) {
-    if (p.nodes == 0) return out_row;
-    const int row = (int)(out_row / p.Hq), hq = (int)(out_row - (size_t)row * p.Hq), b = row / p.nodes;
-    return ((size_t)b * p.Hq + hq) * p.nodes + (row - b * p.nodes);
+// Where the log-sum-exp of token `tok` of a block goes that starts at packed row row0, and at node node0 of sequence b.
+__device__ __forceinline__ size_t lse_at(const PromptParams &p, int b, int row0, int node0, int tok, int hq) {
+    return p.nodes == 0 ? ((size_t)row0 + tok) * p.Hq + hq : ((size_t)b * p.Hq + hq) * p.nodes + node0 + tok;
 }
 
 // This workgroup's range of the (head, sequence, block, key) axis, found by every wavefront for itself: false if there is none.  Its

@@ -295,7 +295,8 @@ __global__ __launch_bounds__(64 * kRowWaves * kKeyWaves) void kvq_attn_kernel(Kv
                     rec[(size_t)kRows * D + row] = sum == 0.f ? -INFINITY : top;
                     rec[(size_t)kRows * (D + 1) + row] = sum;
                 } else if (rows.real[r] && p.lse) {
-                    p.lse[lse_at(p, Rows::out_row(p, o.head, row0, nt, row))] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+                    const int tok = (int)(((float)row + 0.5f) * p.g_rcp);
+                    p.lse[lse_at(p, o.b, row0, o.k * tb, tok, o.head * p.G + row - tok * p.G)] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
                 }
             };
             if constexpr (!kMeet) {

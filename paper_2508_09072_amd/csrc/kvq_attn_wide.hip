@@ -19,8 +19,8 @@ template <int D>
 struct WideLayout {
     static constexpr int kFrag = 1024;                                            // an operand: 16 bytes a lane
     static constexpr int kFrags = D / 16;                                         // of K in a step, and of V
-    static constexpr int kStepBytes = 2 * kFrags * kFrag, kBuffers = 3;
-    static constexpr int kCodes = kStepPages * 16 * D, kRaw = kCodes + 256;       // codes of two pages, their scales (D bytes each)
+    static constexpr int kHalfBytes = kFrags * kFrag;                             // of K, of V
+    static constexpr int kCodes = kStepPages * 16 * D, kRaw = kCodes + 2 * D;     // codes of two pages, their scales
     static constexpr int kSlots = 6, kDepth = 3;                                  // raw steps in the ring; asked for as many steps before they are used
 };
 
@@ -122,16 +122,16 @@ struct Part {
             v[0] = c.x; v[1] = c.y;
         }
     }
-    __device__ __forceinline__ void write(char *to, int part, int i16, int quad) const {
+    __device__ __forceinline__ void write(char *k_to, char *v_to, int part, int i16, int quad) const {
         const int pg = part / kWords, w = part % kWords;
         const float sc = scale_of(ks);
-        *reinterpret_cast<u32x4 *>(to + ((quad >> 1) * kWords + w) * W::kFrag + (pg * 16 + i16 + 32 * (quad & 1)) * 16) =
+        *reinterpret_cast<u32x4 *>(k_to + ((quad >> 1) * kWords + w) * W::kFrag + (pg * 16 + i16 + 32 * (quad & 1)) * 16) =
             u32x4{two_values<0>(k, sc), two_values<1>(k, sc), two_values<2>(k, sc), two_values<3>(k, sc)};
         uint32_t y[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) y[e] = two_values<0>((D == 128 ? v[e] : v[e / 2] >> (e % 2 * 16)) >> (8 * w), scale_of(vs >> (8 * e) & 255u));
         // (keys 4 quad .. + 3: half quad & 1 of the operand, place quad / 2 of its lanes)
-        char *at = to + (W::kFrags + pg * (D / 32) + w) * W::kFrag + (i16 + 32 * (quad & 1)) * 16 + (quad >> 1) * 8;
+        char *at = v_to + (pg * (D / 32) + w) * W::kFrag + (i16 + 32 * (quad & 1)) * 16 + (quad >> 1) * 8;
         *reinterpret_cast<uint2 *>(at) = make_uint2(__builtin_amdgcn_perm(y[1], y[0], 0x05040100), __builtin_amdgcn_perm(y[3], y[2], 0x05040100));
         *reinterpret_cast<uint2 *>(at + 16 * 16) = make_uint2(__builtin_amdgcn_perm(y[1], y[0], 0x07060302), __builtin_amdgcn_perm(y[3], y[2], 0x07060302));
     }
@@ -147,7 +147,9 @@ struct PageWindow {
     int *window;                         // [2][64] in LDS, the wavefront's own
     int now, then;
     unsigned long long ok_now, ok_then;
+    int first_bad;                       // the first step, as far as windows have been taken, with a page that is not there
     __device__ __forceinline__ void ask(int c, int lane) const {
+        asm("" : "+v"(lane));                            // (an address that is kept would cost registers)
         const int32_t *src = table + min(page0 + c * 64 + lane, max_pages - 1);
         const unsigned dst = (unsigned)(size_t)(lds_char *)reinterpret_cast<char *>(window) + (c & 1) * 256;
         asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" :: "v"(src), "s"(dst) : "memory", "m0");
@@ -157,6 +159,7 @@ struct PageWindow {
         const bool there = (unsigned)id < num_pages && (page0 + c * 64 + lane) * READER_PAGE_SIZE < keys;
         ok_then = __ballot(there);
         then = there ? id : 0;
+        if (first_bad == 0x7fffffff && ~ok_then != 0) first_bad = c * 32 + (__builtin_ctzll(~ok_then) >> 1);
     }
     // at the head of step i: a window is asked for when the one in front of it begins, and taken 20 steps later
     __device__ __forceinline__ void advance(int i, int steps, int lane) {
@@ -176,6 +179,12 @@ struct PageWindow {
     __device__ __forceinline__ unsigned there(int step, int i) const { return (unsigned)(((step ^ i) & 32 ? ok_then : ok_now) >> (step * 2 & 63)) & 3u; }
 };
 
+// Asynchronous copy to LDS: a lane of `lanes` moves 16 bytes to lds + 16 * lane.  (All lanes are active around it.)
+__device__ __forceinline__ void copy_lanes(const char *base, unsigned lane_off, unsigned lds, unsigned long long lanes) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_mov_b64 exec, %3\n\tglobal_load_lds_dwordx4 %0, %1 nt\n\ts_mov_b64 exec, -1"
+                 :: "v"(lane_off), "s"(base), "s"(lds), "s"(lanes) : "memory", "m0");
+}
+
 template <int D, int kWaves, bool kTree>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void kvq_attn_wide_kernel(KvqAttnParams p) {
     using Rows = WideRows<D>;
@@ -183,7 +192,13 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     constexpr int kRows = kWaveRows * kWaves, kMinRange = 4 * kStep;
     constexpr int kCopies = 8 / kWaves;                  // copy instructions of a wavefront in a step
     constexpr int kParts = (Part<D>::kParts + kWaves - 1) / kWaves;          // parts of the operands that it makes
-    __shared__ __attribute__((aligned(1024))) char s_frag[W::kBuffers * W::kStepBytes];
+    // With eight wavefronts, the second of each SIMD is half a step behind the first: its barrier is in front of its second product, not
+    // behind it, so that one of them has the matrix unit while the other makes weights.
+    constexpr bool kOffset = kWaves == 8;
+    // Between two barriers, of steps n and n + 1: K's operands of step n + 2 are read (by those behind: n + 1), V's of step n (n - 1), and
+    // those of step n + 3 are made.
+    constexpr int kKBuffers = kOffset ? 3 : 2, kVBuffers = kOffset ? 5 : 4, kVAt = kKBuffers * W::kHalfBytes;
+    __shared__ __attribute__((aligned(1024))) char s_frag[(kKBuffers + kVBuffers) * W::kHalfBytes];
     __shared__ __attribute__((aligned(1024))) char s_raw[W::kSlots * W::kRaw];
     __shared__ int s_ids[kWaves][2][64];
     __shared__ uint32_t s_mask[kTree ? READER_MAX_T : 1][4];
@@ -200,9 +215,14 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     if (threadIdx.x == 0) reinterpret_cast<RangeNote *>(p.workspace)[range] = note;
     int bad = 0;
     const unsigned raw_lds = (unsigned)(size_t)(lds_char *)&s_raw[0];
-    // this lane's bytes of a step's copies: codes of page copy_page, 16 bytes; scales of both pages, 4 bytes
-    const int copy_page = D == 128 ? (wave >> 1) & 1 : wave & 1, copy_part = D == 128 ? wave & 1 : 0;
-    const int scale_page = D == 128 ? lane >> 5 : lane >> 4 & 1, scale_word = D == 128 ? lane & 31 : lane & 15;
+    // what this wavefront copies of a step: the first four 1 KB of codes each, the others the scales of a page; with four, both
+    const int code_page = D == 128 ? (wave >> 1) & 1 : wave & 1, code_part = D == 128 ? wave & 1 : 0;
+    constexpr unsigned long long scale_lanes = (1ull << (D / 16)) - 1;
+    const int copy_page = wave < 4 ? code_page : wave & 1;
+    const unsigned copy_from = wave < 4 ? code_part * 1024 : 16 * D;
+    const unsigned copy_to = wave < 4 ? code_page * (16 * D) + code_part * 1024 : W::kCodes + (wave & 1) * D;
+    const unsigned long long copy_which = wave < 4 ? ~0ull : scale_lanes;
+    const bool late = kOffset && wave >= 4;
     const unsigned num_pages = (unsigned)(p.num_pages < 0x7fffffffLL ? p.num_pages : 0x7fffffffLL);
 
     WideBlock o = rg.at;
@@ -218,17 +238,18 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
             }
             const int steps = t1 - t0;
             const int unmasked = kTree ? o.L : (int)min(p0 + 1, (long long)p.max_seq_len);     // keys that every row sees
-            PageWindow ids = {p.page_table + (size_t)o.b * p.max_pages, t0 * kStepPages, p.max_pages, keys, num_pages, &s_ids[wave][0][0], 0, 0, 0, 0};
+            PageWindow ids = {p.page_table + (size_t)o.b * p.max_pages, t0 * kStepPages, p.max_pages, keys, num_pages, &s_ids[wave][0][0], 0, 0, 0, 0, 0x7fffffff};
             const int full = keys / kStep - t0;          // steps in front of this one have 32 keys that somebody sees
-            auto whole_step = [&](int step, int now) { return (step < full) & (ids.there(step, now) == 3u); };
+            const int free = unmasked / kStep - t0;      // ... that every row sees
+            auto whole_step = [&](int step) { return step < min(full, ids.first_bad); };
             const char *const cache = reinterpret_cast<const char *>(p.cache) + (size_t)o.head * KvqBlock<D>::kBytes;
             const unsigned page_bytes = (unsigned)p.Hkv * KvqBlock<D>::kBytes;
             auto issue = [&](int step, int now, unsigned slot) {     // (at step `now`) kCopies copy instructions, whatever the pages are
-                const char *b0 = cache + (size_t)ids.id(step, now, 0) * page_bytes, *b1 = cache + (size_t)ids.id(step, now, 1) * page_bytes;
-                if (kWaves == 4 || wave < 4) copy16_uniform((copy_page ? b1 : b0) + copy_part * 1024, lane * 16, raw_lds + slot + copy_page * (16 * D) + copy_part * 1024);
-                if (kWaves == 4 || wave >= 4) {
-                    const char *from = (scale_page ? b1 : b0) + 16 * D + scale_word * 4;
-                    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" :: "v"(from), "s"(raw_lds + slot + W::kCodes) : "memory", "m0");
+                if (kWaves == 4) {
+                    copy_lanes(cache + (size_t)ids.id(step, now, code_page) * page_bytes + code_part * 1024, lane * 16, raw_lds + slot + code_page * (16 * D) + code_part * 1024, ~0ull);
+                    copy_lanes(cache + (size_t)ids.id(step, now, wave & 1) * page_bytes + 16 * D, lane * 16, raw_lds + slot + W::kCodes + (wave & 1) * D, scale_lanes);
+                } else {
+                    copy_lanes(cache + (size_t)ids.id(step, now, copy_page) * page_bytes + copy_from, lane * 16, raw_lds + slot + copy_to, copy_which);
                 }
             };
             // What this wavefront has copied of keys that nobody sees becomes zeros: their bytes must not meet a weight of zero.
@@ -241,7 +262,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                 for (int pg = 0; pg < kStepPages; ++pg) {
                     const int n = there >> pg & 1 ? keys - j0 - pg * READER_PAGE_SIZE : 0;
                     char *codes = s_raw + slot + pg * (16 * D);
-                    if ((kWaves == 4 || wave < 4) && copy_page == pg && (D == 64 || copy_part == 1)) {
+                    if ((kWaves == 4 || wave < 4) && code_page == pg && (D == 64 || code_part == 1)) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             if (4 * (l >> 4) + e < n) continue;
@@ -249,18 +270,14 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                             else *reinterpret_cast<uint16_t *>(codes + 8 * D + l * 8 + e * 2) = 0;
                         }
                     }
-                    if (kWaves == 4 || wave >= 4) {          // a byte of the scales a lane, of the first D / 2
+                    if ((kWaves == 4 || wave >= 4) && (wave & 1) == pg) {        // a byte of the scales a lane, of the first D / 2
                         if (l < D / 2 && (l / (D / 8)) * 4 + l % 4 >= n) s_raw[slot + W::kCodes + pg * D + D / 2 + l] = 127;
                     }
                 }
             };
-            auto read_parts = [&](Part<D> (&part)[kParts], unsigned slot) {
-#pragma unroll
-                for (int i = 0; i < kParts; ++i) part[i].read(s_raw + slot, (wave + i * kWaves) % Part<D>::kParts, lane, i16, quad);
-            };
-            auto write_parts = [&](const Part<D> (&part)[kParts], unsigned buffer) {
-#pragma unroll
-                for (int i = 0; i < kParts; ++i) part[i].write(s_frag + buffer, (wave + i * kWaves) % Part<D>::kParts, i16, quad);
+            auto read_part = [&](Part<D> &part, int i, unsigned slot) { part.read(s_raw + slot, (wave + i * kWaves) % Part<D>::kParts, lane, i16, quad); };
+            auto write_part = [&](const Part<D> &part, int i, unsigned k_at, unsigned v_at) {
+                part.write(s_frag + k_at, s_frag + v_at, (wave + i * kWaves) % Part<D>::kParts, i16, quad);
             };
             auto meet = [&] {
                 __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
@@ -270,83 +287,112 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
             };
             ids.ask(0, lane);
             Rows rows;
-            int row = wave * kWaveRows + (lane & 31);
+            int row = lane;
+            asm("" : "+v"(row));
+            row = wave * kWaveRows + (row & 31);
             rows.load(p, o.head, row0, nt, row, half);
             wait_vmcnt<0>();                             // the first page ids are there
             asm volatile("" ::: "memory");
             ids.take(0, lane);
             ids.now = ids.then; ids.ok_now = ids.ok_then;
-            for (int s = 0; s < W::kDepth + 2; ++s) issue(s, 0, s * W::kRaw);
-            wait_vmcnt<kCopies * (W::kDepth - 1)>();     // steps 0, 1 and 2
+            for (int s = 0; s < W::kDepth + 3; ++s) issue(s, 0, s * W::kRaw);
+            wait_vmcnt<kCopies * (W::kDepth - 1)>();     // steps 0 to 3
             asm volatile("" ::: "memory");
-            for (int s = 0; s < 3; ++s)
-                if (!whole_step(s, 0)) blank(s, 0, s * W::kRaw);
+            for (int s = 0; s < 4; ++s)
+                if (!whole_step(s)) blank(s, 0, s * W::kRaw);
             meet();
-            Part<D> part[kParts];
-            for (int s = 0; s < 2; ++s) {
-                read_parts(part, s * W::kRaw);
-                write_parts(part, s * W::kStepBytes);
+            f32x16 x0, x1;
+            typename Rows::Frags k;                      // K's operands of step s + 1
+            for (int s = 0; s < 4; ++s) {
+                if (s == 2) {
+                    meet();
+                    Rows::read(k, s_frag, lane);
+                    rows.scores(x0, k);
+                    Rows::read(k, s_frag + W::kHalfBytes, lane);
+                    meet();
+                }
+                if (s == 3 && !late) break;              // (those behind make a step's part between the same barriers as the others)
+                for (int i = 0; i < kParts; ++i) {
+                    Part<D> part;
+                    read_part(part, i, s * W::kRaw);
+                    write_part(part, i, s % kKBuffers * W::kHalfBytes, kVAt + s * W::kHalfBytes);
+                }
             }
             meet();
-            auto masked = [&](int s) { return (t0 + s + 1) * kStep > unmasked || !whole_step(s, s); };
+            if (late) issue(3 + W::kDepth, 0, (3 + W::kDepth) % W::kSlots * W::kRaw);      // (... and ask for one)
+            auto masked = [&](int s) { return s >= min(free, ids.first_bad); };
             bool move = true;                            // (the reference is yet to be found)
             int s = 0;
-            // where the operands of steps s, s + 1, s + 2 are, and the bytes of steps s + 2, s + 3, s + 2 + kDepth
-            unsigned at0 = 0, at1 = W::kStepBytes, at2 = 2 * W::kStepBytes, raw2 = 2 * W::kRaw, raw5 = (2 + W::kDepth) * W::kRaw;
-            auto behind = [](unsigned slot) { return slot == (W::kSlots - 1) * W::kRaw ? 0u : slot + W::kRaw; };
-            f32x16 x0, x1;
+            // The operands of K of step s + 2 and of V of step s are read; those of step s + 3 + late are made, of bytes that have come, and
+            // bytes are asked for kDepth steps ahead of them.
+            auto next = [](unsigned at, unsigned size, unsigned end) { return at + size == end ? 0u : at + size; };
+            constexpr unsigned kKEnd = kKBuffers * W::kHalfBytes, kVEnd = kVBuffers * W::kHalfBytes, kRawEnd = W::kSlots * W::kRaw;
+            const int behind = late ? 1 : 0;
+            unsigned k_read = 2 % kKBuffers * W::kHalfBytes, v_read = 0;
+            unsigned k_make = (3 + behind) % kKBuffers * W::kHalfBytes, v_make = (3 + behind) % kVBuffers * W::kHalfBytes;
+            unsigned raw_make = (3 + behind) % W::kSlots * W::kRaw, raw_ask = (3 + behind + W::kDepth) % W::kSlots * W::kRaw;
+            unsigned raw_new = 4 * W::kRaw;              // of step s + 4
+            auto barrier = [&] {
+                wait_vmcnt<kCopies * (W::kDepth - 1)>();     // step s + 4 has come
+                asm volatile("" ::: "memory");
+                if (!whole_step(s + 4)) blank(s + 4, s, raw_new);
+                raw_new = next(raw_new, W::kRaw, kRawEnd);
+                meet();
+            };
             // One step: the weights of the scores `xa` of step s, the scores `xb` of step s + 1, the products.  true: on with the next one.
             auto step = [&](const f32x16 &xa, f32x16 &xb) -> bool {
-                typename Rows::Frags k, v;
-                Rows::read(k, s_frag + at1, lane);
+                typename Rows::Frags v;
+                Rows::read(v, s_frag + kVAt + v_read, lane);
+                Part<D> part;
+                if constexpr (kParts == 1 && !kOffset) read_part(part, 0, raw_make);
                 rows.scores(xb, k);
                 const float sum = rows.weights(xa, p.scale_log2);
-                Rows::read(v, s_frag + at0 + W::kFrags * W::kFrag, lane);
-                read_parts(part, raw2);
-                // the order: K's operands, then a product and a part of the weights in turn, V's operands and the bytes between them
-                __builtin_amdgcn_sched_group_barrier(0x100, W::kFrags, 0);
-                __builtin_amdgcn_sched_group_barrier(0x002, 10, 0);
+                // the order: a product and a part of the weights in turn, what is read between them
 #pragma unroll
                 for (int i = 0; i < W::kFrags; ++i) {
                     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x002, 48 / W::kFrags, 0);
                     __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, 56 / W::kFrags, 0);
                 }
                 if (__any(sum > kMostSum)) {
                     move = true;
                     return false;
                 }
                 rows.l = sum;
+                if (kOffset && late) barrier();
+                __builtin_amdgcn_s_setprio(1);           // (products in front of the other wavefront's weights)
+                issue(s + 3 + behind + W::kDepth, s, raw_ask);
+                if constexpr (kParts == 1 && kOffset) read_part(part, 0, raw_make);
+                Rows::read(k, s_frag + k_read, lane);
                 rows.products(v);
-                write_parts(part, at2);
+#pragma unroll
+                for (int i = 0; i < kParts; ++i) {
+                    if constexpr (kParts > 1) read_part(part, i, raw_make);      // (beside the scores there are no registers for two)
+                    write_part(part, i, k_make, kVAt + v_make);
+                }
 #pragma unroll
                 for (int i = 0; i < W::kFrags; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
                     __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
                     __builtin_amdgcn_sched_group_barrier(0x002, 4 * kParts, 1);
                 }
-                issue(s + 2 + W::kDepth, s, raw5);
-                wait_vmcnt<kCopies * (W::kDepth - 1)>();     // step s + 3 has come
-                asm volatile("" ::: "memory");
-                raw2 = behind(raw2);
-                raw5 = behind(raw5);
-                if (!whole_step(s + 3, s)) blank(s + 3, s, raw2);
-                meet();
-                const unsigned free = at0;
-                at0 = at1; at1 = at2; at2 = free;
+                __builtin_amdgcn_s_setprio(0);
+                if (!(kOffset && late)) barrier();
+                k_read = next(k_read, W::kHalfBytes, kKEnd);
+                k_make = next(k_make, W::kHalfBytes, kKEnd);
+                v_read = next(v_read, W::kHalfBytes, kVEnd);
+                v_make = next(v_make, W::kHalfBytes, kVEnd);
+                raw_make = next(raw_make, W::kRaw, kRawEnd);
+                raw_ask = next(raw_ask, W::kRaw, kRawEnd);
                 ++s;
                 if (s >= steps) return false;
                 ids.advance(s, steps, lane);
                 return !masked(s);
             };
             ids.advance(0, steps, lane);
-            // (references are moved, and scores masked, outside the loop over the steps, with the scores computed again: a path around the
-            // accumulators inside it is paid for in every step)
+            // (references are moved, and scores masked, outside the loop over the steps: a path around the accumulators inside it is paid for in
+            // every step)
             while (s < steps) {
-                {
-                    typename Rows::Frags k;
-                    Rows::read(k, s_frag + at0, lane);
-                    rows.scores(x0, k);
-                }
                 if (masked(s)) {
                     const int j0 = (t0 + s) * kStep;
                     const unsigned there = ids.there(s, s);
@@ -367,7 +413,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                     rows.move_reference(x0, p.scale_log2);
                     move = false;
                 }
-                while (step(x0, x1) && step(x1, x0)) {}
+                bool on;
+                do {
+                    on = step(x0, x1);
+                    if (move) break;
+                    x0 = x1;
+                } while (on);
             }
             wait_vmcnt<0>();                             // copies that nobody needed
             asm volatile("" ::: "memory");
@@ -400,7 +451,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                     rec[(size_t)kRows * D + row] = sum == 0.f ? -INFINITY : rows.m;
                     rec[(size_t)kRows * (D + 1) + row] = sum;
                 } else if (real && p.lse) {
-                    p.lse[lse_at(p, at)] = sum == 0.f ? -INFINITY : (rows.m + __builtin_amdgcn_logf(sum)) * kLn2;
+                    const int tok = Rows::token(p, row);
+                    p.lse[lse_at(p, o.b, row0, o.k * tb, tok, o.head * p.G + row - tok * p.G)] = sum == 0.f ? -INFINITY : (rows.m + __builtin_amdgcn_logf(sum)) * kLn2;
                 }
             }
         }
