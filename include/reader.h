@@ -894,7 +894,7 @@ int reader_pages_reorder(const reader_dims *dims, const int32_t *sources, int32_
  *   k_cache, v_cache    [num_layers, num_pages, page_bytes] in/out, 16-byte aligned; v_cache may be NULL (one cache: the one in 4 bits)
  *   status       i32 [1] or NULL                            in/out
  *
- * A page id out of range in the middle of which seq_lens[b] falls sets BAD_PAGE and stays.  Two launches.
+ * A page id out of range in the middle of which seq_lens[b] falls sets BAD_PAGE and stays.  Four launches.
  */
 int reader_pages_reserve(const reader_dims *dims, int32_t num_layers, int64_t page_bytes, const int32_t *seq_lens, const int32_t *new_lens,
                          void *k_cache, void *v_cache, int32_t *page_table, int32_t *page_refs, void *workspace,

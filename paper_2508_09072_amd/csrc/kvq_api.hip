@@ -45,7 +45,7 @@ static int kvq_attn(const reader_dims *dims, int32_t N, const void *q, const voi
 }
 
 static size_t pages_workspace(const reader_dims *dims) {
-    const size_t reserve = (size_t)dims->num_pages + 2 * (size_t)dims->B, reorder = (size_t)dims->B * ((size_t)dims->max_pages_per_seq + 1);
+    const size_t reserve = (size_t)dims->num_pages + 4 * (size_t)dims->B + 1, reorder = (size_t)dims->B * ((size_t)dims->max_pages_per_seq + 1);
     return ((reserve > reorder ? reserve : reorder) * sizeof(int32_t) + 255) & ~(size_t)255;
 }
 

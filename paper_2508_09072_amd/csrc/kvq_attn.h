@@ -54,6 +54,47 @@ __device__ __forceinline__ size_t lse_at(const PromptParams &p, int b, int row0,
     return p.nodes == 0 ? ((size_t)row0 + tok) * p.Hq + hq : ((size_t)b * p.Hq + hq) * p.nodes + node0 + tok;
 }
 
+// What is wrong with the lengths and bounds of all sequences (threads side by side).
+template <bool kTree>
+__device__ __forceinline__ int wrong_sequence(const KvqAttnParams &p, int b) {
+    if constexpr (kTree) return p.seq_lens[b] < 0 || p.seq_lens[b] > p.max_seq_len - p.nodes ? READER_STATUS_BAD_LENGTH : 0;
+    else return bad_sequence(p, b);
+}
+template <bool kTree>
+__device__ __forceinline__ void report_sequences(const KvqAttnParams &p, int threads) {
+    int bad = 0;
+    for (int b = threadIdx.x; b < p.B; b += threads) bad |= wrong_sequence<kTree>(p, b);
+    if (bad && p.status) atomicOr(p.status, bad);
+}
+
+// Block number `at` of a kv head, of all sequences' (o.head is set): false if there are not as many.
+template <bool kTree, class Block>
+__device__ __forceinline__ bool find_block(const KvqAttnParams &p, const Sequences &seqs, int at, int lane, Block &o) {
+    const int tb = p.tokens_per_block;
+    if constexpr (kTree) {
+        const int each = (p.nodes + tb - 1) / tb;
+        o.b = at / each;
+        o.k = at - o.b * each;
+        if (o.b >= p.B) return false;
+    } else {
+        for (int base = 0, before = 0;; base += 64) {
+            if (base >= p.B) return false;
+            const int b = base + lane, mine = b < p.B ? (seqs.tokens(b) + tb - 1) / tb : 0;
+            const int upto = before + (int)scan64(mine);
+            const unsigned long long in = __ballot(at < upto);
+            if (in) {
+                const int i = (int)__builtin_ctzll(in);
+                o.b = base + i;
+                o.k = at - (__builtin_amdgcn_readlane(upto, i) - __builtin_amdgcn_readlane(mine, i));
+                break;
+            }
+            before = __builtin_amdgcn_readlane(upto, 63);
+        }
+    }
+    o.load(seqs);
+    return true;
+}
+
 // This workgroup's range of the (head, sequence, block, key) axis, found by every wavefront for itself: false if there is none.  Its
 // note is written, and what the first workgroup finds wrong with lengths and bounds.
 template <class Block, int kMinRange, bool kTree>
@@ -66,9 +107,7 @@ __device__ __forceinline__ bool find_range(const KvqAttnParams &p, const Sequenc
         long long c = 0;
         if (b < p.B) {
             c = Block::sequence_cost(seqs.length(b), seqs.tokens(b), tb);
-            if constexpr (kTree) {
-                if (p.seq_lens[b] < 0 || p.seq_lens[b] > p.max_seq_len - p.nodes) bad |= READER_STATUS_BAD_LENGTH;
-            } else bad |= bad_sequence(p, b);
+            bad |= wrong_sequence<kTree>(p, b);
         }
         return scan64(c);
     };

@@ -1,5 +1,7 @@
 // Attention over a cache in 4 bits, of packed prompts, chunks and single tokens (causal) and of draft trees whose rows are in the
 // cache behind their sequence (ancestors only).
+#include <math.h>
+
 #include "kvq_attn.h"
 
 namespace reader {
@@ -169,9 +171,10 @@ struct KvqRows {
     }
 };
 
-// A workgroup takes a range of the (head, sequence, block of query rows, key) axis; kRowWaves groups of 16 kBlocks rows, each carried
-// by kKeyWaves wavefronts that take the steps of 32 keys in turn.
-template <int D, int kBlocks, int kRowWaves, int kKeyWaves, bool kTree>
+// kRowWaves groups of 16 kBlocks rows, each carried by kKeyWaves wavefronts that take the steps of 32 keys in turn.  kCut: a workgroup
+// takes a range of the (head, sequence, block of query rows, key) axis, and blocks that are cut leave records for a second launch;
+// else it takes a block.
+template <int D, int kBlocks, int kRowWaves, int kKeyWaves, bool kTree, bool kCut>
 __global__ __launch_bounds__(64 * kRowWaves * kKeyWaves) void kvq_attn_kernel(KvqAttnParams p) {
     using Rows = KvqRows<D, kBlocks>;
     constexpr int kWaveRows = kBlocks * 16, kRows = kWaveRows * kRowWaves, kWaves = kRowWaves * kKeyWaves;
@@ -187,21 +190,27 @@ __global__ __launch_bounds__(64 * kRowWaves * kKeyWaves) void kvq_attn_kernel(Kv
     RangeNote *const notes = reinterpret_cast<RangeNote *>(p.workspace);
     const Sequences seqs{p.seq_lens, p.cu_tokens, p.N, p.max_seq_len, kTree ? p.nodes : 0};
     const int range = blockIdx.x;
-    Block place;
-    int t_place;
-    if (!find_range<Block, kMinRange, kTree>(p, seqs, lane, place, t_place)) return;
-    const PromptRange<Block> rg(place, t_place, p.Hkv);
-    const RangeNote note = rg.note(seqs, p.B, tb, lane);
-    if (threadIdx.x == 0) notes[range] = note;
     int bad = 0;
-
-    Block o = rg.at;
-    for (bool first_block = true; !rg.behind(o); first_block = false) {
-        int t0, t1;
-        rg.share(o, first_block, tb, p.max_seq_len, t0, t1);
+    Block o;
+    PromptRange<Block> rg;
+    if constexpr (kCut) {
+        int t_place;
+        if (!find_range<Block, kMinRange, kTree>(p, seqs, lane, o, t_place)) return;
+        rg = PromptRange<Block>(o, t_place, p.Hkv);
+        const RangeNote note = rg.note(seqs, p.B, tb, lane);
+        if (threadIdx.x == 0) notes[range] = note;
+        o = rg.at;
+    } else {
+        if (blockIdx.x == 0 && blockIdx.y == 0) report_sequences<kTree>(p, blockDim.x);
+        o.head = blockIdx.y;
+        if (!find_block<kTree>(p, seqs, blockIdx.x, lane, o)) return;
+    }
+    for (bool first_block = true; !kCut || !rg.behind(o); first_block = false) {
         const int keys = o.keys(tb, p.max_seq_len), nt = o.tokens(tb), row0 = o.c0 + o.k * tb, all = o.tiles(tb, p.max_seq_len);
+        int t0 = 0, t1 = all;
+        if constexpr (kCut) rg.share(o, first_block, tb, p.max_seq_len, t0, t1);
         const long long p0 = (long long)o.L + o.k * tb;
-        const bool last_block = rg.is_stop(o);
+        const bool last_block = !kCut || rg.is_stop(o);
         if (t1 > t0) {
             if constexpr (kTree) {
                 if ((long long)t1 * kStep > o.L) ancestors(p.parents + (size_t)o.b * p.nodes, p.nodes, s_mask, s_up, bad);
@@ -209,7 +218,8 @@ __global__ __launch_bounds__(64 * kRowWaves * kKeyWaves) void kvq_attn_kernel(Kv
             const int first = row_wave * kWaveRows;
             // steps key_wave, key_wave + kKeyWaves, ... of the segment are this wavefront's (none, if it has no rows)
             const int steps = first < nt * p.G ? (t1 - t0 - key_wave + kKeyWaves - 1) / kKeyWaves : 0;
-            const int32_t *table = p.page_table + (size_t)o.b * p.max_pages;
+            // (through the scalar cache: among the loads of keys, an id that is waited for would wait for all of them)
+            const auto *table = (const __attribute__((address_space(4))) int32_t *)(uintptr_t)(p.page_table + (size_t)o.b * p.max_pages);
             const int unmasked = kTree ? o.L : (int)min(p0 + 1, (long long)p.max_seq_len);     // keys that every row sees
             // pages of step j: their ids, -1 for one that is not there (nobody sees its keys)
             auto page_id = [&](int j, int pg) {
@@ -226,16 +236,18 @@ __global__ __launch_bounds__(64 * kRowWaves * kKeyWaves) void kvq_attn_kernel(Kv
             Rows rows;
             rows.load(p, o.head, row0, p0, o.k * tb, nt, first, i16, quad);
             if (steps > 0) {
-                int id[kStepPages] = {page_id(0, 0), page_id(0, 1)}, id_next[kStepPages] = {page_id(1, 0), page_id(1, 1)};
-                KvqPage<D> now[kStepPages], next[kStepPages];
+                int id[kStepPages] = {page_id(0, 0), page_id(0, 1)}, id1[kStepPages] = {page_id(1, 0), page_id(1, 1)};
+                int id2[kStepPages] = {page_id(2, 0), page_id(2, 1)};
+                KvqPage<D> now[kStepPages], next[kStepPages], then[kStepPages];
                 load(now, id);
+                load(next, id1);
                 int j = 0;
                 // (the references are moved outside the loop over the steps: a path around its accumulators inside it is paid for in every step)
                 while (true) {
                     bool move = false;
                     for (; j < steps; ++j) {
-                        load(next, id_next);
-                        const int id_then[kStepPages] = {page_id(j + 2, 0), page_id(j + 2, 1)};
+                        load(then, id2);
+                        const int id3[kStepPages] = {page_id(j + 3, 0), page_id(j + 3, 1)};
                         const int j0 = (t0 + key_wave + j * kKeyWaves) * kStep;
                         rows.scores(now);
                         if (j0 + kStep > unmasked || id[0] < 0 || id[1] < 0) {
@@ -269,8 +281,10 @@ __global__ __launch_bounds__(64 * kRowWaves * kKeyWaves) void kvq_attn_kernel(Kv
 #pragma unroll
                         for (int pg = 0; pg < kStepPages; ++pg) {
                             now[pg] = next[pg];
-                            id[pg] = id_next[pg];
-                            id_next[pg] = id_then[pg];
+                            next[pg] = then[pg];
+                            id[pg] = id1[pg];
+                            id1[pg] = id2[pg];
+                            id2[pg] = id3[pg];
                         }
                     }
                     if (!move) break;
@@ -346,43 +360,100 @@ __global__ __launch_bounds__(64 * kRowWaves * kKeyWaves) void kvq_attn_kernel(Kv
             }
         }
         if (last_block) break;
-        o.next(seqs, p.B, tb);
-        o = o.of_lane(0);
+        if constexpr (kCut) {
+            o.next(seqs, p.B, tb);
+            o = o.of_lane(0);
+        }
     }
     if (p.status && bad) atomicOr(p.status, bad);
 }
 
-template <int D, int kBlocks, int kRowWaves, int kKeyWaves>
+// Blocks of a kv head, at most: every sequence has one that is not full.
+int block_count(const KvqAttnParams &p) {
+    if (p.nodes > 0) return p.B * ((p.nodes + p.tokens_per_block - 1) / p.tokens_per_block);
+    return (int)min((long long)p.N, (long long)p.N / p.tokens_per_block + p.B);
+}
+
+template <int D, int kBlocks, int kRowWaves, int kKeyWaves, bool kCut>
 hipError_t launch(KvqAttnParams p, int ranges, hipStream_t stream) {
     constexpr int kRows = 16 * kBlocks * kRowWaves;
     p.n_ranges = ranges;
     p.tokens_per_block = kRows / p.G;
-    const dim3 grid(ranges), block(64 * kRowWaves * kKeyWaves);
-    if (p.nodes > 0) hipLaunchKernelGGL((kvq_attn_kernel<D, kBlocks, kRowWaves, kKeyWaves, true>), grid, block, 0, stream, p);
-    else hipLaunchKernelGGL((kvq_attn_kernel<D, kBlocks, kRowWaves, kKeyWaves, false>), grid, block, 0, stream, p);
+    const dim3 grid = kCut ? dim3(ranges) : dim3(block_count(p), p.Hkv), block(64 * kRowWaves * kKeyWaves);
+    if (p.nodes > 0) hipLaunchKernelGGL((kvq_attn_kernel<D, kBlocks, kRowWaves, kKeyWaves, true, kCut>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((kvq_attn_kernel<D, kBlocks, kRowWaves, kKeyWaves, false, kCut>), grid, block, 0, stream, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return note_hip_error("launch kvq_attn_kernel", e);
-    return launch_prompt_merge(p, kRows, stream);
+    return kCut ? launch_prompt_merge(p, kRows, stream) : e;
 }
 
 template <int D>
 hipError_t launch_rows(const KvqAttnParams &p, hipStream_t stream) {
-    switch (kvq_attn_rows(p)) {
-        case 16: return launch<D, 1, 1, 4>(p, 2 * kNumCU, stream);
-        case 32: return launch<D, 2, 1, 4>(p, 2 * kNumCU, stream);
-        case 64: return launch<D, 2, 2, 2>(p, kNumCU, stream);
-        default: return launch_kvq_attn_wide(p, kvq_attn_rows(p), stream);
+    const int rows = kvq_attn_rows(p);
+    switch (rows) {
+        case 16: return launch<D, 1, 1, 4, true>(p, 2 * kNumCU, stream);
+        case kUncut16: return launch<D, 1, 1, 8, false>(p, 0, stream);
+        case kUncut32: return launch<D, 2, 1, 8, false>(p, 0, stream);
+        case kUncut64: return launch<D, 2, 2, 4, false>(p, 0, stream);
+        default: return launch_kvq_attn_wide(p, rows, stream);
     }
 }
 
 }  // namespace
 
-// Query rows of a kv head that a workgroup takes: as many as a sequence has.
+// Query rows of a kv head that a workgroup takes: the shortest of six estimates, in us, of what the host knows (sequences of one
+// length, max_seq_len with their last tokens).
+//   16, 32, 64 rows, blocks that are not cut: a launch, and per block that a compute unit takes its ends and its wavefronts' steps of
+//     32 keys; keys of a call that do not stay in the caches come from memory;
+//   16 rows, keys cut into ranges: start and merge, steps that all compute units share out evenly, blocks' ends;
+//   128, 256 rows, keys cut into ranges: the same, a range a workgroup; parts beyond four of a block cost the merge.
+// The constants are fitted to 122 shapes (32 query and 8 kv heads of 128, 8 and 8 of 64; 1 to 64 sequences, trees of 8 to 128 nodes,
+// 1 to 1000 tokens, up to 12 K positions).  Some of them, 16, 16 uncut, 32 uncut, 64 uncut, 128 and 256 rows: one token on 700
+// positions 16.0, 9.0, 11.2, 10.4, 20.0, 20.7; on 12 K 24.9, 52, 64, 79, 38, 33; 16 trees of 32 nodes on 1500 46, 56, 35, 25.1, 51, 47;
+// of 64 nodes on 6000 256, 241, 161, 145, 147, 129; 64 of 32 nodes on 6000 622, 551, 340, 310, 256, 386; 4 prompts of 1000 tokens 230,
+// 216, 157, 117, 89.6, 98.8.  The estimates pick the fastest on 108 of the 122 and are 1 % behind it on average, 35 % at most (all of
+// them: profiles/kvq_rows_sweep.txt).  A bound that is loose is taken for the longest sequence.
 int kvq_attn_rows(const KvqAttnParams &p) {
     const int forced = tuning(READER_TUNE_PROMPT_ROWS);
-    if (forced == 16 || forced == 32 || forced == 64 || forced == 128 || forced == 256) return forced;
-    const long long rows = ((long long)p.N + p.B - 1) / (p.B > 0 ? p.B : 1) * p.G;
-    return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+    // (blocks that are not cut are counted with the threads of a launch)
+    const bool countable = (long long)p.N < (1 << 22);
+    if (forced == 16 || forced == 128 || forced == 256) return forced;
+    if ((forced == kUncut16 || forced == kUncut32 || forced == kUncut64) && countable) return forced;
+    const bool large = p.D == 128;
+    const double tokens = p.nodes > 0 ? p.nodes : (double)p.N / p.B, longest = p.max_seq_len > tokens ? p.max_seq_len : tokens;
+    const double longest_tiles = ceil(longest / kStep), tiles = (p.nodes > 0 ? longest : longest - 0.5 * tokens) / kStep + 0.5;
+    auto blocks = [&](int rows) { return (double)p.Hkv * p.B * ceil(tokens / (rows / p.G)); };
+    const double values = (double)p.B * p.Hkv * longest * p.D, from_memory = values > 1e8 ? 8.0 + values * (17.0 / 16.0) / 5.3e6 : 0.0;
+    double best = 1e30;
+    int rows = 16;
+    auto offer = [&](int r, double us) {
+        if (us < best) { best = us; rows = r; }
+    };
+    auto uncut = [&](int r, double ends, double step, int waves) {
+        const double turns = ceil(blocks(r) / kNumCU), one = ends + step * ceil(longest_tiles / waves);
+        const double each = ends + (turns > 1 ? (large ? 2.2 : 1.1) : 0.0) + step * (tiles > waves ? tiles / waves : 1.0);
+        const double us = turns * each > one ? turns * each : one;
+        return 2.5 + (us > from_memory ? us : from_memory);
+    };
+    if (countable) {
+        offer(kUncut16, large ? uncut(16, 3.3, 1.0, 8) : uncut(16, 2.9, 0.73, 8));
+        offer(kUncut32, large ? uncut(32, 4.1, 1.32, 8) : uncut(32, 3.2, 0.92, 8));
+        offer(kUncut64, large ? uncut(64, 4.8, 1.29, 4) : uncut(64, 3.5, 0.95, 4));
+    }
+    auto parts = [&](int r, int ranges, int least) {      // of a block
+        const double n = blocks(r) * tiles / least;
+        return (n < ranges ? n : ranges) / blocks(r);
+    };
+    auto over = [](double n, double free) { return n > free ? n - free : 0.0; };
+    offer(16, (large ? 15.0 : 13.0) + (large ? 0.195 : 0.095) * blocks(16) * tiles / kNumCU + 0.15 * over(parts(16, 2 * kNumCU, 8), 8) +
+                  (large ? 1.4 : 1.1) * blocks(16) / kNumCU);
+    auto wide = [&](int r, int ranges, double start, double step, double ends) {
+        const double steps = blocks(r) * tiles / ranges;
+        return start + step * (steps > 4 ? steps : 4.0) + ends * blocks(r) / ranges + 0.3 * over(parts(r, ranges, 4), 4);
+    };
+    offer(128, large ? wide(128, 2 * kNumCU, 20, 1.25, 8) : wide(128, 2 * kNumCU, 16, 0.78, 8));
+    offer(256, large ? wide(256, kNumCU, 22, 1.09, 9) : wide(256, kNumCU, 17, 0.84, 9));
+    return rows;
 }
 
 size_t kvq_attn_workspace_bytes(int D) { return ranges_workspace_bytes(kNumCU, 256, D); }

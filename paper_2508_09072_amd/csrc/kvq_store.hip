@@ -91,6 +91,9 @@ __global__ __launch_bounds__(kStoreThreads) void kvq_store_kernel(KvqStoreParams
     if (bad && p.status) atomicOr(p.status, bad);
 }
 
+// (read once: streamed past the caches)
+__device__ __forceinline__ u32x4 load_once(const uint16_t *from) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(from)); }
+
 // Pages of a bf16 cache: a wavefront takes a page of a kv head of a layer.
 template <int D>
 __global__ __launch_bounds__(kStoreThreads) void kvq_pack_kernel(KvqStoreParams p) {
@@ -116,7 +119,7 @@ __global__ __launch_bounds__(kStoreThreads) void kvq_pack_kernel(KvqStoreParams 
         for (int i = 0; i < READER_PAGE_SIZE / kRows; ++i) {
             const int s = i * kRows + lane / kLanes;
             if (s < lo || s >= hi) continue;                 // (the four lanes of a group go the same way)
-            const u32x4 k = ld16(p.k + at + i * 512), v = ld16(p.v + at + i * 512);
+            const u32x4 k = load_once(p.k + at + i * 512), v = load_once(p.v + at + i * 512);
             if (!store_eight<D>(block, s, lane % kLanes, k, v)) bad = READER_STATUS_BAD_VALUE;
         }
     }

@@ -36,6 +36,7 @@ __global__ __launch_bounds__(kRowThreads) void pages_leave_kernel(PagesParams p)
         p.work[(size_t)p.B * p.max_pages + b] = L;
         if (L < 0 || pages_of(max(L, 0)) > p.max_pages) bad |= READER_STATUS_BAD_LENGTH;
     }
+#pragma unroll 4
     for (int j = threadIdx.x; j < p.max_pages; j += kRowThreads) {
         const int id = row[j];
         const bool real = in_pool(id, p.num_pages);
@@ -55,6 +56,7 @@ __global__ __launch_bounds__(kRowThreads) void pages_take_kernel(PagesParams p) 
     const int32_t *from = p.work + (size_t)max(s, 0) * p.max_pages;
     if (s != b) {
         if (threadIdx.x == 0) p.seq_lens[b] = L;
+#pragma unroll 4
         for (int j = threadIdx.x; j < held; j += kRowThreads) {
             const int id = from[j];
             row[j] = id;
@@ -64,26 +66,26 @@ __global__ __launch_bounds__(kRowThreads) void pages_take_kernel(PagesParams p) 
     for (int j = held + threadIdx.x; j < p.max_pages; j += kRowThreads) row[j] = -1;
 }
 
-// ---- reserve: one workgroup does the bookkeeping, a second launch copies pages.
-constexpr int kBookThreads = 1024, kBookWaves = kBookThreads / 64;
+// ---- reserve: four launches.  Rows are marked, settled and applied by a wavefront each; in between one workgroup adds up what they ask
+// for and finds the lowest free pages.  Counts change in the second and the fourth launch only, and nobody reads one there that
+// another wavefront may be changing: what the first has read of them is kept in the workspace.
+constexpr int kBookWaves = 16, kBookThreads = 64 * kBookWaves, kPerWave = 8;      // (words of 64 pages that a wavefront looks over at a time)
+constexpr int kMarkRows = 4;                          // rows of a workgroup
 
+// The workspace: pages to take, then of every sequence
 struct Book {
-    int32_t part[READER_MAX_B];        // page that the first new position falls into the middle of, or -1
-    int32_t need[READER_MAX_B];        // pages to take; then: of all sequences in front
-    uint8_t copies[READER_MAX_B];      // that page is copied
-    int sums[kBookWaves], free_here[kBookWaves];
-    int found, total, bad;
-};
-
-// Inclusive sums over the lanes.
-__device__ __forceinline__ int scan_lanes(int v, int lane) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int u = __shfl_up(v, d);
-        if (lane >= d) v += u;
+    int32_t *list;             // [num_pages] the free pages that are taken, in the order in which they are
+    int32_t *part;             // page that the first new position falls into the middle of, or -1
+    int32_t *holders;          // its count
+    int32_t *copies;           // it is copied
+    int32_t *need;             // pages to take; then: of all sequences in front
+    int32_t *enough;           // [1]
+    __device__ __forceinline__ explicit Book(const PagesParams &p) {
+        list = p.work;
+        part = list + p.num_pages;
+        holders = part + p.B; copies = holders + p.B; need = copies + p.B; enough = need + p.B;
     }
-    return v;
-}
+};
 
 // What a sequence asks for: positions [L, new) on pages of its own.
 struct Wish {
@@ -99,133 +101,154 @@ struct Wish {
     }
 };
 
-// A wavefront takes a row of the table at a time.  Entries in front of `used` are read at one place at most; behind it, an entry that
-// is given back is marked -2 - id until all are known (whether others hold a page is asked of the counts as they were).
-__global__ __launch_bounds__(kBookThreads) void pages_book_kernel(PagesParams p) {
-    __shared__ Book s;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int32_t *const list = p.work, *const pairs = p.work + p.num_pages;
-    if (tid == 0) s.found = s.bad = 0;
-    __syncthreads();
-    int bad = 0;
-    for (int b = wave; b < p.B; b += kBookWaves) {
-        const Wish w(p, b);
-        int32_t *row = p.page_table + (size_t)b * p.max_pages;
-        int need = 0, part = -1;
-        if (!w.ok) bad |= READER_STATUS_BAD_LENGTH;
-        else {
-            if (w.writes && w.first % kPage != 0) {
-                part = row[w.first / kPage];
-                if (!in_pool(part, p.num_pages)) { part = -1; bad |= READER_STATUS_BAD_PAGE; }
-            }
-            for (int j = w.used + lane; j < p.max_pages; j += 64) {
-                const int id = row[j];
-                const bool real = in_pool(id, p.num_pages), drop = real && (j >= w.want || p.page_refs[id] > 1);
-                if (drop) row[j] = -2 - id;
-                else if (!real && id != -1) row[j] = -1;
-                need += j < w.want && (drop || !real);
-            }
-            need = __builtin_amdgcn_readlane(scan_lanes(need, lane), 63);
-        }
-        if (lane == 0) { s.part[b] = part; s.need[b] = need; }
+// Inclusive sums over the lanes.
+__device__ __forceinline__ int scan_lanes(int v, int lane) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int u = __shfl_up(v, d);
+        if (lane >= d) v += u;
     }
-    __syncthreads();
-    // of the sequences that write into one page, the last keeps it if nobody else holds it
-    for (int b = tid; b < p.B; b += kBookThreads) {
-        const int part = s.part[b], holders = part >= 0 ? p.page_refs[part] : 0;
-        bool copies = false;
-        if (holders > 1) {
-            int writers = 0, last = b;
-            for (int c = 0; c < p.B; ++c)
-                if (s.part[c] == part) { ++writers; last = max(last, c); }
-            copies = !(last == b && writers == holders);
+    return v;
+}
+
+// Entries behind `used` that are given back become -2 - id.
+__global__ __launch_bounds__(64 * kMarkRows) void pages_mark_kernel(PagesParams p) {
+    const int lane = threadIdx.x & 63, b = blockIdx.x * kMarkRows + (threadIdx.x >> 6);
+    if (b >= p.B) return;
+    const Book s(p);
+    const Wish w(p, b);
+    int32_t *row = p.page_table + (size_t)b * p.max_pages;
+    int need = 0, part = -1, holders = 0, bad = 0;
+    if (!w.ok) bad = READER_STATUS_BAD_LENGTH;
+    else {
+        if (w.writes && w.first % kPage != 0) {
+            part = row[w.first / kPage];
+            if (in_pool(part, p.num_pages)) holders = p.page_refs[part];
+            else { part = -1; bad = READER_STATUS_BAD_PAGE; }
         }
+#pragma unroll 2
+        for (int j = w.used + lane; j < p.max_pages; j += 64) {
+            const int id = row[j];
+            const bool real = in_pool(id, p.num_pages), drop = real && (j >= w.want || p.page_refs[id] > 1);
+            if (drop) row[j] = -2 - id;
+            else if (!real && id != -1) row[j] = -1;
+            need += j < w.want && (drop || !real);
+        }
+        need = __builtin_amdgcn_readlane(scan_lanes(need, lane), 63);
+    }
+    if (lane == 0) {
+        s.part[b] = part; s.holders[b] = holders; s.need[b] = need;
+        if (bad && p.status) atomicOr(p.status, bad);
+    }
+}
+
+// What is given back leaves the counts.  Of the sequences that write into one page, the last keeps it if nobody else holds it.
+__global__ __launch_bounds__(64 * kMarkRows) void pages_settle_kernel(PagesParams p) {
+    const int lane = threadIdx.x & 63, b = blockIdx.x * kMarkRows + (threadIdx.x >> 6);
+    if (b >= p.B) return;
+    const Book s(p);
+    const int part = s.part[b], holders = s.holders[b];
+    bool copies = false;
+    if (holders > 1) {
+        int writers = 0, last = b;
+        for (int base = 0; base < p.B; base += 64) {
+            const unsigned long long same = __ballot(base + lane < p.B && s.part[min(base + lane, p.B - 1)] == part);
+            writers += (int)__popcll(same);
+            if (same) last = max(last, base + 63 - (int)__builtin_clzll(same));
+        }
+        copies = !(last == b && writers == holders);
+    }
+    const Wish w(p, b);
+    if (w.ok) {
+        const int32_t *row = p.page_table + (size_t)b * p.max_pages;
+#pragma unroll 2
+        for (int j = w.used + lane; j < p.max_pages; j += 64) {
+            const int id = row[j];
+            if (id < -1) atomicSub(&p.page_refs[-2 - id], 1);
+        }
+    }
+    if (lane == 0) {
+        if (copies) atomicSub(&p.page_refs[part], 1);
         s.copies[b] = copies;
     }
-    __syncthreads();
-    // pages to take in front of each sequence: four sequences a thread
+}
+
+// The sums in front of every sequence, and the lowest free pages.
+__global__ __launch_bounds__(kBookThreads) void pages_find_kernel(PagesParams p) {
+    __shared__ int s_sums[kBookWaves], s_free[2][kBookWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const Book s(p);
+    int total = 0;
     {
-        int mine[4], sum = 0;
+        int mine[READER_MAX_B / kBookThreads], sum = 0;      // sequences of a thread
+        const int first = tid * (READER_MAX_B / kBookThreads);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int b = tid * 4 + i;
+        for (int i = 0; i < READER_MAX_B / kBookThreads; ++i) {
             mine[i] = sum;
-            if (b < p.B) sum += s.need[b] + s.copies[b];
+            if (first + i < p.B) sum += s.need[first + i] + s.copies[first + i];
         }
         const int upto = scan_lanes(sum, lane);
-        if (lane == 63) s.sums[wave] = upto;
+        if (lane == 63) s_sums[wave] = upto;
         __syncthreads();
         int before = upto - sum;
-        for (int w = 0; w < wave; ++w) before += s.sums[w];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (tid * 4 + i < p.B) s.need[tid * 4 + i] = before + mine[i];
-        if (tid == kBookThreads - 1) s.total = before + sum;
-    }
-    // what is given back leaves the counts
-    for (int b = wave; b < p.B; b += kBookWaves) {
-        const Wish w(p, b);
-        if (!w.ok) continue;
-        const int32_t *row = p.page_table + (size_t)b * p.max_pages;
-        for (int j = w.used + lane; j < p.max_pages; j += 64)
-            if (row[j] < -1) atomicSub(&p.page_refs[-2 - row[j]], 1);
-        if (lane == 0 && s.copies[b]) atomicSub(&p.page_refs[s.part[b]], 1);
-    }
-    __syncthreads();
-    __threadfence();                                         // (the counts have changed behind this compute unit's cache)
-    // the lowest free pages, as many as are wanted
-    const int total = s.total;
-    for (int64_t base = 0; base < p.num_pages && s.found < total; base += kBookThreads * 4) {
-        const int64_t at = base + tid * 4;
-        unsigned free_bits = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (at + i < p.num_pages && p.page_refs[at + i] == 0) free_bits |= 1u << i;
-        const int mine = __popc(free_bits), upto = scan_lanes(mine, lane);
-        if (lane == 63) s.free_here[wave] = upto;
-        __syncthreads();
-        int before = s.found + upto - mine, all = 0;
         for (int w = 0; w < kBookWaves; ++w) {
-            if (w < wave) before += s.free_here[w];
-            all += s.free_here[w];
+            if (w < wave) before += s_sums[w];
+            total += s_sums[w];
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (free_bits >> i & 1) {
-                if (before < total) list[before] = (int32_t)(at + i);
-                ++before;
-            }
-        __syncthreads();
-        if (tid == 0) s.found += all;
-        __syncthreads();
+        for (int i = 0; i < READER_MAX_B / kBookThreads; ++i)
+            if (first + i < p.B) s.need[first + i] = before + mine[i];
     }
-    const bool enough = s.found >= total;
-    if (!enough) bad |= READER_STATUS_NO_PAGES;
-    __threadfence_block();
-    __syncthreads();
-    for (int b = wave; b < p.B; b += kBookWaves) {
+    int found = 0;
+    for (int64_t base = 0, turn = 0; base < p.num_pages && found < total; base += kBookThreads * kPerWave, turn ^= 1) {
+        const int64_t from = base + wave * (64 * kPerWave);
+        unsigned long long free_pages[kPerWave];
+        int count = 0;
+#pragma unroll
+        for (int i = 0; i < kPerWave; ++i) {
+            const int64_t at = from + i * 64 + lane;
+            free_pages[i] = __ballot(at < p.num_pages && p.page_refs[min(at, p.num_pages - 1)] == 0);
+            count += (int)__popcll(free_pages[i]);
+        }
+        if (lane == 0) s_free[turn][wave] = count;
+        __syncthreads();                                     // (the next turn writes the other half)
+        int before = found;
+        for (int w = 0; w < kBookWaves; ++w) {
+            if (w < wave) before += s_free[turn][w];
+            found += s_free[turn][w];
+        }
+#pragma unroll
+        for (int i = 0; i < kPerWave; ++i) {
+            const int at = before + (int)__popcll(free_pages[i] & ((1ull << lane) - 1ull));
+            if ((free_pages[i] >> lane & 1) && at < total) s.list[at] = (int32_t)(from + i * 64 + lane);
+            before += (int)__popcll(free_pages[i]);
+        }
+    }
+    if (tid == 0) {
+        s.enough[0] = found >= total;
+        if (found < total && p.status) atomicOr(p.status, READER_STATUS_NO_PAGES);
+    }
+}
+
+// A workgroup copies one page of one layer's cache; the first of each sequence writes its row of the table.
+constexpr int kCopyThreads = 256;
+__global__ __launch_bounds__(kCopyThreads) void pages_apply_kernel(PagesParams p) {
+    const int b = blockIdx.x, lane = threadIdx.x & 63;
+    const Book s(p);
+    const bool copies = s.copies[b] != 0, enough = s.enough[0] != 0;
+    const int from = s.part[b], base = s.need[b], to = copies && enough ? s.list[base] : -1;
+    if (blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x < 64) {
         const Wish w(p, b);
         int32_t *row = p.page_table + (size_t)b * p.max_pages;
-        const bool copies = s.copies[b];
-        int next = s.need[b], from = -1, to = -1;
-        if (copies) {
-            from = s.part[b];
-            if (lane == 0) {
-                if (!enough) atomicAdd(&p.page_refs[from], 1);
-                else {
-                    to = list[next];
-                    row[w.first / kPage] = to;
-                    p.page_refs[to] = 1;
-                }
+        int next = base + copies;
+        if (copies && lane == 0) {
+            if (!enough) atomicAdd(&p.page_refs[from], 1);
+            else {
+                row[w.first / kPage] = to;
+                p.page_refs[to] = 1;
             }
-            ++next;
         }
-        if (lane == 0) {
-            pairs[2 * b] = enough && copies ? from : -1;
-            pairs[2 * b + 1] = to;
-        }
-        if (!w.ok) continue;
-        for (int j0 = w.used; j0 < p.max_pages; j0 += 64) {
+        for (int j0 = w.used; w.ok && j0 < p.max_pages; j0 += 64) {
             const int j = j0 + lane;
             const int id = j < p.max_pages ? row[j] : -1;
             if (!enough) {                                   // everything as it was
@@ -235,28 +258,20 @@ __global__ __launch_bounds__(kBookThreads) void pages_book_kernel(PagesParams p)
             const bool take = j < w.want && id < 0;
             const unsigned long long takers = __ballot(take);
             if (take) {
-                const int page = list[next + __popcll(takers & ((1ull << lane) - 1ull))];
+                const int page = s.list[next + (int)__popcll(takers & ((1ull << lane) - 1ull))];
                 row[j] = page;
                 p.page_refs[page] = 1;
             } else if (id < -1) row[j] = -1;
             next += (int)__popcll(takers);
         }
     }
-    if (bad && p.status) atomicOr(p.status, bad);
-}
-
-// A workgroup copies one page of one layer's cache.
-constexpr int kCopyThreads = 256;
-__global__ __launch_bounds__(kCopyThreads) void pages_copy_kernel(PagesParams p) {
-    const int32_t *pairs = p.work + p.num_pages;
-    const int from = pairs[2 * blockIdx.x], to = pairs[2 * blockIdx.x + 1];
-    if (from < 0) return;
+    if (to < 0 || p.NL == 0) return;
     char *cache = (blockIdx.z == 0 ? p.k_cache : p.v_cache) + (size_t)blockIdx.y * p.num_pages * p.page_bytes;
     const uint4 *src = reinterpret_cast<const uint4 *>(cache + (size_t)from * p.page_bytes);
     uint4 *dst = reinterpret_cast<uint4 *>(cache + (size_t)to * p.page_bytes);
-    const int64_t n = p.page_bytes / 16;
+    const int n = (int)(p.page_bytes / 16);
 #pragma unroll 4
-    for (int64_t i = threadIdx.x; i < n; i += kCopyThreads) dst[i] = src[i];
+    for (int i = threadIdx.x; i < n; i += kCopyThreads) dst[i] = src[i];
 }
 
 }  // namespace
@@ -270,12 +285,12 @@ hipError_t launch_pages_reorder(const PagesParams &p, hipStream_t stream) {
 }
 
 hipError_t launch_pages_reserve(const PagesParams &p, hipStream_t stream) {
-    hipLaunchKernelGGL(pages_book_kernel, dim3(1), dim3(kBookThreads), 0, stream, p);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return note_hip_error("launch pages_book_kernel", e);
-    if (p.NL == 0) return e;
-    hipLaunchKernelGGL(pages_copy_kernel, dim3(p.B, p.NL, p.v_cache ? 2 : 1), dim3(kCopyThreads), 0, stream, p);
-    return note_hip_error("launch pages_copy_kernel", hipGetLastError());
+    const dim3 rows((p.B + kMarkRows - 1) / kMarkRows), row_threads(64 * kMarkRows);
+    hipLaunchKernelGGL(pages_mark_kernel, rows, row_threads, 0, stream, p);
+    hipLaunchKernelGGL(pages_settle_kernel, rows, row_threads, 0, stream, p);
+    hipLaunchKernelGGL(pages_find_kernel, dim3(1), dim3(kBookThreads), 0, stream, p);
+    hipLaunchKernelGGL(pages_apply_kernel, dim3(p.B, p.NL > 0 ? p.NL : 1, p.NL > 0 && p.v_cache ? 2 : 1), dim3(kCopyThreads), 0, stream, p);
+    return note_hip_error("launch pages_apply_kernel", hipGetLastError());
 }
 
 }  // namespace reader

@@ -132,6 +132,7 @@ template <class Block>
 struct PromptRange {
     Block at;
     int t_lo, t_hi, stop_head, stop_b, stop_k, heads;
+    PromptRange() = default;
     // `o` and `t`: lanes 0..31 have found the first tile, the others the one behind the last.  (Side by side: a search costs as much
     // for one place as for two, a microsecond and a half.)
     __device__ __forceinline__ PromptRange(const Block &o, int t, int Hkv) : at(o.of_lane(0)), heads(Hkv) {
