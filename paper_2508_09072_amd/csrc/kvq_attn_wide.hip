@@ -58,12 +58,6 @@ struct WideRows {
 #pragma unroll
         for (int t = 0; t < W::kFrags; ++t) f[t] = *reinterpret_cast<const bf16x8 *>(from + t * W::kFrag + lane * 16);
     }
-    __device__ __forceinline__ void scores(f32x16 &x, const Frags &k) const {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = 0.f;
-#pragma unroll
-        for (int t = 0; t < W::kFrags; ++t) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[t], q[t], x, 0, 0, 0);
-    }
     // Weights of the scores, and what the lane's sum becomes with them.
     __device__ __forceinline__ float weights(const f32x16 &x, float c2) {
         float sum[2] = {l, 0.f};
@@ -75,13 +69,6 @@ struct WideRows {
             pk[e / 8][e / 2 % 4] = pack_bf16x2(w0, w1);
         }
         return sum[0] + sum[1];
-    }
-    __device__ __forceinline__ void products(const Frags &v) {
-#pragma unroll
-        for (int pg = 0; pg < kStepPages; ++pg)
-#pragma unroll
-            for (int b = 0; b < kOut; ++b)
-                acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[pg * kOut + b], __builtin_bit_cast(bf16x8, pk[pg]), acc[b], 0, 0, 0);
     }
     // Moves the reference so that no weight of these scores is above one, nor the row's sum.
     __device__ __forceinline__ void move_reference(const f32x16 &x, float c2) {
@@ -99,6 +86,27 @@ struct WideRows {
             for (int e = 0; e < 16; ++e) acc[b][e] *= f;
     }
 };
+
+// Scores and products of kCols such groups of rows, each operand of the keys for all of them.
+template <int D, int kCols>
+__device__ __forceinline__ void scores(f32x16 (&x)[kCols], const WideRows<D> (&rows)[kCols], const typename WideRows<D>::Frags &k) {
+#pragma unroll
+    for (int c = 0; c < kCols; ++c)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[c][e] = 0.f;
+#pragma unroll
+    for (int t = 0; t < WideLayout<D>::kFrags; ++t)
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) x[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[t], rows[c].q[t], x[c], 0, 0, 0);
+}
+// (operand t of the values)
+template <int D, int kCols>
+__device__ __forceinline__ void product(WideRows<D> (&rows)[kCols], const bf16x8 &v, int t) {
+    constexpr int kOut = D / 32;
+#pragma unroll
+    for (int c = 0; c < kCols; ++c)
+        rows[c].acc[t % kOut] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, rows[c].pk[t / kOut]), rows[c].acc[t % kOut], 0, 0, 0);
+}
 
 // What one of D / 16 parts of a step's operands is made of: eight codes a lane of a page's K, and columns 2 b, 2 b + 1 of every chunk
 // of a page's V for the lane's four keys.
@@ -122,18 +130,24 @@ struct Part {
             v[0] = c.x; v[1] = c.y;
         }
     }
-    __device__ __forceinline__ void write(char *k_to, char *v_to, int part, int i16, int quad) const {
+    // in four pieces
+    uint32_t y[4];
+    __device__ __forceinline__ void write(int piece, char *k_to, char *v_to, int part, int i16, int quad) {
         const int pg = part / kWords, w = part % kWords;
-        const float sc = scale_of(ks);
-        *reinterpret_cast<u32x4 *>(k_to + ((quad >> 1) * kWords + w) * W::kFrag + (pg * 16 + i16 + 32 * (quad & 1)) * 16) =
-            u32x4{two_values<0>(k, sc), two_values<1>(k, sc), two_values<2>(k, sc), two_values<3>(k, sc)};
-        uint32_t y[4];
+        if (piece == 0) {
+            const float sc = scale_of(ks);
+            *reinterpret_cast<u32x4 *>(k_to + ((quad >> 1) * kWords + w) * W::kFrag + (pg * 16 + i16 + 32 * (quad & 1)) * 16) =
+                u32x4{two_values<0>(k, sc), two_values<1>(k, sc), two_values<2>(k, sc), two_values<3>(k, sc)};
+        } else if (piece < 3) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = two_values<0>((D == 128 ? v[e] : v[e / 2] >> (e % 2 * 16)) >> (8 * w), scale_of(vs >> (8 * e) & 255u));
-        // (keys 4 quad .. + 3: half quad & 1 of the operand, place quad / 2 of its lanes)
-        char *at = v_to + (pg * (D / 32) + w) * W::kFrag + (i16 + 32 * (quad & 1)) * 16 + (quad >> 1) * 8;
-        *reinterpret_cast<uint2 *>(at) = make_uint2(__builtin_amdgcn_perm(y[1], y[0], 0x05040100), __builtin_amdgcn_perm(y[3], y[2], 0x05040100));
-        *reinterpret_cast<uint2 *>(at + 16 * 16) = make_uint2(__builtin_amdgcn_perm(y[1], y[0], 0x07060302), __builtin_amdgcn_perm(y[3], y[2], 0x07060302));
+            for (int e = 2 * piece - 2; e < 2 * piece; ++e)
+                y[e] = two_values<0>((D == 128 ? v[e] : v[e / 2] >> (e % 2 * 16)) >> (8 * w), scale_of(vs >> (8 * e) & 255u));
+        } else {
+            // (keys 4 quad .. + 3: half quad & 1 of the operand, place quad / 2 of its lanes)
+            char *at = v_to + (pg * (D / 32) + w) * W::kFrag + (i16 + 32 * (quad & 1)) * 16 + (quad >> 1) * 8;
+            *reinterpret_cast<uint2 *>(at) = make_uint2(__builtin_amdgcn_perm(y[1], y[0], 0x05040100), __builtin_amdgcn_perm(y[3], y[2], 0x05040100));
+            *reinterpret_cast<uint2 *>(at + 16 * 16) = make_uint2(__builtin_amdgcn_perm(y[1], y[0], 0x07060302), __builtin_amdgcn_perm(y[3], y[2], 0x07060302));
+        }
     }
 };
 
@@ -185,16 +199,16 @@ __device__ __forceinline__ void copy_lanes(const char *base, unsigned lane_off, 
                  :: "v"(lane_off), "s"(base), "s"(lds), "s"(lanes) : "memory", "m0");
 }
 
-template <int D, int kWaves, bool kTree>
-__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void kvq_attn_wide_kernel(KvqAttnParams p) {
+template <int D, int kWaves, int kCols, bool kTree>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCols == 1 ? 2 : 1, kCols == 1 ? 2 : 1))) void kvq_attn_wide_kernel(KvqAttnParams p) {
     using Rows = WideRows<D>;
     using W = WideLayout<D>;
-    constexpr int kRows = kWaveRows * kWaves, kMinRange = 4 * kStep;
+    constexpr int kRows = kWaveRows * kCols * kWaves, kMinRange = 4 * kStep;
     constexpr int kCopies = 8 / kWaves;                  // copy instructions of a wavefront in a step
     constexpr int kParts = (Part<D>::kParts + kWaves - 1) / kWaves;          // parts of the operands that it makes
     // With eight wavefronts, the second of each SIMD is half a step behind the first: its barrier is in front of its second product, not
     // behind it, so that one of them has the matrix unit while the other makes weights.
-    constexpr bool kOffset = kWaves == 8;
+    constexpr bool kOffset = kWaves == 8, kEarly = kCols == 2 || kOffset;
     // Between two barriers, of steps n and n + 1: K's operands of step n + 2 are read (by those behind: n + 1), V's of step n (n - 1), and
     // those of step n + 3 are made.
     constexpr int kKBuffers = kOffset ? 3 : 2, kVBuffers = kOffset ? 5 : 4, kVAt = kKBuffers * W::kHalfBytes;
@@ -276,8 +290,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                 }
             };
             auto read_part = [&](Part<D> &part, int i, unsigned slot) { part.read(s_raw + slot, (wave + i * kWaves) % Part<D>::kParts, lane, i16, quad); };
-            auto write_part = [&](const Part<D> &part, int i, unsigned k_at, unsigned v_at) {
-                part.write(s_frag + k_at, s_frag + v_at, (wave + i * kWaves) % Part<D>::kParts, i16, quad);
+            auto write_part = [&](Part<D> &part, int piece, int i, unsigned k_at, unsigned v_at) {
+                part.write(piece, s_frag + k_at, s_frag + v_at, (wave + i * kWaves) % Part<D>::kParts, i16, quad);
             };
             auto meet = [&] {
                 __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
@@ -286,11 +300,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                 asm volatile("" ::: "memory");
             };
             ids.ask(0, lane);
-            Rows rows;
+            Rows rows[kCols];
             int row = lane;
             asm("" : "+v"(row));
-            row = wave * kWaveRows + (row & 31);
-            rows.load(p, o.head, row0, nt, row, half);
+            row = wave * (kWaveRows * kCols) + (row & 31);
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) rows[c].load(p, o.head, row0, nt, row + c * kWaveRows, half);
             wait_vmcnt<0>();                             // the first page ids are there
             asm volatile("" ::: "memory");
             ids.take(0, lane);
@@ -301,13 +316,13 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
             for (int s = 0; s < 4; ++s)
                 if (!whole_step(s)) blank(s, 0, s * W::kRaw);
             meet();
-            f32x16 x0, x1;
+            f32x16 x0[kCols], x1[kCols];
             typename Rows::Frags k;                      // K's operands of step s + 1
             for (int s = 0; s < 4; ++s) {
                 if (s == 2) {
                     meet();
                     Rows::read(k, s_frag, lane);
-                    rows.scores(x0, k);
+                    scores(x0, rows, k);
                     Rows::read(k, s_frag + W::kHalfBytes, lane);
                     meet();
                 }
@@ -315,7 +330,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                 for (int i = 0; i < kParts; ++i) {
                     Part<D> part;
                     read_part(part, i, s * W::kRaw);
-                    write_part(part, i, s % kKBuffers * W::kHalfBytes, kVAt + s * W::kHalfBytes);
+#pragma unroll
+                    for (int piece = 0; piece < 4; ++piece) write_part(part, piece, i, s % kKBuffers * W::kHalfBytes, kVAt + s * W::kHalfBytes);
                 }
             }
             meet();
@@ -340,41 +356,62 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                 meet();
             };
             // One step: the weights of the scores `xa` of step s, the scores `xb` of step s + 1, the products.  true: on with the next one.
-            auto step = [&](const f32x16 &xa, f32x16 &xb) -> bool {
+            auto step = [&](const f32x16 (&xa)[kCols], f32x16 (&xb)[kCols]) -> bool {
                 typename Rows::Frags v;
                 Rows::read(v, s_frag + kVAt + v_read, lane);
-                Part<D> part;
-                if constexpr (kParts == 1 && !kOffset) read_part(part, 0, raw_make);
-                rows.scores(xb, k);
-                const float sum = rows.weights(xa, p.scale_log2);
+                Part<D> part[kEarly ? kParts : 1];
+                if constexpr (kEarly && !kOffset) {
+#pragma unroll
+                    for (int i = 0; i < kParts; ++i) read_part(part[i], i, raw_make);
+                }
+                scores(xb, rows, k);
+                float sum[kCols], most = 0.f;
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) {
+                    sum[c] = rows[c].weights(xa[c], p.scale_log2);
+                    most = fmaxf(most, sum[c]);
+                }
                 // the order: a product and a part of the weights in turn, what is read between them
 #pragma unroll
-                for (int i = 0; i < W::kFrags; ++i) {
+                for (int i = 0; i < W::kFrags * kCols; ++i) {
                     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
                     __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
                     __builtin_amdgcn_sched_group_barrier(0x002, 56 / W::kFrags, 0);
                 }
-                if (__any(sum > kMostSum)) {
+                if (__any(most > kMostSum)) {
                     move = true;
                     return false;
                 }
-                rows.l = sum;
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) rows[c].l = sum[c];
                 if (kOffset && late) barrier();
                 __builtin_amdgcn_s_setprio(1);           // (products in front of the other wavefront's weights)
                 issue(s + 3 + behind + W::kDepth, s, raw_ask);
-                if constexpr (kParts == 1 && kOffset) read_part(part, 0, raw_make);
+                if constexpr (kOffset) read_part(part[0], 0, raw_make);
                 Rows::read(k, s_frag + k_read, lane);
-                rows.products(v);
+                if constexpr (kOffset) {
 #pragma unroll
-                for (int i = 0; i < kParts; ++i) {
-                    if constexpr (kParts > 1) read_part(part, i, raw_make);      // (beside the scores there are no registers for two)
-                    write_part(part, i, k_make, kVAt + v_make);
-                }
+                    for (int i = 0; i < W::kFrags; ++i) product(rows, v[i], i);
 #pragma unroll
-                for (int i = 0; i < W::kFrags; ++i) {
-                    __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
-                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
-                    __builtin_amdgcn_sched_group_barrier(0x002, 4 * kParts, 1);
+                    for (int piece = 0; piece < 4; ++piece) write_part(part[0], piece, 0, k_make, kVAt + v_make);
+#pragma unroll
+                    for (int i = 0; i < W::kFrags; ++i) {
+                        __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+                        __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+                        __builtin_amdgcn_sched_group_barrier(0x002, 4, 1);
+                    }
+                } else {
+                    // (the order is kept: a product, then a piece of the operands to come, while the matrix unit works on it; 2 to 4 % faster,
+                    // but where another wavefront's weights fill the gaps 2 % slower)
+#pragma unroll
+                    for (int i = 0; i < W::kFrags; ++i) {
+                        product(rows, v[i], i);
+                        if (i < 4 * kParts) {
+                            if (!kEarly && i % 4 == 0) read_part(part[0], i / 4, raw_make);  // (beside the scores there are no registers for them)
+                            write_part(part[kEarly ? i / 4 : 0], i % 4, i / 4, k_make, kVAt + v_make);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
                 __builtin_amdgcn_s_setprio(0);
                 if (!(kOffset && late)) barrier();
@@ -397,27 +434,33 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
                     const int j0 = (t0 + s) * kStep;
                     const unsigned there = ids.there(s, s);
                     if ((j0 < keys && !(there & 1)) || (j0 + READER_PAGE_SIZE < keys && !(there & 2))) bad |= READER_STATUS_BAD_PAGE;
-                    asm("" : "+v"(row));                 // (what follows from the row is found again: kept through the steps, it would cost registers)
-                    const int tok = min(Rows::token(p, row), nt - 1), lim = (int)min(p0 + tok + 1, (long long)p.max_seq_len);
-                    const uint32_t *mask = s_mask[kTree ? o.k * tb + tok : 0];
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int at = e / 4 * 8 + half * 4 + e % 4, key = j0 + at, n = key - o.L;
-                        // (no branches: with them the compiler has lost the assignment on one of the ways)
-                        bool sees = ((there >> (e / 8) & 1u) != 0) & (key < lim);
-                        if constexpr (kTree) sees &= (n < 0) | ((mask[(n >> 5) & 3] >> (n & 31) & 1u) != 0);
-                        x0[e] = sees ? x0[e] : -INFINITY;
+                    for (int c = 0; c < kCols; ++c) {
+                        int r = row + c * kWaveRows;
+                        asm volatile("" : "+v"(r) :: "memory");      // (what follows from the row is found again: kept through the steps, it would cost registers)
+                        const int tok = min(Rows::token(p, r), nt - 1), lim = (int)min(p0 + tok + 1, (long long)p.max_seq_len);
+                        const uint32_t *mask = s_mask[kTree ? o.k * tb + tok : 0];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const int at = e / 4 * 8 + half * 4 + e % 4, key = j0 + at, n = key - o.L;
+                            // (no branches: with them the compiler has lost the assignment on one of the ways)
+                            bool sees = ((there >> (e / 8) & 1u) != 0) & (key < lim);
+                            if constexpr (kTree) sees &= (n < 0) | ((mask[(n >> 5) & 3] >> (n & 31) & 1u) != 0);
+                            x0[c][e] = sees ? x0[c][e] : -INFINITY;
+                        }
                     }
                 }
                 if (move) {
-                    rows.move_reference(x0, p.scale_log2);
+#pragma unroll
+                    for (int c = 0; c < kCols; ++c) rows[c].move_reference(x0[c], p.scale_log2);
                     move = false;
                 }
                 bool on;
                 do {
                     on = step(x0, x1);
                     if (move) break;
-                    x0 = x1;
+#pragma unroll
+                    for (int c = 0; c < kCols; ++c) x0[c] = x1[c];
                 } while (on);
             }
             wait_vmcnt<0>();                             // copies that nobody needed
@@ -427,32 +470,35 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
             const bool whole = t0 == 0 && t1 == all;
             float *rec = reinterpret_cast<float *>(reinterpret_cast<char *>(p.workspace) + kNotesBytes) +
                          (size_t)(2 * range + (t0 == 0 ? 1 : 0)) * ((size_t)kRows * (D + 2));
-            int half_ = half;
-            asm("" : "+v"(row), "+v"(half_));
-            const float sum = rows.l + __shfl_xor(rows.l, 32), inv = sum == 0.f ? 0.f : 1.f / sum;
-            const bool real = Rows::token(p, row) < nt;
-            const size_t at = Rows::out_row(p, o.head, row0, nt, row);
 #pragma unroll
-            for (int g = 0; g < 2; ++g)
+            for (int c = 0; c < kCols; ++c) {
+                int half_ = half, r = row + c * kWaveRows;
+                asm volatile("" : "+v"(r), "+v"(half_) :: "memory");
+                const float sum = rows[c].l + __shfl_xor(rows[c].l, 32), inv = sum == 0.f ? 0.f : 1.f / sum;
+                const int tok = Rows::token(p, r);
+                const bool real = tok < nt;
+                const size_t at = Rows::out_row(p, o.head, row0, nt, r);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {            // the D / 16 values of chunk 8 g + 4 half + i
-                    const int chunk = 8 * g + 4 * half_ + i;
+                for (int g = 0; g < 2; ++g)
 #pragma unroll
-                    for (int h = 0; h < D / 64; ++h) {
-                        const f32x4 v = f32x4{rows.acc[2 * h][4 * g + i], rows.acc[2 * h][4 * g + 8 + i], rows.acc[2 * h + 1][4 * g + i],
-                                              rows.acc[2 * h + 1][4 * g + 8 + i]} * inv;
-                        const int piece = chunk * (D / 64) + h;
-                        if (!whole) reinterpret_cast<f32x4 *>(rec)[piece * kRows + row] = v;
-                        else if (real) *reinterpret_cast<uint2 *>(p.out + at * D + piece * 4) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+                    for (int i = 0; i < 4; ++i) {        // the D / 16 values of chunk 8 g + 4 half + i
+                        const int chunk = 8 * g + 4 * half_ + i;
+#pragma unroll
+                        for (int h = 0; h < D / 64; ++h) {
+                            const f32x4 v = f32x4{rows[c].acc[2 * h][4 * g + i], rows[c].acc[2 * h][4 * g + 8 + i], rows[c].acc[2 * h + 1][4 * g + i],
+                                                  rows[c].acc[2 * h + 1][4 * g + 8 + i]} * inv;
+                            const int piece = chunk * (D / 64) + h;
+                            if (!whole) reinterpret_cast<f32x4 *>(rec)[piece * kRows + r] = v;
+                            else if (real) *reinterpret_cast<uint2 *>(p.out + at * D + piece * 4) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+                        }
                     }
-                }
-            if (half_ == 0) {
-                if (!whole) {
-                    rec[(size_t)kRows * D + row] = sum == 0.f ? -INFINITY : rows.m;
-                    rec[(size_t)kRows * (D + 1) + row] = sum;
-                } else if (real && p.lse) {
-                    const int tok = Rows::token(p, row);
-                    p.lse[lse_at(p, o.b, row0, o.k * tb, tok, o.head * p.G + row - tok * p.G)] = sum == 0.f ? -INFINITY : (rows.m + __builtin_amdgcn_logf(sum)) * kLn2;
+                if (half_ == 0) {
+                    if (!whole) {
+                        rec[(size_t)kRows * D + r] = sum == 0.f ? -INFINITY : rows[c].m;
+                        rec[(size_t)kRows * (D + 1) + r] = sum;
+                    } else if (real && p.lse) {
+                        p.lse[lse_at(p, o.b, row0, o.k * tb, tok, o.head * p.G + r - tok * p.G)] = sum == 0.f ? -INFINITY : (rows[c].m + __builtin_amdgcn_logf(sum)) * kLn2;
+                    }
                 }
             }
         }
@@ -463,13 +509,13 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     if (p.status && bad) atomicOr(p.status, bad);
 }
 
-template <int D, int kWaves>
+template <int D, int kWaves, int kCols>
 hipError_t launch_wide(KvqAttnParams p, hipStream_t stream) {
-    constexpr int kRows = kWaveRows * kWaves;
-    p.n_ranges = kNumCU * 8 / kWaves;                    // (as many as run at once)
+    constexpr int kRows = kWaveRows * kCols * kWaves;
+    p.n_ranges = kNumCU * 8 / (kWaves * kCols);          // (as many as run at once)
     p.tokens_per_block = kRows / p.G;
-    if (p.nodes > 0) hipLaunchKernelGGL((kvq_attn_wide_kernel<D, kWaves, true>), dim3(p.n_ranges), dim3(64 * kWaves), 0, stream, p);
-    else hipLaunchKernelGGL((kvq_attn_wide_kernel<D, kWaves, false>), dim3(p.n_ranges), dim3(64 * kWaves), 0, stream, p);
+    if (p.nodes > 0) hipLaunchKernelGGL((kvq_attn_wide_kernel<D, kWaves, kCols, true>), dim3(p.n_ranges), dim3(64 * kWaves), 0, stream, p);
+    else hipLaunchKernelGGL((kvq_attn_wide_kernel<D, kWaves, kCols, false>), dim3(p.n_ranges), dim3(64 * kWaves), 0, stream, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return note_hip_error("launch kvq_attn_wide_kernel", e);
     return launch_prompt_merge(p, kRows, stream);
@@ -478,8 +524,8 @@ hipError_t launch_wide(KvqAttnParams p, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_kvq_attn_wide(const KvqAttnParams &p, int rows, hipStream_t stream) {
-    if (rows == 128) return p.D == 64 ? launch_wide<64, 4>(p, stream) : launch_wide<128, 4>(p, stream);
-    return p.D == 64 ? launch_wide<64, 8>(p, stream) : launch_wide<128, 8>(p, stream);
+    if (rows == 128) return p.D == 64 ? launch_wide<64, 4, 1>(p, stream) : launch_wide<128, 4, 1>(p, stream);
+    return p.D == 64 ? launch_wide<64, 4, 2>(p, stream) : launch_wide<128, 8, 1>(p, stream);
 }
 
 }  // namespace reader
