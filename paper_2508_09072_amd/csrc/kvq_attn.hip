@@ -178,7 +178,7 @@ template <int D, int kBlocks, int kRowWaves, int kKeyWaves, bool kTree, bool kCu
 __global__ __launch_bounds__(64 * kRowWaves * kKeyWaves) void kvq_attn_kernel(KvqAttnParams p) {
     using Rows = KvqRows<D, kBlocks>;
     constexpr int kWaveRows = kBlocks * 16, kRows = kWaveRows * kRowWaves, kWaves = kRowWaves * kKeyWaves;
-    constexpr int kMinRange = 2 * kStep * kKeyWaves;
+    constexpr int kMinRange = 8 * kStep;
     constexpr bool kMeet = kKeyWaves > 1;
     __shared__ __attribute__((aligned(16))) f32x4 s_part[kMeet ? kWaves : 1][kMeet ? kWaveRows * D / 4 : 1];
     __shared__ float s_sum[kWaves][2][kWaveRows];
@@ -392,6 +392,7 @@ hipError_t launch_rows(const KvqAttnParams &p, hipStream_t stream) {
     const int rows = kvq_attn_rows(p);
     switch (rows) {
         case 16: return launch<D, 1, 1, 4, true>(p, 2 * kNumCU, stream);
+        case kFew16: return launch<D, 1, 1, 8, true>(p, kNumCU, stream);
         case kUncut16: return launch<D, 1, 1, 8, false>(p, 0, stream);
         case kUncut32: return launch<D, 2, 1, 8, false>(p, 0, stream);
         case kUncut64: return launch<D, 2, 2, 4, false>(p, 0, stream);
@@ -401,23 +402,30 @@ hipError_t launch_rows(const KvqAttnParams &p, hipStream_t stream) {
 
 }  // namespace
 
-// Query rows of a kv head that a workgroup takes: the shortest of six estimates, in us, of what the host knows (sequences of one
+// Query rows of a kv head that a workgroup takes: the shortest of seven estimates, in us, of what the host knows (sequences of one
 // length, max_seq_len with their last tokens).
 //   16, 32, 64 rows, blocks that are not cut: a launch, and per block that a compute unit takes its ends and its wavefronts' steps of
 //     32 keys; keys of a call that do not stay in the caches come from memory;
-//   16 rows, keys cut into ranges: start and merge, steps that all compute units share out evenly, blocks' ends;
+//   16 rows, keys cut into ranges: start and merge, steps that all compute units share out evenly, blocks' ends; 256 ranges of eight
+//     wavefronts where no compute unit has a second block (a step's loads are out sooner, half the records), else 512 of four;
 //   128, 256 rows, keys cut into ranges: the same, a range a workgroup; parts beyond four of a block cost the merge.
 // The constants are fitted to 122 shapes (32 query and 8 kv heads of 128, 8 and 8 of 64; 1 to 64 sequences, trees of 8 to 128 nodes,
-// 1 to 1000 tokens, up to 12 K positions).  Some of them, 16, 16 uncut, 32 uncut, 64 uncut, 128 and 256 rows: one token on 700
-// positions 16.0, 9.0, 11.2, 10.4, 20.0, 20.7; on 12 K 24.9, 52, 64, 79, 38, 33; 16 trees of 32 nodes on 1500 46, 56, 35, 25.1, 51, 47;
-// of 64 nodes on 6000 256, 241, 161, 145, 147, 129; 64 of 32 nodes on 6000 622, 551, 340, 310, 256, 386; 4 prompts of 1000 tokens 230,
-// 216, 157, 117, 89.6, 98.8.  The estimates pick the fastest on 108 of the 122 and are 1 % behind it on average, 35 % at most (all of
-// them: profiles/kvq_rows_sweep.txt).  A bound that is loose is taken for the longest sequence.
+// 1 to 1000 tokens, up to 12 K positions).
+// The estimates pick the fastest on 108 of the 122 and are 0.7 % behind it on average, 12.5 % at most.  Some of them, in us (all of
+// them: profiles/kvq_rows_sweep.txt):
+//                                              16  16 few  16 uncut  32 uncut  64 uncut    128    256
+//   one token on 700 positions               15.9    15.6       9.0      11.2      10.4   19.7   20.8
+//   one token on 12 K positions              25.0    20.1      52.1      63.7      79.5   36.9   33.4
+//   16 trees of 32 nodes on 1500             46.3    59.1      56.5      35.0      25.1   50.6   45.9
+//   16 trees of 64 nodes on 6000              256     270       241       158       140    136    119
+//   64 trees of 32 nodes on 6000              615     536       549       319       292    244    374
+//   4 prompts of 1000 tokens                  229     328       216       157       117   89.0   99.0
+// A bound that is loose is taken for the longest sequence.
 int kvq_attn_rows(const KvqAttnParams &p) {
     const int forced = tuning(READER_TUNE_PROMPT_ROWS);
     // (blocks that are not cut are counted with the threads of a launch)
     const bool countable = (long long)p.N < (1 << 22);
-    if (forced == 16 || forced == 128 || forced == 256) return forced;
+    if (forced == 16 || forced == kFew16 || forced == 128 || forced == 256) return forced;
     if ((forced == kUncut16 || forced == kUncut32 || forced == kUncut64) && countable) return forced;
     const bool large = p.D == 128;
     const double tokens = p.nodes > 0 ? p.nodes : (double)p.N / p.B, longest = p.max_seq_len > tokens ? p.max_seq_len : tokens;
@@ -445,13 +453,14 @@ int kvq_attn_rows(const KvqAttnParams &p) {
         return (n < ranges ? n : ranges) / blocks(r);
     };
     auto over = [](double n, double free) { return n > free ? n - free : 0.0; };
-    offer(16, (large ? 15.0 : 13.0) + (large ? 0.195 : 0.095) * blocks(16) * tiles / kNumCU + 0.15 * over(parts(16, 2 * kNumCU, 8), 8) +
-                  (large ? 1.4 : 1.1) * blocks(16) / kNumCU);
+    const bool few = blocks(16) <= kNumCU;
+    offer(few ? kFew16 : 16, (large ? (few ? 13.0 : 15.0) : (few ? 12.0 : 13.0)) + (large ? 0.195 : 0.095) * blocks(16) * tiles / kNumCU +
+                                 0.15 * over(parts(16, few ? kNumCU : 2 * kNumCU, 8), 8) + (large ? 1.4 : 1.1) * blocks(16) / kNumCU);
     auto wide = [&](int r, int ranges, double start, double step, double ends) {
         const double steps = blocks(r) * tiles / ranges;
         return start + step * (steps > 4 ? steps : 4.0) + ends * blocks(r) / ranges + 0.3 * over(parts(r, ranges, 4), 4);
     };
-    offer(128, large ? wide(128, 2 * kNumCU, 20, 1.25, 8) : wide(128, 2 * kNumCU, 16, 0.78, 8));
+    offer(128, large ? wide(128, 2 * kNumCU, 20, 1.25, 8) : wide(128, 2 * kNumCU, 16, 0.70, 8));
     offer(256, large ? wide(256, kNumCU, 22, 1.09, 9) : wide(256, kNumCU, 17, 0.84, 9));
     return rows;
 }

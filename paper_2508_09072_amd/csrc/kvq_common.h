@@ -55,7 +55,8 @@ struct KvqAttnParams : PromptParams {      // (k_cache and v_cache are not used;
     const uint8_t *cache;                  // [num_pages, Hkv, 17 D]
     const int32_t *parents;                // draft trees [B, nodes], or null
 };
-constexpr int kUncut16 = 17, kUncut64 = 65;      // of kvq_attn_rows: rows a workgroup, blocks that are not cut (and kUncut32)
+// of kvq_attn_rows: 16 and 64 rows a workgroup, blocks that are not cut (and kUncut32); 16 rows, ranges for few blocks
+constexpr int kUncut16 = 17, kUncut64 = 65, kFew16 = 18;
 size_t kvq_attn_workspace_bytes(int D);
 int kvq_attn_rows(const KvqAttnParams &p);
 hipError_t launch_kvq_attn(const KvqAttnParams &p, hipStream_t stream);

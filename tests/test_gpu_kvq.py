@@ -17,7 +17,7 @@ def R():
     return binding
 
 
-@pytest.fixture(params=[0, 16, 17, 33, 65, 128, 256])
+@pytest.fixture(params=[0, 16, 17, 18, 33, 65, 128, 256])
 def rows(R, request):
     """Every kernel takes every problem: query rows a workgroup; 0: as they are chosen."""
     R.reader_tuning_override(R.TUNE_PROMPT_ROWS, request.param or -1)
