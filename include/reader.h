@@ -884,8 +884,8 @@ int reader_pages_reorder(const reader_dims *dims, const int32_t *sources, int32_
  *   - pages that lie wholly behind seq_lens[b]: entries that hold none, or one that others hold too, get a free page
  *   - pages behind new_lens[b] are given back; entries there that name no page become -1
  * Free pages are taken in ascending order, for the sequences in their order and the pages of each from the first; what the call
- * gives back can be taken by it.  If there are not as many as are wanted, none is taken or given back and READER_STATUS_NO_PAGES is
- * set.  seq_lens is not changed.
+ * gives back can be taken by it, but for pages that it copies from.  If there are not as many as are wanted, none is taken or given
+ * back and READER_STATUS_NO_PAGES is set.  seq_lens is not changed.
  *
  *   num_layers   >= 0 (0: no contents to copy, the caches are not used)
  *   page_bytes   bytes of a page of one layer, a multiple of 16

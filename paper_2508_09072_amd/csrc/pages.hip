@@ -190,10 +190,8 @@ __device__ __forceinline__ void settle(const PagesParams &p, const Book &s, int 
             if (id < -1) atomicSub(&p.page_refs[-2 - id], 1);
         }
     }
-    if (lane == 0) {
-        if (copies) atomicSub(&p.page_refs[part], 1);
-        s.copies[b] = copies;
-    }
+    // (a page that is copied from leaves with the copy: it is in use till then, also where all others give it back here)
+    if (lane == 0) s.copies[b] = copies;
 }
 
 // The sums in front of every sequence, and the lowest free pages: a workgroup of kBookThreads.
@@ -273,12 +271,10 @@ __global__ __launch_bounds__(kCopyThreads) void pages_apply_kernel(PagesParams p
         const Wish w(p, b);
         int32_t *row = p.page_table + (size_t)b * p.max_pages;
         int next = base + copies;
-        if (copies && lane == 0) {
-            if (!enough) atomicAdd(&p.page_refs[from], 1);
-            else {
-                row[w.first / kPage] = to;
-                p.page_refs[to] = 1;
-            }
+        if (to >= 0 && lane == 0) {
+            atomicSub(&p.page_refs[from], 1);
+            row[w.first / kPage] = to;
+            p.page_refs[to] = 1;
         }
         for (int j0 = w.used; w.ok && j0 < p.max_pages; j0 += 64) {
             const int j = j0 + lane;

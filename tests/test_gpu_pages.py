@@ -62,7 +62,6 @@ class Pool:
             used, want = pages_of(self.lens[b]), pages_of(new[b])
             part = table[b][self.lens[b] // PAGE] if self.lens[b] % PAGE and new[b] > self.lens[b] else -1
             if part >= 0 and self.refs[part] > 1 and not (writers[part][-1] == b and len(writers[part]) == self.refs[part]):
-                refs[part] -= 1
                 wants.append((b, self.lens[b] // PAGE))
                 copies.append((b, part))
             for j in range(used, self.max_pages):
@@ -79,6 +78,8 @@ class Pool:
         for (b, j), p in zip(wants, free):
             table[b][j] = taken[b, j] = p
             refs[p] = 1
+        for _, part in copies:
+            refs[part] -= 1
         self.refs, self.table = refs, table
         return [(part, taken[b, self.lens[b] // PAGE]) for b, part in copies]
 
@@ -205,6 +206,20 @@ def test_pages_that_are_reserved_twice_are_not_shared(R):
         pool.refs[pool.table[0][j]] += 1
     reserve(R, pool, [64, 64], contents(torch.Generator().manual_seed(1), 1, 30))
     assert max(pool.refs) == 1
+
+
+@pytest.mark.parametrize("lens,new", [
+    ([20, 10], [36, 20]), ([20, 16], [21, 90]), ([20, 0], [40, 96]), ([20, 20, 4], [30, 30, 60]), ([20, 20, 4, 4], [30, 30, 60, 60]),
+])
+def test_a_page_that_is_copied_from_is_not_taken_where_its_other_holders_give_it_back(R, lens, new):
+    """Forks of which some have been taken back to fewer positions: a page that one of them is in the middle of lies behind another."""
+    for seed in range(4):
+        pool = Pool(12 + seed, [20] * len(lens), 6, 30)
+        pool.reorder([0] * len(lens))
+        pool.lens = list(lens)
+        assert len(reserve(R, pool, new, contents(torch.Generator().manual_seed(seed), 3, 30))) > 0
+        for p in range(30):
+            assert pool.refs[p] == sum(row.count(p) for row in pool.table)
 
 
 def test_a_pool_that_is_short_changes_nothing(R):
