@@ -545,7 +545,8 @@ int reader_measure_peaks(const void *src, size_t src_bytes, void *scratch, size_
  *                               than 10 ms), the one that appends four times as long
  *   READER_TUNE_JOIN_SPREAD     1 = the shares of a pair run on different XCDs there (0 or cleared: on one)
  *   READER_TUNE_PROMPT_ROWS     one of the values of reader_prompt_rows: 16, 32, READER_PROMPT_ROWS_32_UNCUT, 64, 128 or 256 (other
- *                               values: planner decides)
+ *                               values: planner decides); of the attention over the cache in 4 bits 16, 128, 256 (cut into ranges;
+ *                               18: 16 rows, half as many ranges), 17, READER_PROMPT_ROWS_32_UNCUT, 65 (16, 32, 64 rows, not cut)
  * Returns READER_OK, or READER_EINVAL for an unknown `which`.
  */
 enum {
@@ -757,6 +758,8 @@ int reader_kv_evict(const reader_dims *dims, int32_t num_layers, int32_t keep, i
  * called, as in the in-cache layout of reader_tree_attn: plain decoding and the verification of a tree then read the same
  * values.  dims->variant must be 0; the bf16 tensors start at a multiple of 16 bytes.  A page that rows are stored in
  * belongs to one sequence (reader_pages_reserve).
+ * The attention takes up to 2^30 positions a sequence.  Scores are held in 32 bits: a row whose scores times log2(e) reach 2^30 in
+ * magnitude, or whose query holds a NaN or an infinity, is unspecified; other rows are not.
  */
 #define READER_KVQ_BLOCK_BYTES(D) (17 * (D))
 

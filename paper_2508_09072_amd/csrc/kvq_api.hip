@@ -32,7 +32,7 @@ static int kvq_attn(const reader_dims *dims, int32_t N, const void *q, const voi
                     size_t workspace_bytes, int32_t *status, KvqAttnParams &p) {
     if (!q || !seq_lens || !out || !kvq_cache(dims, cache, page_table) || !aligned(q, out)) return READER_EINVAL;
     if ((long long)dims->max_pages_per_seq * dims->page_size < (long long)max_seq_len + room) return READER_EINVAL;
-    if ((long long)max_seq_len + room > 0x7fffffffLL - READER_MAX_T) return READER_EUNSUPPORTED;
+    if ((long long)max_seq_len + room > kKvqMaxPositions) return READER_EUNSUPPORTED;      // (steps ahead of the last one are counted too)
     if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < reader_kvq_workspace_bytes(dims, N, max_seq_len)) return READER_EWORKSPACE;
     p.q = (const uint16_t *)q; p.cache = (const uint8_t *)cache;
     p.page_table = page_table; p.seq_lens = seq_lens;

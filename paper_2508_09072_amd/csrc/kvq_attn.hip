@@ -241,7 +241,8 @@ __global__ __launch_bounds__(64 * kRowWaves * kKeyWaves) void kvq_attn_kernel(Kv
                 KvqPage<D> now[kStepPages], next[kStepPages], then[kStepPages];
                 load(now, id);
                 load(next, id1);
-                int j = 0;
+                int j = 0, moved_at = -1;
+                // (a step's references are moved once: of scores so large that a reference cannot move by less, weights may stay large)
                 // (the references are moved outside the loop over the steps: a path around its accumulators inside it is paid for in every step)
                 while (true) {
                     bool move = false;
@@ -271,7 +272,7 @@ __global__ __launch_bounds__(64 * kRowWaves * kKeyWaves) void kvq_attn_kernel(Kv
                             }
                         }
                         float sum[kBlocks];
-                        if (__any(rows.weights(p.scale_log2, sum) > kMostSum)) {
+                        if (__any(rows.weights(p.scale_log2, sum) > kMostSum) & (j != moved_at)) {
                             move = true;
                             break;
                         }
@@ -289,6 +290,7 @@ __global__ __launch_bounds__(64 * kRowWaves * kKeyWaves) void kvq_attn_kernel(Kv
                     }
                     if (!move) break;
                     rows.move_references(p.scale_log2);
+                    moved_at = j;
                 }
             }
             rows.finish_sums();

@@ -339,6 +339,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCo
             auto masked = [&](int s) { return s >= min(free, ids.first_bad); };
             bool move = true;                            // (the reference is yet to be found)
             int s = 0;
+            // (a step's reference is moved once: of scores so large that it cannot move by less, weights stay large)
+            float most_now = kMostSum;
             // The operands of K of step s + 2 and of V of step s are read; those of step s + 3 + late are made, of bytes that have come, and
             // bytes are asked for kDepth steps ahead of them.
             auto next = [](unsigned at, unsigned size, unsigned end) { return at + size == end ? 0u : at + size; };
@@ -378,7 +380,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCo
                     __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
                     __builtin_amdgcn_sched_group_barrier(0x002, 56 / W::kFrags, 0);
                 }
-                if (__any(most > kMostSum)) {
+                if (__any(most > most_now)) {
                     move = true;
                     return false;
                 }
@@ -421,6 +423,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCo
                 v_make = next(v_make, W::kHalfBytes, kVEnd);
                 raw_make = next(raw_make, W::kRaw, kRawEnd);
                 raw_ask = next(raw_ask, W::kRaw, kRawEnd);
+                most_now = kMostSum;
                 ++s;
                 if (s >= steps) return false;
                 ids.advance(s, steps, lane);
@@ -454,6 +457,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCo
 #pragma unroll
                     for (int c = 0; c < kCols; ++c) rows[c].move_reference(x0[c], p.scale_log2);
                     move = false;
+                    most_now = INFINITY;
                 }
                 bool on;
                 do {

@@ -55,6 +55,7 @@ struct KvqAttnParams : PromptParams {      // (k_cache and v_cache are not used;
     const uint8_t *cache;                  // [num_pages, Hkv, 17 D]
     const int32_t *parents;                // draft trees [B, nodes], or null
 };
+constexpr int kKvqMaxPositions = 1 << 30;              // of a sequence
 // of kvq_attn_rows: 16 and 64 rows a workgroup, blocks that are not cut (and kUncut32); 16 rows, ranges for few blocks
 constexpr int kUncut16 = 17, kUncut64 = 65, kFew16 = 18;
 size_t kvq_attn_workspace_bytes(int D);

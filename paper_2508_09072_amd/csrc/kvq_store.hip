@@ -3,6 +3,8 @@
 // A group of 32 values gets the scale 2^e, e = floor(log2 of the largest magnitude) - 2, one more where that magnitude is above 7
 // times it (kept within [-125, 125]): no value is further from its code than 2^e, half of the largest step.  Codes are rounded to
 // nearest even by v_cvt_scalef32_pk_fp4_bf16, whose operands are exact here.  A lane takes eight values, four lanes a group.
+#include <limits.h>
+
 #include "kvq_common.h"
 #include "tree_attn_common.h"
 
@@ -143,7 +145,7 @@ __device__ inline void check_path(const KvqCompactParams &p, int b, PathShared &
     if (tid == 0) { sh.L = p.seq_lens[b]; sh.n = p.accept_len[b]; sh.bad = 0; }
     __syncthreads();
     const int L = sh.L, n = sh.n;
-    const long long mapped = (long long)p.max_pages * READER_PAGE_SIZE;
+    const long long mapped = min((long long)p.max_pages * READER_PAGE_SIZE, (long long)INT_MAX);
     int bad = 0;
     if (n < 0 || n > p.max_path - 1 || L < 0 || (long long)L + n + 1 > mapped) bad = READER_STATUS_BAD_PATH;
     else if (tid <= n) {

@@ -357,6 +357,56 @@ def test_scores_far_from_the_first_ones(R, rows, new, L, D, up):
     p.check(*p.run(R))
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("tree", [False, True])
+def test_large_scores(R, rows, D, tree):
+    """Queries with one value: the keys with the largest one there share the row, the others are 32 (size 2^12) to millions behind.  The
+    products are exact: the weights of a value are equal, rounded to bf16 alike, added up in 32 bits, divided, and the output rounded.  A
+    weight at a distance x has a relative error of three roundings of x, which is below 104 where it is not zero in 32 bits, and one
+    below the smallest normal number is lost."""
+    parents = bushy(torch.Generator().manual_seed(5), 2, 40) if tree else None
+    p = Problem([40, 40], [500, 3], 4, 2, D, seed=23, parents=parents)
+    for size in (2.0 ** 12, 2.0 ** 20, 2.0 ** 28):
+        at = torch.randint(0, D, (p.N, 4, 1), generator=p.gen)
+        p.q = torch.zeros_like(p.q).scatter_(-1, at, torch.where(torch.rand((p.N, 4, 1), generator=p.gen) < 0.5, -size, size).bfloat16())
+        out, lse = p.run(R)
+        for b in range(2):
+            k, v = p.cache.rows(b, p.L[b] + 40, False), p.cache.rows(b, p.L[b] + 40, True)
+            q = p.q[40 * b:40 * b + 40].double().view(40, 2, 2, D).permute(1, 2, 0, 3)
+            x = (q @ k[:, None].transpose(-1, -2)).masked_fill(~p.sees(b), -math.inf)
+            w = ((x - x.amax(-1, keepdim=True)) * D ** -0.5).exp()
+            n = w.sum(-1)
+            want, mass = (w @ v[:, None]) / n[..., None], (w @ v[:, None].abs()) / n[..., None]
+            flat = lambda t: t.permute(2, 0, 1, *range(3, t.dim())).reshape(40, 4, *t.shape[3:])  # noqa: E731
+            S = k.shape[1]
+            bound = P.BF16 * (want.abs() + mass) * (1 + 2 * P.BF16) + (320 + S) * P.F32 * mass + S * 2.0 ** -126 * float(v.abs().max())
+            P.check(out[40 * b:40 * b + 40], flat(want), flat(bound), "out")
+            top = flat(x.amax(-1) * D ** -0.5 + n.log())
+            P.check(lse[40 * b:40 * b + 40], top, 8 * P.F32 * (1 + top.abs()), "lse")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("tree", [False, True])
+def test_queries_that_are_no_numbers_stay_to_themselves(R, rows, D, tree):
+    """Infinite, huge and undefined queries: the call ends, and the other rows are what they are without them."""
+    parents = bushy(torch.Generator().manual_seed(6), 2, 70) if tree else None
+    p = Problem([70, 70], [900, 40], 4, 2, D, seed=24, parents=parents)
+    usual = p.q.clone()
+    for bad in (math.nan, math.inf, -math.inf, 3.3e38, 2.0 ** 100, 2.0 ** 45, 2.0 ** 34):
+        odd = torch.rand((p.N, 4), generator=p.gen) < 0.2
+        p.q = torch.where(odd[..., None], (torch.randn((p.N, 4, D), generator=p.gen).clamp(-1, 1) * bad).bfloat16(), usual)
+        p.q[0, 0] = usual[0, 0]
+        p.q[1, 0, 3] = bad
+        odd[0, 0], odd[1, 0] = False, True
+        out, lse = p.run(R)
+        for b in range(2):
+            mine = slice(70 * b, 70 * b + 70)
+            want, s, bo, bs = K.attention(usual[mine], p.cache.rows(b, p.L[b] + 70, False), p.cache.rows(b, p.L[b] + 70, True), p.sees(b))
+            good = ~odd[mine]
+            P.check(out[mine][good], want[good], bo[good], "out")
+            P.check(lse[mine][good], s[good], bs[good], "lse")
+
+
 def test_scales_at_both_ends(R, rows):
     """The smallest and the largest scales that rows are stored with: weights of one key, values that are next to nothing."""
     p = Problem([3], [60], 2, 1, 64, seed=6)
@@ -566,6 +616,37 @@ def test_replays_of_a_captured_step(R):
         assert float(noise) == float(noise)
         for a, b in zip(outs + [lse, data, lens], want):
             assert torch.equal(a, b), "replay %d" % turn
+
+
+def test_replays_of_captured_packing(R):
+    gen = torch.Generator().manual_seed(25)
+    L, NL = [100, 33], 2
+    cache, source = K.Cache(gen, L, 2, 64, lead=(NL,)), K.Cache(gen, L, 2, 64)
+    k, v = (torch.randn((NL, source.num_pages, 2, 16, 64), generator=gen).bfloat16().cuda() for _ in range(2))
+    data0 = cache.data.cuda()
+    data, lens, status, from_table, table = data0.clone(), i32(L), status_word(), source.table.cuda(), cache.table.cuda()
+    dims = R.make_dims(2, 1, 2, 2, 64, max(cache.max_pages, source.max_pages), 1, cache.num_pages)
+    assert cache.max_pages == source.max_pages
+
+    def step():
+        R.reader_kvq_pack(dims, k, v, from_table, None, lens, 112, data, table, status)
+
+    graph = torch.cuda.CUDAGraph()
+    step()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        step()
+    for turn in range(4):
+        k.normal_()
+        lens.copy_(i32([100 - 30 * turn, 5 * turn]))
+        data.copy_(data0)
+        step()
+        want = data.clone()
+        data.copy_(data0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(data, want) and int(status) == 0
 
 
 def test_two_streams_at_once(R):

@@ -326,3 +326,69 @@ def test_beams_write_without_disturbing_each_other(R, kind):
         for j in range(37, 57):
             assert bool((got[j] == 10 * b + j % 10).all())
     assert int(status) == 0 and int((refs > 1).sum()) == 2        # the two full pages of the prefix
+
+
+def test_replays_of_a_captured_reorder_and_reserve(R):
+    """Captured once; replayed on other selections and lengths, with eager work between, next to a graph that shares the workspace."""
+    for B, max_pages, num_pages in ((5, 9, 60), (70, 80, 6000)):  # one workgroup, and a workgroup a sequence
+        gen = torch.Generator().manual_seed(B)
+        lens = torch.randint(1, 16 * max_pages - 20, (B,), generator=gen).tolist()
+        pool = Pool(B, lens, max_pages, num_pages)
+        dims, ws, status = setup(R, pool)
+        table, seq, refs = pool.tensors()
+        caches = contents(gen, 2, num_pages)
+        i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+        sources, new = i32(list(range(B))), i32(lens)
+
+        def step():
+            R.reader_pages_reorder(dims, sources, table, seq, refs, ws, status)
+            R.reader_pages_reserve(dims, seq, new, caches[0], caches[1], table, refs, ws, status)
+
+        graphs = []
+        step()
+        for _ in range(2):
+            torch.cuda.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+                step()
+            graphs.append(graph)
+        for turn in range(6):
+            chosen = torch.randint(0, B, (B,), generator=gen).tolist()
+            pool.reorder(chosen)
+            wanted = [min(n + turn, 16 * max_pages) for n in pool.lens]
+            before = [c.clone() for c in caches]
+            copies = pool.reserve(wanted)
+            sources.copy_(i32(chosen))
+            new.copy_(i32(wanted))
+            ws.fill_(0xff)
+            torch.cuda.synchronize()
+            graphs[turn % 2].replay()
+            torch.cuda.synchronize()
+            assert int(status) == 0
+            pool.same(table, seq, refs)
+            for c, old in zip(caches, before):
+                for a, b in copies:
+                    old[:, b] = old[:, a]
+                assert torch.equal(c, old)
+            pool.lens = wanted                                    # (the rows that were made room for)
+            seq.copy_(new)
+
+
+def test_two_pools_on_two_streams(R):
+    pools = [Pool(40 + i, [30 + i] * 40, 60, 4000) for i in range(2)]
+    sources = [torch.randint(-1, 40, (40,), generator=torch.Generator().manual_seed(i)).tolist() for i in range(2)]
+    jobs = [(*setup(R, p), *p.tensors(), torch.tensor(s, dtype=torch.int32, device="cuda")) for p, s in zip(pools, sources)]
+    new = torch.full((40,), 100, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    for stream, (dims, ws, status, table, seq, refs, src) in zip([torch.cuda.Stream() for _ in pools], jobs):
+        with torch.cuda.stream(stream):
+            for _ in range(3):
+                R.reader_pages_reorder(dims, src, table, seq, refs, ws, status)
+                R.reader_pages_reserve(dims, seq, new, None, None, table, refs, ws, status)
+    torch.cuda.synchronize()
+    for pool, source, (dims, ws, status, table, seq, refs, src) in zip(pools, sources, jobs):
+        for _ in range(3):
+            pool.reorder(source)
+            pool.reserve([100] * 40)
+        assert int(status) == 0
+        pool.same(table, seq, refs)

@@ -143,6 +143,7 @@ def test_lengths_and_workspaces_of_the_attention(R, name):
         assert call(R, name, dims(R), max_seq_len=125) == EINVAL   # ... four of them for the tree
     # beyond what 31 bits count, a last block's tokens included
     assert call(R, name, dims(R, max_pages_per_seq=(1 << 27) + 10, B=1), max_seq_len=0x7fffffff) == EUNSUPPORTED
+    assert call(R, name, dims(R, max_pages_per_seq=(1 << 26) + 10, B=1), max_seq_len=(1 << 30) + 1) == EUNSUPPORTED
     d = dims(R)
     N = 8 if "tree" in name else 10
     need = R.reader_kvq_workspace_bytes(d, N, 100)
