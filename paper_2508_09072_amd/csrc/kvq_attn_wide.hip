@@ -18,8 +18,8 @@ constexpr int kWaveRows = 32;
 template <int D>
 struct WideLayout {
     static constexpr int kFrag = 1024;                                            // an operand: 16 bytes a lane
-    static constexpr int kFrags = D / 16;                                         // of K in a step, and of V
-    static constexpr int kHalfBytes = kFrags * kFrag;                             // of K, of V
+    static constexpr int kFrags = D / 16;                                         // of V in a step
+    static constexpr int kStepFrags = kFrags * kFrag;
     static constexpr int kCodes = kStepPages * 16 * D, kRaw = kCodes + 2 * D;     // codes of two pages, their scales
     static constexpr int kSlots = 6, kDepth = 3;                                  // raw steps in the ring; asked for as many steps before they are used
 };
@@ -30,7 +30,7 @@ template <int D>
 struct WideRows {
     using W = WideLayout<D>;
     static constexpr int kOut = D / 32;
-    bf16x8 q[W::kFrags];                 // step t: values ((t / (D/32)) * 2 + half) D / 4 + t % (D/32) * 8 .. + 7 of the row
+    QueryPieces q[D / 64];               // [t]: values 64 t + 32 half .. + 31 of the row
     f32x16 acc[kOut];                    // [b][4 g + i]: with rho = 8 g + 4 half + i, value rho % 16 * D / 16 + 2 b + rho / 16 of the row
     float m, l;                          // reference (exponent of two), this lane's part of the sum
     u32x4 pk[kStepPages];
@@ -44,8 +44,12 @@ struct WideRows {
         const bool real = token(p, row) < nt;
         const size_t at = out_row(p, head, row0, nt, row);
 #pragma unroll
-        for (int t = 0; t < W::kFrags; ++t)
-            q[t] = __builtin_bit_cast(bf16x8, keep_if(real, ld16(p.q + at * D + (t / (D / 32) * 2 + half) * (D / 4) + t % (D / 32) * 8)));
+        for (int t = 0; t < D / 64; ++t) {
+            u32x4 bits[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) bits[i] = __builtin_bit_cast(u32x4, keep_if(real, ld16(p.q + at * D + t * 64 + half * 32 + i * 8)));
+            q[t].make(bits);
+        }
         m = kNoReference;
         l = 0.f;
 #pragma unroll
@@ -87,17 +91,43 @@ struct WideRows {
     }
 };
 
+// K of a step, as it is stored: lane (half, key) holds the codes of values 64 t + 32 half .. + 31 and their scale.
+template <int D>
+struct WideKeys {
+    u32x4 codes[D / 64];
+    uint32_t scale[D / 64];
+    __device__ __forceinline__ void read(const char *raw, int lane) {
+        const int key = lane & 31, pg = key >> 4, row = key & 15, half = lane >> 5;
+        const char *from = raw + pg * (16 * D) + row * (D / 8), *scales = raw + WideLayout<D>::kCodes + pg * D + row;
+#pragma unroll
+        for (int t = 0; t < D / 64; ++t) {
+            if constexpr (D == 128) codes[t] = *reinterpret_cast<const u32x4 *>(from + (2 * t + half) * (2 * D));
+            else {
+                const uint2 a = *reinterpret_cast<const uint2 *>(from + 2 * half * (2 * D)), b = *reinterpret_cast<const uint2 *>(from + (2 * half + 1) * (2 * D));
+                codes[t] = u32x4{a.x, a.y, b.x, b.y};
+            }
+            scale[t] = *reinterpret_cast<const uint8_t *>(scales + (2 * t + half) * 16);
+        }
+    }
+};
+
 // Scores and products of kCols such groups of rows, each operand of the keys for all of them.
 template <int D, int kCols>
-__device__ __forceinline__ void scores(f32x16 (&x)[kCols], const WideRows<D> (&rows)[kCols], const typename WideRows<D>::Frags &k) {
+__device__ __forceinline__ void scores(f32x16 (&x)[kCols], const WideRows<D> (&rows)[kCols], const WideKeys<D> &k) {
 #pragma unroll
     for (int c = 0; c < kCols; ++c)
 #pragma unroll
         for (int e = 0; e < 16; ++e) x[c][e] = 0.f;
+    // (formats: 4 is e2m1, 2 is e2m3)
 #pragma unroll
-    for (int t = 0; t < WideLayout<D>::kFrags; ++t)
+    for (int t = 0; t < D / 64; ++t)
 #pragma unroll
-        for (int c = 0; c < kCols; ++c) x[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[t], rows[c].q[t], x[c], 0, 0, 0);
+        for (int c = 0; c < kCols; ++c) {
+            const QueryPieces &q = rows[c].q[t];
+            x[c] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(k.codes[t]), operand(q.piece[0]), x[c], 4, 2, 0, k.scale[t], 0, q.scales);
+            x[c] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(k.codes[t]), operand(q.piece[1]), x[c], 4, 2, 0, k.scale[t], 1, q.scales);
+            x[c] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(k.codes[t]), operand(q.piece[2]), x[c], 4, 2, 0, k.scale[t], 2, q.scales);
+        }
 }
 // (operand t of the values)
 template <int D, int kCols>
@@ -108,18 +138,15 @@ __device__ __forceinline__ void product(WideRows<D> (&rows)[kCols], const bf16x8
         rows[c].acc[t % kOut] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, rows[c].pk[t / kOut]), rows[c].acc[t % kOut], 0, 0, 0);
 }
 
-// What one of D / 16 parts of a step's operands is made of: eight codes a lane of a page's K, and columns 2 b, 2 b + 1 of every chunk
-// of a page's V for the lane's four keys.
+// What one of D / 16 parts of a step's operands of V is made of: columns 2 b, 2 b + 1 of every chunk of a page for the lane's four keys.
 template <int D>
 struct Part {
     using W = WideLayout<D>;
     static constexpr int kWords = D / 32, kParts = D / 16;
-    uint32_t k, ks, vs, v[D == 128 ? 4 : 2];
+    uint32_t vs, v[D == 128 ? 4 : 2];
     __device__ __forceinline__ void read(const char *raw, int part, int lane, int i16, int quad) {
-        const int pg = part / kWords, w = part % kWords;
+        const int pg = part / kWords;
         const char *codes = raw + pg * (16 * D), *scales = raw + W::kCodes + pg * D;
-        k = *reinterpret_cast<const uint32_t *>(codes + lane * (D / 8) + w * 4);
-        ks = *reinterpret_cast<const uint8_t *>(scales + (D == 128 ? quad : quad >> 1) * 16 + i16);
         vs = *reinterpret_cast<const uint32_t *>(scales + D / 2 + quad * (D / 8) + (i16 * (D / 16) / 32) * 4);
         if constexpr (D == 128) {
             const u32x4 c = *reinterpret_cast<const u32x4 *>(codes + 8 * D + lane * 16);
@@ -130,17 +157,13 @@ struct Part {
             v[0] = c.x; v[1] = c.y;
         }
     }
-    // in four pieces
+    // in three pieces
     uint32_t y[4];
-    __device__ __forceinline__ void write(int piece, char *k_to, char *v_to, int part, int i16, int quad) {
+    __device__ __forceinline__ void write(int piece, char *v_to, int part, int i16, int quad) {
         const int pg = part / kWords, w = part % kWords;
-        if (piece == 0) {
-            const float sc = scale_of(ks);
-            *reinterpret_cast<u32x4 *>(k_to + ((quad >> 1) * kWords + w) * W::kFrag + (pg * 16 + i16 + 32 * (quad & 1)) * 16) =
-                u32x4{two_values<0>(k, sc), two_values<1>(k, sc), two_values<2>(k, sc), two_values<3>(k, sc)};
-        } else if (piece < 3) {
+        if (piece < 2) {
 #pragma unroll
-            for (int e = 2 * piece - 2; e < 2 * piece; ++e)
+            for (int e = 2 * piece; e < 2 * piece + 2; ++e)
                 y[e] = two_values<0>((D == 128 ? v[e] : v[e / 2] >> (e % 2 * 16)) >> (8 * w), scale_of(vs >> (8 * e) & 255u));
         } else {
             // (keys 4 quad .. + 3: half quad & 1 of the operand, place quad / 2 of its lanes)
@@ -209,10 +232,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCo
     // With eight wavefronts, the second of each SIMD is half a step behind the first: its barrier is in front of its second product, not
     // behind it, so that one of them has the matrix unit while the other makes weights.
     constexpr bool kOffset = kWaves == 8, kEarly = kCols == 2 || kOffset;
-    // Between two barriers, of steps n and n + 1: K's operands of step n + 2 are read (by those behind: n + 1), V's of step n (n - 1), and
-    // those of step n + 3 are made.
-    constexpr int kKBuffers = kOffset ? 3 : 2, kVBuffers = kOffset ? 5 : 4, kVAt = kKBuffers * W::kHalfBytes;
-    __shared__ __attribute__((aligned(1024))) char s_frag[(kKBuffers + kVBuffers) * W::kHalfBytes];
+    // Between two barriers, of steps n and n + 1: K of step n + 2 is read (by those behind: n + 1), V's operands of step n (n - 1), and those of
+    // step n + 3 are made, while the bytes of steps n + 4 to n + 6 come.
+    constexpr int kVBuffers = kOffset ? 5 : 4;
+    __shared__ __attribute__((aligned(1024))) char s_frag[kVBuffers * W::kStepFrags];
     __shared__ __attribute__((aligned(1024))) char s_raw[W::kSlots * W::kRaw];
     __shared__ int s_ids[kWaves][2][64];
     __shared__ uint32_t s_mask[kTree ? READER_MAX_T : 1][4];
@@ -290,8 +313,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCo
                 }
             };
             auto read_part = [&](Part<D> &part, int i, unsigned slot) { part.read(s_raw + slot, (wave + i * kWaves) % Part<D>::kParts, lane, i16, quad); };
-            auto write_part = [&](Part<D> &part, int piece, int i, unsigned k_at, unsigned v_at) {
-                part.write(piece, s_frag + k_at, s_frag + v_at, (wave + i * kWaves) % Part<D>::kParts, i16, quad);
+            auto write_part = [&](Part<D> &part, int piece, int i, unsigned v_at) {
+                part.write(piece, s_frag + v_at, (wave + i * kWaves) % Part<D>::kParts, i16, quad);
             };
             auto meet = [&] {
                 __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
@@ -317,13 +340,13 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCo
                 if (!whole_step(s)) blank(s, 0, s * W::kRaw);
             meet();
             f32x16 x0[kCols], x1[kCols];
-            typename Rows::Frags k;                      // K's operands of step s + 1
+            WideKeys<D> k;                               // of step s + 1
             for (int s = 0; s < 4; ++s) {
                 if (s == 2) {
                     meet();
-                    Rows::read(k, s_frag, lane);
+                    k.read(s_raw, lane);
                     scores(x0, rows, k);
-                    Rows::read(k, s_frag + W::kHalfBytes, lane);
+                    k.read(s_raw + W::kRaw, lane);
                     meet();
                 }
                 if (s == 3 && !late) break;              // (those behind make a step's part between the same barriers as the others)
@@ -331,7 +354,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCo
                     Part<D> part;
                     read_part(part, i, s * W::kRaw);
 #pragma unroll
-                    for (int piece = 0; piece < 4; ++piece) write_part(part, piece, i, s % kKBuffers * W::kHalfBytes, kVAt + s * W::kHalfBytes);
+                    for (int piece = 0; piece < 3; ++piece) write_part(part, piece, i, s * W::kStepFrags);
                 }
             }
             meet();
@@ -341,13 +364,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCo
             int s = 0;
             // (a step's reference is moved once: of scores so large that it cannot move by less, weights stay large)
             float most_now = kMostSum;
-            // The operands of K of step s + 2 and of V of step s are read; those of step s + 3 + late are made, of bytes that have come, and
+            // K of step s + 2 and the operands of V of step s are read; those of step s + 3 + late are made, of bytes that have come, and
             // bytes are asked for kDepth steps ahead of them.
             auto next = [](unsigned at, unsigned size, unsigned end) { return at + size == end ? 0u : at + size; };
-            constexpr unsigned kKEnd = kKBuffers * W::kHalfBytes, kVEnd = kVBuffers * W::kHalfBytes, kRawEnd = W::kSlots * W::kRaw;
+            constexpr unsigned kVEnd = kVBuffers * W::kStepFrags, kRawEnd = W::kSlots * W::kRaw;
             const int behind = late ? 1 : 0;
-            unsigned k_read = 2 % kKBuffers * W::kHalfBytes, v_read = 0;
-            unsigned k_make = (3 + behind) % kKBuffers * W::kHalfBytes, v_make = (3 + behind) % kVBuffers * W::kHalfBytes;
+            unsigned k_read = 2 * W::kRaw, v_read = 0, v_make = (3 + behind) % kVBuffers * W::kStepFrags;
             unsigned raw_make = (3 + behind) % W::kSlots * W::kRaw, raw_ask = (3 + behind + W::kDepth) % W::kSlots * W::kRaw;
             unsigned raw_new = 4 * W::kRaw;              // of step s + 4
             auto barrier = [&] {
@@ -360,7 +382,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCo
             // One step: the weights of the scores `xa` of step s, the scores `xb` of step s + 1, the products.  true: on with the next one.
             auto step = [&](const f32x16 (&xa)[kCols], f32x16 (&xb)[kCols]) -> bool {
                 typename Rows::Frags v;
-                Rows::read(v, s_frag + kVAt + v_read, lane);
+                Rows::read(v, s_frag + v_read, lane);
                 Part<D> part[kEarly ? kParts : 1];
                 if constexpr (kEarly && !kOffset) {
 #pragma unroll
@@ -375,11 +397,14 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCo
                 }
                 // the order: a product and a part of the weights in turn, what is read between them
 #pragma unroll
-                for (int i = 0; i < W::kFrags * kCols; ++i) {
+                for (int i = 0; i < 3 * D / 64 * kCols; ++i) {
                     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
                     __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x002, 56 / W::kFrags, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, 56 / (3 * D / 64), 0);
                 }
+                // (here, and not behind the branch, where nothing would be beside them)
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) asm volatile("" : "+v"(xb[c]));
                 if (__any(most > most_now)) {
                     move = true;
                     return false;
@@ -390,12 +415,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCo
                 __builtin_amdgcn_s_setprio(1);           // (products in front of the other wavefront's weights)
                 issue(s + 3 + behind + W::kDepth, s, raw_ask);
                 if constexpr (kOffset) read_part(part[0], 0, raw_make);
-                Rows::read(k, s_frag + k_read, lane);
+                k.read(s_raw + k_read, lane);
                 if constexpr (kOffset) {
 #pragma unroll
                     for (int i = 0; i < W::kFrags; ++i) product(rows, v[i], i);
 #pragma unroll
-                    for (int piece = 0; piece < 4; ++piece) write_part(part[0], piece, 0, k_make, kVAt + v_make);
+                    for (int piece = 0; piece < 3; ++piece) write_part(part[0], piece, 0, v_make);
 #pragma unroll
                     for (int i = 0; i < W::kFrags; ++i) {
                         __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
@@ -408,19 +433,18 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCo
 #pragma unroll
                     for (int i = 0; i < W::kFrags; ++i) {
                         product(rows, v[i], i);
-                        if (i < 4 * kParts) {
-                            if (!kEarly && i % 4 == 0) read_part(part[0], i / 4, raw_make);  // (beside the scores there are no registers for them)
-                            write_part(part[kEarly ? i / 4 : 0], i % 4, i / 4, k_make, kVAt + v_make);
+                        if (i < 3 * kParts) {
+                            if (!kEarly && i % 3 == 0) read_part(part[0], i / 3, raw_make);  // (beside the scores there are no registers for them)
+                            write_part(part[kEarly ? i / 3 : 0], i % 3, i / 3, v_make);
                         }
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }
                 __builtin_amdgcn_s_setprio(0);
                 if (!(kOffset && late)) barrier();
-                k_read = next(k_read, W::kHalfBytes, kKEnd);
-                k_make = next(k_make, W::kHalfBytes, kKEnd);
-                v_read = next(v_read, W::kHalfBytes, kVEnd);
-                v_make = next(v_make, W::kHalfBytes, kVEnd);
+                k_read = next(k_read, W::kRaw, kRawEnd);
+                v_read = next(v_read, W::kStepFrags, kVEnd);
+                v_make = next(v_make, W::kStepFrags, kVEnd);
                 raw_make = next(raw_make, W::kRaw, kRawEnd);
                 raw_ask = next(raw_ask, W::kRaw, kRawEnd);
                 most_now = kMostSum;
@@ -463,6 +487,11 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCo
                 do {
                     on = step(x0, x1);
                     if (move) break;
+                    if (on) {
+                        on = step(x1, x0);
+                        if (!move) continue;
+                        on = false;
+                    }
 #pragma unroll
                     for (int c = 0; c < kCols; ++c) x0[c] = x1[c];
                 } while (on);
