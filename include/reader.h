@@ -828,7 +828,8 @@ int reader_kvq_compact_layers(const reader_dims *dims, int32_t num_layers, const
  *
  * A node whose link is wrong counts as a root (BAD_TREE): it sees the prefix and itself.  Keys behind a page id out of range are left
  * out (BAD_PAGE); a row that sees no key gives zeros and a log-sum-exp of -inf.  What the pages hold behind the last row does
- * not reach the outputs.  Softmax weights are rounded to bf16 before they multiply V.  dims->max_path is not used.  Two launches.
+ * not reach the outputs.  Softmax weights are rounded to bf16 before they multiply V.  dims->max_path is not used.  One launch, or two
+ * where the keys of a block of rows are shared out.
  */
 size_t reader_kvq_workspace_bytes(const reader_dims *dims, int32_t N, int32_t max_seq_len);
 int reader_kvq_tree_attn(const reader_dims *dims, const void *q, const void *kvq_cache, const int32_t *page_table,
@@ -875,7 +876,8 @@ size_t reader_pages_workspace_bytes(const reader_dims *dims);
  *   status       i32 [1] or NULL                            in/out
  *
  * A source outside [-1, B) counts as b (READER_STATUS_BAD_PATH).  An entry in front of a sequence's length that names no page
- * is handed on as it is (BAD_PAGE); a length that the table does not hold takes the whole row (BAD_LENGTH).  Two launches.
+ * is handed on as it is (BAD_PAGE); a length that the table does not hold takes the whole row (BAD_LENGTH).  One launch up to
+ * B * (max_pages_per_seq + 1) = 4096, else two.
  */
 int reader_pages_reorder(const reader_dims *dims, const int32_t *sources, int32_t *page_table, int32_t *seq_lens, int32_t *page_refs,
                          void *workspace, size_t workspace_bytes, int32_t *status, void *stream);

@@ -18,52 +18,6 @@ __device__ __forceinline__ uint32_t two_values(uint32_t word, float scale) {
 }
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
-// 32 values of a query row, as matrix instructions multiply them with codes of 4 bits as they are stored: three pieces of 6 bits (e2m3:
-// sign, up to 7.5, steps of 1/8 below 2, of 1/4 and 1/2 above) with scales of their own, the rounding of each left to the next.  With E =
-// floor(log2 of the largest magnitude) - 2 the pieces count in steps of 2^(E - 3), 2^(E - 7) and 2^(E - 12) at least, so that a value above
-// 1/240 of the largest keeps all bits that bf16 has and no value is off by more than 2^(E - 13), 2^-15 of the largest.  Two of
-// these products take the time of one with bf16 operands.
-typedef uint32_t u32x6 __attribute__((ext_vector_type(6)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-struct QueryPieces {
-    u32x6 piece[3];
-    uint32_t scales;                     // a byte each: exponent + 127
-    __device__ __forceinline__ void make(const u32x4 (&bits)[4]) {
-        typedef float f32x32 __attribute__((ext_vector_type(32)));
-        typedef float f32x16_ __attribute__((ext_vector_type(16)));
-        uint32_t top = 0;
-        f32x16_ even, odd;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const uint32_t w = bits[i / 4][i % 4];
-            top = max(top, max(w & 0x7fffu, w >> 16 & 0x7fffu));
-            even[i] = __uint_as_float(w << 16);
-            odd[i] = __uint_as_float(w & 0xffff0000u);
-        }
-        const uint32_t e = (uint32_t)max((int)(top >> 7) - 2, 10);
-        scales = top < 0x7f80u ? e | (e - 4) << 8 | (e - 9) << 16 : ~0u;         // (255: all products are NaN)
-#pragma unroll
-        for (int k = 0; k < 3; ++k) {
-            const float s = __uint_as_float((e - (k == 0 ? 0u : k == 1 ? 4u : 9u)) << 23);
-            piece[k] = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, s);
-            // (the instruction writes before it has read all: its operands stay where they are)
-            asm volatile("" :: "v"(even), "v"(odd), "v"(s), "v"(piece[k]));
-            if (k == 2) break;
-            const f32x32 was = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(piece[k], s);
-            asm volatile("" :: "v"(piece[k]), "v"(s), "v"(was));
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                even[i] -= was[2 * i];
-                odd[i] -= was[2 * i + 1];
-            }
-        }
-    }
-};
-__device__ __forceinline__ i32x8 operand(u32x4 codes) { return i32x8{(int)codes[0], (int)codes[1], (int)codes[2], (int)codes[3], 0, 0, 0, 0}; }
-__device__ __forceinline__ i32x8 operand(u32x6 piece) {
-    return i32x8{(int)piece[0], (int)piece[1], (int)piece[2], (int)piece[3], (int)piece[4], (int)piece[5], 0, 0};
-}
-
 // Which nodes every node of a draft tree sees: itself and its ancestors, a bit each.  By doubling the links, seven times for 128 nodes;
 // a node whose link is wrong is a root.  All threads of the workgroup; barriers at both ends.
 __device__ inline void ancestors(const int32_t *parents, int T, uint32_t (&s_mask)[READER_MAX_T][4], int (&s_up)[READER_MAX_T], int &bad) {

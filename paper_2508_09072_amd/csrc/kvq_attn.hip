@@ -1,5 +1,20 @@
 // Attention over a cache in 4 bits, of packed prompts, chunks and single tokens (causal) and of draft trees whose rows are in the
-// cache behind their sequence (ancestors only).
+// cache behind their sequence (ancestors only): few query rows a kv head here, 128 and more in kvq_attn_wide.hip.
+//
+//   out = sum_j w_j V_j / sum_j w_j,  w_j = 2^(c q.K_j - m),  c = scale * log2(e),  one pass over the keys j that a row sees
+//
+// A value is its code's times a power of two, exact in bf16: codes become operands by one instruction for two of them, and everything
+// behind is an attention in bf16 with 32-bit sums.  A lane's bytes of a page are one load of K and one of V, each wavefront's 1 KB in a
+// piece, straight into registers two steps of 32 keys ahead: nothing is shared between wavefronts before their rows' ends, so there is
+// no barrier in the loop and eight wavefronts can walk the keys of one block side by side.  The reference m is moved only where a
+// lane's sum passes 2^16: a wavefront's exponentials do not wait for maxima.
+//
+// What bounds it: bytes where each kv head has a handful of rows (16 sequences of 1 K to 16 K positions, one token each, 32 and 8 heads of
+// 128: 153 MB in 39 us, 34 of them the first launch at 4.5 TB/s, start and first loads included; the loop runs at 5.6, a copy of 2 GiB at
+// 4.9, the rest is the second launch); the chain page id, page, products, exponentials, sums of wavefronts in small calls (a tree of 16
+// nodes on 512 positions, 8 heads of 64: 7.5 us, the launch 4 of them); exponentials and the making of operands, which every block of
+// rows does anew, in between: the more rows a workgroup has, the fewer times (64 trees of 32 nodes on 6000 positions: 540 us
+// with 16 rows a workgroup, 319 with 32, 292 with 64, 225 with the wide kernel's 128).
 #include <math.h>
 
 #include "kvq_attn.h"
@@ -413,15 +428,15 @@ hipError_t launch_rows(const KvqAttnParams &p, hipStream_t stream) {
 //   128, 256 rows, keys cut into ranges: the same, a range a workgroup; parts beyond four of a block cost the merge.
 // The constants are fitted to 122 shapes (32 query and 8 kv heads of 128, 8 and 8 of 64; 1 to 64 sequences, trees of 8 to 128 nodes,
 // 1 to 1000 tokens, up to 12 K positions).
-// The estimates pick the fastest on 108 of the 122 and are 0.7 % behind it on average, 12.5 % at most.  Some of them, in us (all of
+// The estimates pick the fastest on 107 of the 122 and are 0.6 % behind it on average, 14 % at most.  Some of them, in us (all of
 // them: profiles/kvq_rows_sweep.txt):
 //                                              16  16 few  16 uncut  32 uncut  64 uncut    128    256
-//   one token on 700 positions               15.9    15.6       9.0      11.2      10.4   19.7   20.8
-//   one token on 12 K positions              25.0    20.1      52.1      63.7      79.5   36.9   33.4
-//   16 trees of 32 nodes on 1500             46.3    59.1      56.5      35.0      25.1   50.6   45.9
-//   16 trees of 64 nodes on 6000              256     270       241       158       140    136    119
-//   64 trees of 32 nodes on 6000              615     536       549       319       292    244    374
-//   4 prompts of 1000 tokens                  229     328       216       157       117   89.0   99.0
+//   one token on 700 positions                 16.4    15.7       9.0      11.3      10.5   19.5   21.1
+//   one token on 12 K positions                25.2    20.1      52.5      64.7      80.9   37.7   33.8
+//   16 trees of 32 nodes on 1500               47.8    58.9      56.4      35.3      25.1   49.6   45.3
+//   16 trees of 64 nodes on 6000                263     268       245       159       139    124    114
+//   64 trees of 32 nodes on 6000                683     530       540       323       298    225    383
+//   4 prompts of 1000 tokens                    240     328       218       159       117   92.6   99.2
 // A bound that is loose is taken for the longest sequence.
 int kvq_attn_rows(const KvqAttnParams &p) {
     const int forced = tuning(READER_TUNE_PROMPT_ROWS);

@@ -1,10 +1,20 @@
-// Attention over a cache in 4 bits for many query rows a kv head: trees of many nodes, chunks of prompts.
+// Attention over a cache in 4 bits for many query rows a kv head: trees of many nodes, chunks of prompts (the mathematics: kvq_attn.hip).
 //
-// Bound by the matrix units.  A workgroup takes a range of the (head, sequence, block of rows, key) axis with 4 wavefronts, one per
-// SIMD, of 16 kBlocks rows each.  They share the keys: bytes come into a ring in LDS by asynchronous copies, every wavefront
-// makes a quarter of each step's operands of them (32 keys; two codes an instruction, exact in bf16) and leaves them in LDS as the
-// matrix instructions read them, 1 KB an operand, conflict-free.  The scores of step s + 1 are computed beside the weights of
-// step s, the operands of step s + 2 made beside the second product of step s; one barrier a step.
+// A workgroup takes a range of the (head, sequence, block of rows, key) axis with one or two wavefronts a SIMD, each with 32 query rows or
+// two times 32, through 32 keys a step.  Bytes come into a ring in LDS by asynchronous copies, three steps ahead of their use.  K is
+// multiplied as it is stored (QueryPieces); of V every wavefront makes a share of each step's operands (two codes an instruction, exact in
+// bf16), because a scale belongs to 32 columns of one key and the matrix instructions scale along the keys; they are left in LDS as the
+// products read them, 1 KB an operand, conflict-free.  The scores of step s + 1 are computed beside the weights of step s, V's operands
+// of step s + 3 are made beside the second product of step s; one barrier a step, two steps a turn of the loop (16 copies a step less, 1 %).
+//   128 rows: four wavefronts, two workgroups a compute unit.
+//   256 rows, head dimension 128: eight wavefronts, the second of each SIMD half a step behind the first, so that one has the
+//     matrix unit while the other makes weights (priority to products: 1 to 2 %).  Four wavefronts of twice 32 rows read V half as often
+//     but have nothing to fill the gaps with: 889 instead of 756 us on the same card (64 trees of 64 nodes on 2 K to 8 K positions).
+//   256 rows, head dimension 64: four wavefronts of twice 32 rows (half the operands a row; their scores fill the gaps).
+// What bounds it: exponentials and the other 80 vector instructions of a wavefront's step take 600 cycles, its 14 products 448, and the two
+// wavefronts of a SIMD cover each other's only in part; with calls back to back the clock falls as well.  64 trees of 64 nodes on 2 K to
+// 8 K positions, 64 and 8 heads of 128: 679 to 716 us (0.98 to 1.03 PFLOP/s); 2 chunks of 512 tokens behind 20 K to 28 K: 732 to 763 us
+// (1.04 to 1.08), where a library's product of 8192^3 reaches 1.14.
 #include "kvq_attn.h"
 
 namespace reader {
@@ -23,6 +33,53 @@ struct WideLayout {
     static constexpr int kCodes = kStepPages * 16 * D, kRaw = kCodes + 2 * D;     // codes of two pages, their scales
     static constexpr int kSlots = 6, kDepth = 3;                                  // raw steps in the ring; asked for as many steps before they are used
 };
+
+// 32 values of a query row, as matrix instructions multiply them with codes of 4 bits as they are stored: three pieces of 6 bits (e2m3:
+// sign, up to 7.5, steps of 1/8 below 2, of 1/4 and 1/2 above) with scales of their own, the rounding of each left to the next.  With E =
+// floor(log2 of the largest magnitude) - 2 the pieces count in steps of 2^(E - 3), 2^(E - 7) and 2^(E - 12) at least, so that a value above
+// 1/240 of the largest keeps all bits that bf16 has and no value is off by more than 2^(E - 13), 2^-15 of the largest.  The
+// three products take 3/4 of the time of one with bf16 operands, and K needs no operands made of it (735 us without, 684 with: 64 trees
+// of 64 nodes on 2 K to 8 K positions).  The few rows of kvq_attn.hip gain 2 to 4 % where calls are long and lose up to 10 % to the
+// splitting where they are short: bf16 there.
+typedef uint32_t u32x6 __attribute__((ext_vector_type(6)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+struct QueryPieces {
+    u32x6 piece[3];
+    uint32_t scales;                     // a byte each: exponent + 127
+    __device__ __forceinline__ void make(const u32x4 (&bits)[4]) {
+        typedef float f32x32 __attribute__((ext_vector_type(32)));
+        uint32_t top = 0;
+        f32x16 even, odd;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const uint32_t w = bits[i / 4][i % 4];
+            top = max(top, max(w & 0x7fffu, w >> 16 & 0x7fffu));
+            even[i] = __uint_as_float(w << 16);
+            odd[i] = __uint_as_float(w & 0xffff0000u);
+        }
+        const uint32_t e = (uint32_t)max((int)(top >> 7) - 2, 10);
+        scales = top < 0x7f80u ? e | (e - 4) << 8 | (e - 9) << 16 : ~0u;         // (255: all products are NaN)
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            const float s = __uint_as_float((e - (k == 0 ? 0u : k == 1 ? 4u : 9u)) << 23);
+            piece[k] = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, s);
+            // (the instruction writes before it has read all: its operands stay where they are)
+            asm volatile("" :: "v"(even), "v"(odd), "v"(s), "v"(piece[k]));
+            if (k == 2) break;
+            const f32x32 was = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(piece[k], s);
+            asm volatile("" :: "v"(piece[k]), "v"(s), "v"(was));
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                even[i] -= was[2 * i];
+                odd[i] -= was[2 * i + 1];
+            }
+        }
+    }
+};
+__device__ __forceinline__ i32x8 operand(u32x4 codes) { return i32x8{(int)codes[0], (int)codes[1], (int)codes[2], (int)codes[3], 0, 0, 0, 0}; }
+__device__ __forceinline__ i32x8 operand(u32x6 piece) {
+    return i32x8{(int)piece[0], (int)piece[1], (int)piece[2], (int)piece[3], (int)piece[4], (int)piece[5], 0, 0};
+}
 
 // 32 query rows of a wavefront.  S^T = K.Q^T, 32 keys x 32 rows, leaves lane (half, row) with keys 8 g + 4 half + i in register 4 g + i:
 // as they stand, the operand of O^T += V^T.P^T for the 16 keys of page g / 2, if lane (half, column) of the other one holds the same.

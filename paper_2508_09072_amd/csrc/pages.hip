@@ -15,7 +15,8 @@ __device__ __forceinline__ bool in_pool(int id, int64_t num_pages) { return id >
 __device__ __forceinline__ int pages_of(int positions) { return positions / kPage + (positions % kPage != 0); }
 
 // ---- reorder: two launches, a workgroup per sequence.  The first copies the tables and takes the old entries out of the counts, the
-// second writes the new rows and counts theirs.  A row that stays itself keeps the pages of its positions and their counts.
+// second writes the new rows and counts theirs.  A row that stays itself keeps the pages of its positions and their counts.  512 rows of
+// 1100 entries: 7.5 and 6.8 us, most of it the launch and two dependent trips to memory.
 constexpr int kRowThreads = 256;
 
 // the row that row b becomes (-1: none), and what is wrong with it
@@ -95,8 +96,10 @@ __global__ __launch_bounds__(kSmallThreads) void pages_reorder_small_kernel(Page
 
 // ---- reserve: four launches.  Rows are marked, settled and applied by a wavefront each; in between one workgroup adds up what they ask
 // for and finds the lowest free pages.  (One workgroup for all of that but the copies: 16 sequences the same time, 64 32 us instead
-// of 22, 256 98 instead of 41.)  Counts change in the second and the fourth launch only, and nobody reads one there that
-// another wavefront may be changing: what the first has read of them is kept in the workspace.
+// of 22, 256 98 instead of 41.)  16 sequences: the launches take 4, 2.5, 6 and 4 us, latency; 256 of which 174 copy a page in each of 32
+// layers: 4, 3.7, 6 and 24, the copies at 8 TB/s (read and written; the caches hold a part of what the call before left).  Counts change
+// in the second and the fourth launch only, and nobody reads one there that another wavefront may be changing: what the first has read
+// of them is kept in the workspace.
 constexpr int kBookWaves = 16, kBookThreads = 64 * kBookWaves, kPerWave = 8;      // (words of 64 pages that a wavefront looks over at a time)
 constexpr int kMarkRows = 4;                          // rows of a workgroup
 
