@@ -1,20 +1,22 @@
 // Attention over a cache in 4 bits for many query rows a kv head: trees of many nodes, chunks of prompts (the mathematics: kvq_attn.hip).
 //
 // A workgroup takes a range of the (head, sequence, block of rows, key) axis with one or two wavefronts a SIMD, each with 32 query rows or
-// two times 32, through 32 keys a step.  Bytes come into a ring in LDS by asynchronous copies, three steps ahead of their use.  K is
+// two times 32, through 32 keys a step.  Bytes come into a ring in LDS by asynchronous copies, steps ahead of their use.  K is
 // multiplied as it is stored (QueryPieces); of V every wavefront makes a share of each step's operands (two codes an instruction, exact in
 // bf16), because a scale belongs to 32 columns of one key and the matrix instructions scale along the keys; they are left in LDS as the
 // products read them, 1 KB an operand, conflict-free.  The scores of step s + 1 are computed beside the weights of step s, V's operands
-// of step s + 3 are made beside the second product of step s; one barrier a step, two steps a turn of the loop (16 copies a step less, 1 %).
-//   128 rows: four wavefronts, two workgroups a compute unit.
+// of step s + 3 are made beside the second product of step s; two steps are a turn of the loop (16 copies a step less, 1 %).
+//   128 rows: four wavefronts, two workgroups a compute unit, a barrier a step.
 //   256 rows, head dimension 128: eight wavefronts, the second of each SIMD half a step behind the first, so that one has the
-//     matrix unit while the other makes weights (priority to products: 1 to 2 %).  Four wavefronts of twice 32 rows read V half as often
-//     but have nothing to fill the gaps with: 889 instead of 756 us on the same card (64 trees of 64 nodes on 2 K to 8 K positions).
+//     matrix unit while the other makes weights (priority to products: 1 to 2 %), a barrier every two steps (3 % of long calls).  Four
+//     wavefronts of twice 32 rows read V half as often but have nothing to fill the gaps with: 889 instead of 756 us on the same card
+//     (64 trees of 64 nodes on 2 K to 8 K positions).
 //   256 rows, head dimension 64: four wavefronts of twice 32 rows (half the operands a row; their scores fill the gaps).
 // What bounds it: exponentials and the other 80 vector instructions of a wavefront's step take 600 cycles, its 14 products 448, and the two
-// wavefronts of a SIMD cover each other's only in part; with calls back to back the clock falls as well.  64 trees of 64 nodes on 2 K to
-// 8 K positions, 64 and 8 heads of 128: 679 to 716 us (0.98 to 1.03 PFLOP/s); 2 chunks of 512 tokens behind 20 K to 28 K: 732 to 763 us
-// (1.04 to 1.08), where a library's product of 8192^3 reaches 1.14.
+// wavefronts of a SIMD cover each other's only in part (1900 cycles); and power: the clock is at 2.0 of 2.4 GHz then.  64 trees of 64 nodes
+// on 2 K to 8 K positions, 64 and 8 heads of 128: 675 to 700 us (1.00 to 1.03 PFLOP/s), 5 % of them in front of the five blocks of a
+// workgroup (page ids, queries, first bytes, one after the other; with the queries split behind the asking there are no registers).  2
+// chunks of 512 tokens behind 20 K to 28 K: 715 to 745 us (1.07 to 1.11), where a library's product of 8192^3 reaches 1.14.
 #include "kvq_attn.h"
 
 namespace reader {
@@ -31,7 +33,6 @@ struct WideLayout {
     static constexpr int kFrags = D / 16;                                         // of V in a step
     static constexpr int kStepFrags = kFrags * kFrag;
     static constexpr int kCodes = kStepPages * 16 * D, kRaw = kCodes + 2 * D;     // codes of two pages, their scales
-    static constexpr int kSlots = 6, kDepth = 3;                                  // raw steps in the ring; asked for as many steps before they are used
 };
 
 // 32 values of a query row, as matrix instructions multiply them with codes of 4 bits as they are stored: three pieces of 6 bits (e2m3:
@@ -265,7 +266,7 @@ struct PageWindow {
         }
         if (in == 20 && (c + 1) * 32 < steps) take(c + 1, lane);
     }
-    // page pg of a step at most 8 ahead of step i; whether both pages of it are there
+    // page pg of a step at most 11 ahead of step i; whether both pages of it are there
     __device__ __forceinline__ unsigned id(int step, int i, int pg) const {
         const int from = (step ^ i) & 32 ? then : now;
         return (unsigned)__builtin_amdgcn_readlane(from, (step * 2 + pg) & 63);
@@ -289,11 +290,14 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCo
     // With eight wavefronts, the second of each SIMD is half a step behind the first: its barrier is in front of its second product, not
     // behind it, so that one of them has the matrix unit while the other makes weights.
     constexpr bool kOffset = kWaves == 8, kEarly = kCols == 2 || kOffset;
-    // Between two barriers, of steps n and n + 1: K of step n + 2 is read (by those behind: n + 1), V's operands of step n (n - 1), and those of
-    // step n + 3 are made, while the bytes of steps n + 4 to n + 6 come.
-    constexpr int kVBuffers = kOffset ? 5 : 4;
+    // A barrier stands behind every kTurn steps: behind one step, or with eight wavefronts, which are not at the same place anyway, behind
+    // two.  From one of them to the next, steps n to n + kTurn - 1, V's operands of these steps are read (by those behind from n - 1 on), K from
+    // n + 2 on (n + 1), the operands of kTurn steps from n + 3 on are made, and the bytes of as many have to come that follow those.
+    constexpr int kTurn = kOffset ? 2 : 1;
+    constexpr int kVBuffers = kOffset ? 6 : 4;
+    constexpr int kDepth = kOffset ? 5 : 3, kSlots = kOffset ? 9 : 6;         // bytes are asked for kDepth steps ahead of their use; steps of them in the ring
     __shared__ __attribute__((aligned(1024))) char s_frag[kVBuffers * W::kStepFrags];
-    __shared__ __attribute__((aligned(1024))) char s_raw[W::kSlots * W::kRaw];
+    __shared__ __attribute__((aligned(1024))) char s_raw[kSlots * W::kRaw];
     __shared__ int s_ids[kWaves][2][64];
     __shared__ uint32_t s_mask[kTree ? READER_MAX_T : 1][4];
     __shared__ int s_up[kTree ? READER_MAX_T : 1];
@@ -390,10 +394,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCo
             asm volatile("" ::: "memory");
             ids.take(0, lane);
             ids.now = ids.then; ids.ok_now = ids.ok_then;
-            for (int s = 0; s < W::kDepth + 3; ++s) issue(s, 0, s * W::kRaw);
-            wait_vmcnt<kCopies * (W::kDepth - 1)>();     // steps 0 to 3
+            for (int s = 0; s < kDepth + 3; ++s) issue(s, 0, s * W::kRaw);
+            wait_vmcnt<kCopies * (kDepth - kTurn)>();    // steps 0 to 2 + kTurn
             asm volatile("" ::: "memory");
-            for (int s = 0; s < 4; ++s)
+            for (int s = 0; s < 3 + kTurn; ++s)
                 if (!whole_step(s)) blank(s, 0, s * W::kRaw);
             meet();
             f32x16 x0[kCols], x1[kCols];
@@ -415,7 +419,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCo
                 }
             }
             meet();
-            if (late) issue(3 + W::kDepth, 0, (3 + W::kDepth) % W::kSlots * W::kRaw);      // (... and ask for one)
+            if (late) issue(3 + kDepth, 0, (3 + kDepth) % kSlots * W::kRaw);      // (... and ask for one)
             auto masked = [&](int s) { return s >= min(free, ids.first_bad); };
             bool move = true;                            // (the reference is yet to be found)
             int s = 0;
@@ -424,16 +428,19 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCo
             // K of step s + 2 and the operands of V of step s are read; those of step s + 3 + late are made, of bytes that have come, and
             // bytes are asked for kDepth steps ahead of them.
             auto next = [](unsigned at, unsigned size, unsigned end) { return at + size == end ? 0u : at + size; };
-            constexpr unsigned kVEnd = kVBuffers * W::kStepFrags, kRawEnd = W::kSlots * W::kRaw;
+            constexpr unsigned kVEnd = kVBuffers * W::kStepFrags, kRawEnd = kSlots * W::kRaw;
             const int behind = late ? 1 : 0;
             unsigned k_read = 2 * W::kRaw, v_read = 0, v_make = (3 + behind) % kVBuffers * W::kStepFrags;
-            unsigned raw_make = (3 + behind) % W::kSlots * W::kRaw, raw_ask = (3 + behind + W::kDepth) % W::kSlots * W::kRaw;
-            unsigned raw_new = 4 * W::kRaw;              // of step s + 4
+            unsigned raw_make = (3 + behind) % kSlots * W::kRaw, raw_ask = (3 + behind + kDepth) % kSlots * W::kRaw;
+            unsigned raw_new = (3 + kTurn) * W::kRaw;    // of the steps that come next
             auto barrier = [&] {
-                wait_vmcnt<kCopies * (W::kDepth - 1)>();     // step s + 4 has come
+                if (kTurn == 2 && !(s & 1)) return;
+                wait_vmcnt<kCopies * (kDepth - kTurn)>();    // steps s + 4 to s + 3 + kTurn have come
                 asm volatile("" ::: "memory");
-                if (!whole_step(s + 4)) blank(s + 4, s, raw_new);
-                raw_new = next(raw_new, W::kRaw, kRawEnd);
+                for (int n = s + 4; n < s + 4 + kTurn; ++n) {
+                    if (!whole_step(n)) blank(n, s, raw_new);
+                    raw_new = next(raw_new, W::kRaw, kRawEnd);
+                }
                 meet();
             };
             // One step: the weights of the scores `xa` of step s, the scores `xb` of step s + 1, the products.  true: on with the next one.
@@ -470,7 +477,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCo
                 for (int c = 0; c < kCols; ++c) rows[c].l = sum[c];
                 if (kOffset && late) barrier();
                 __builtin_amdgcn_s_setprio(1);           // (products in front of the other wavefront's weights)
-                issue(s + 3 + behind + W::kDepth, s, raw_ask);
+                issue(s + 3 + behind + kDepth, s, raw_ask);
                 if constexpr (kOffset) read_part(part[0], 0, raw_make);
                 k.read(s_raw + k_read, lane);
                 if constexpr (kOffset) {
