@@ -14,9 +14,9 @@
 //   256 rows, head dimension 64: four wavefronts of twice 32 rows (half the operands a row; their scores fill the gaps).
 // What bounds it: exponentials and the other 80 vector instructions of a wavefront's step take 600 cycles, its 14 products 448, and the two
 // wavefronts of a SIMD cover each other's only in part (1900 cycles); and power: the clock is at 2.0 of 2.4 GHz then.  64 trees of 64 nodes
-// on 2 K to 8 K positions, 64 and 8 heads of 128: 675 to 700 us (1.00 to 1.03 PFLOP/s), 5 % of them in front of the five blocks of a
+// on 2 K to 8 K positions, 64 and 8 heads of 128: 685 to 705 us (0.99 to 1.02 PFLOP/s), 5 % of them in front of the five blocks of a
 // workgroup (page ids, queries, first bytes, one after the other; with the queries split behind the asking there are no registers).  2
-// chunks of 512 tokens behind 20 K to 28 K: 715 to 745 us (1.07 to 1.11), where a library's product of 8192^3 reaches 1.14.
+// chunks of 512 tokens behind 20 K to 28 K: 730 to 747 us (1.06 to 1.09), where a library's product of 8192^3 reaches 1.14.
 #include "kvq_attn.h"
 
 namespace reader {
@@ -38,7 +38,7 @@ struct WideLayout {
 // 32 values of a query row, as matrix instructions multiply them with codes of 4 bits as they are stored: three pieces of 6 bits (e2m3:
 // sign, up to 7.5, steps of 1/8 below 2, of 1/4 and 1/2 above) with scales of their own, the rounding of each left to the next.  With E =
 // floor(log2 of the largest magnitude) - 2 the pieces count in steps of 2^(E - 3), 2^(E - 7) and 2^(E - 12) at least, so that a value above
-// 1/240 of the largest keeps all bits that bf16 has and no value is off by more than 2^(E - 13), 2^-15 of the largest.  The
+// 1/128 of the largest keeps all bits that bf16 has and no value is off by more than 2^(E - 13), 2^-15 of the largest.  The
 // three products take 3/4 of the time of one with bf16 operands, and K needs no operands made of it (735 us without, 684 with: 64 trees
 // of 64 nodes on 2 K to 8 K positions).  The few rows of kvq_attn.hip gain 2 to 4 % where calls are long and lose up to 10 % to the
 // splitting where they are short: bf16 there.

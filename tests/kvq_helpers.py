@@ -123,10 +123,10 @@ def ancestors(parents):
     return sees
 
 
-def attention(q, k, v, sees, scale=None):
+def attention(q, k, v, sees, scale=None, query_step=0.0):
     """q [n, Hq, D], k and v [Hkv, S, D] in 64 bits, sees [n, S]: (out, lse, bound on |out error|, bound on |lse error|).  A score is off
     by D roundings of its products' magnitudes and a few of its own, a weight by that much of itself and by its rounding to bf16,
-    the output by one more."""
+    the output by one more.  query_step: what a query's values may be off by, of the largest of each 32."""
     n, Hq, D = q.shape
     Hkv, S = k.shape[:2]
     G = Hq // Hkv
@@ -139,6 +139,9 @@ def attention(q, k, v, sees, scale=None):
     p = (x - lse[..., None]).exp().masked_fill(~sees, 0.0)
     out, mass = p @ v[:, None], p @ v[:, None].abs()
     score = ((D + 4) * F32 * size.masked_fill(~sees, 0.0) + 8 * F32 * x.masked_fill(~sees, 0.0).abs()).amax(-1)
+    if query_step:
+        most, sums = q.abs().unflatten(-1, (-1, 32)).amax(-1), k.abs().unflatten(-1, (-1, 32)).sum(-1)
+        score = score + query_step * scale * (most @ sums[:, None].transpose(-1, -2)).masked_fill(~sees, 0.0).amax(-1)
     rel = 2 * score + 16 * F32 * (1 + lse.abs()) + S * F32
     bound = BF16 * (out.abs() + mass) * (1 + 2 * BF16) + rel[..., None] * mass
     flat = lambda t: t.permute(2, 0, 1, 3).reshape(n, Hq, D)  # noqa: E731

@@ -359,6 +359,29 @@ def test_scores_far_from_the_first_ones(R, rows, new, L, D, up):
 
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("tree", [False, True])
+def test_queries_of_many_sizes(R, rows, D, tree):
+    """Values that are thousands of times smaller than others of their 32, whole rows that are next to nothing, rows of zeros: a kernel
+    may hold a query to 2^-15 of the largest of its 32."""
+    parents = bushy(torch.Generator().manual_seed(7), 2, 60) if tree else None
+    p = Problem([60, 60], [300, 20], 4, 2, D, seed=26, parents=parents)
+    size = torch.randint(-14, 3, p.q.shape, generator=p.gen) + torch.randint(-1, 2, p.q.shape[:2], generator=p.gen)[..., None]
+    p.q = (p.q * size.float().exp2()).bfloat16()
+    p.q[3] = 0.0
+    p.q[5] *= 2.0 ** -120
+    p.q[7] *= 2.0 ** -100
+    p.q[9, :, 32:] = 0.0
+    p.q[11, :, 1:] *= 2.0 ** -20
+    p.q[65, :, :32] *= 2.0 ** -60
+    out, lse = p.run(R)
+    for b in range(2):
+        mine, S = slice(60 * b, 60 * b + 60), p.L[b] + 60
+        want, s, bo, bs = K.attention(p.q[mine], p.cache.rows(b, S, False), p.cache.rows(b, S, True), p.sees(b), query_step=2.0 ** -15)
+        P.check(out[mine], want, bo, "out")
+        P.check(lse[mine], s, bs, "lse")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("tree", [False, True])
 def test_large_scores(R, rows, D, tree):
     """Queries with one value: the keys with the largest one there share the row, the others are 32 (size 2^12) to millions behind.  The
     products are exact: the weights of a value are equal, rounded to bf16 alike, added up in 32 bits, divided, and the output rounded.  A
