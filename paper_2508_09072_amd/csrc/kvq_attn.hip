@@ -10,8 +10,8 @@
 // lane's sum passes 2^16: a wavefront's exponentials do not wait for maxima.
 //
 // What bounds it: bytes where each kv head has a handful of rows (16 sequences of 1 K to 16 K positions, one token each, 32 and 8 heads of
-// 128: 153 MB in 39 us, 34 of them the first launch at 4.5 TB/s, start and first loads included; the loop runs at 5.6, a copy of 2 GiB at
-// 4.9, the rest is the second launch); the chain page id, page, products, exponentials, sums of wavefronts in small calls (a tree of 16
+// 128: 153 MB in 43 us, in 41 if the last-level cache holds them; 6 to find the work and the first pages, 5 for the second launch, in
+// between at the rate of a copy); the chain page id, page, products, exponentials, sums of wavefronts in small calls (a tree of 16
 // nodes on 512 positions, 8 heads of 64: 7.5 us, the launch 4 of them); exponentials and the making of operands, which every block of
 // rows does anew, in between: the more rows a workgroup has, the fewer times (64 trees of 32 nodes on 6000 positions: 540 us
 // with 16 rows a workgroup, 319 with 32, 292 with 64, 225 with the wide kernel's 128).
@@ -30,11 +30,15 @@ template <int D>
 struct KvqPage {
     static constexpr int kWords = D / 32;
     uint32_t k[kWords], v[kWords], ks, vs;
+    // kOnce: nobody else reads these bytes in this call: past the caches, which they would only fill (16 tokens on 9000 positions each, keys that
+    // no call in front has read: 36.7 us instead of 40.3; 64 on 6000: 75.4 instead of 88.9; where blocks share keys 5 to 8 % slower).
+    template <bool kOnce>
     __device__ __forceinline__ void load(const uint8_t *block, int lane, int i16, int quad) {
         using B = KvqBlock<D>;
         typedef uint32_t words __attribute__((ext_vector_type(kWords)));
-        const words kw = *reinterpret_cast<const words *>(block + lane * (kWords * 4));
-        const words vw = *reinterpret_cast<const words *>(block + B::kV + lane * (kWords * 4));
+        const words *const k_at = reinterpret_cast<const words *>(block + lane * (kWords * 4));
+        const words *const v_at = reinterpret_cast<const words *>(block + B::kV + lane * (kWords * 4));
+        const words kw = kOnce ? __builtin_nontemporal_load(k_at) : *k_at, vw = kOnce ? __builtin_nontemporal_load(v_at) : *v_at;
 #pragma unroll
         for (int w = 0; w < kWords; ++w) { k[w] = kw[w]; v[w] = vw[w]; }
         ks = block[B::kKScales + (D == 128 ? quad : quad >> 1) * 16 + i16];
@@ -188,8 +192,8 @@ struct KvqRows {
 
 // kRowWaves groups of 16 kBlocks rows, each carried by kKeyWaves wavefronts that take the steps of 32 keys in turn.  kCut: a workgroup
 // takes a range of the (head, sequence, block of query rows, key) axis, and blocks that are cut leave records for a second launch;
-// else it takes a block.
-template <int D, int kBlocks, int kRowWaves, int kKeyWaves, bool kTree, bool kCut>
+// else it takes a block.  kOnce: a sequence's keys are read by one block of a kv head.
+template <int D, int kBlocks, int kRowWaves, int kKeyWaves, bool kTree, bool kCut, bool kOnce>
 __global__ __launch_bounds__(64 * kRowWaves * kKeyWaves) void kvq_attn_kernel(KvqAttnParams p) {
     using Rows = KvqRows<D, kBlocks>;
     constexpr int kWaveRows = kBlocks * 16, kRows = kWaveRows * kRowWaves, kWaves = kRowWaves * kKeyWaves;
@@ -246,7 +250,7 @@ __global__ __launch_bounds__(64 * kRowWaves * kKeyWaves) void kvq_attn_kernel(Kv
             auto load = [&](KvqPage<D> (&to)[kStepPages], const int (&id)[kStepPages]) {
 #pragma unroll
                 for (int pg = 0; pg < kStepPages; ++pg)
-                    to[pg].load(p.cache + ((size_t)max(id[pg], 0) * p.Hkv + o.head) * KvqBlock<D>::kBytes, lane, i16, quad);
+                    to[pg].template load<kOnce>(p.cache + ((size_t)max(id[pg], 0) * p.Hkv + o.head) * KvqBlock<D>::kBytes, lane, i16, quad);
             };
             Rows rows;
             rows.load(p, o.head, row0, p0, o.k * tb, nt, first, i16, quad);
@@ -397,8 +401,11 @@ hipError_t launch(KvqAttnParams p, int ranges, hipStream_t stream) {
     p.n_ranges = ranges;
     p.tokens_per_block = kRows / p.G;
     const dim3 grid = kCut ? dim3(ranges) : dim3(block_count(p), p.Hkv), block(64 * kRowWaves * kKeyWaves);
-    if (p.nodes > 0) hipLaunchKernelGGL((kvq_attn_kernel<D, kBlocks, kRowWaves, kKeyWaves, true, kCut>), grid, block, 0, stream, p);
-    else hipLaunchKernelGGL((kvq_attn_kernel<D, kBlocks, kRowWaves, kKeyWaves, false, kCut>), grid, block, 0, stream, p);
+    // single tokens, and as many as a block holds of every sequence (if they have alike)
+    const bool once = kRows == 16 && p.nodes == 0 && p.N <= (long long)p.B * p.tokens_per_block;
+    if (p.nodes > 0) hipLaunchKernelGGL((kvq_attn_kernel<D, kBlocks, kRowWaves, kKeyWaves, true, kCut, false>), grid, block, 0, stream, p);
+    else if (once) hipLaunchKernelGGL((kvq_attn_kernel<D, kBlocks, kRowWaves, kKeyWaves, false, kCut, kRows == 16>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((kvq_attn_kernel<D, kBlocks, kRowWaves, kKeyWaves, false, kCut, false>), grid, block, 0, stream, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return note_hip_error("launch kvq_attn_kernel", e);
     return kCut ? launch_prompt_merge(p, kRows, stream) : e;
