@@ -17,6 +17,8 @@ __device__ __forceinline__ uint32_t two_values(uint32_t word, float scale) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, kByte));
 }
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+// ... in byte e of a word.  (What else the word holds is in the sign and the mantissa: the instruction does not look at them.)
+__device__ __forceinline__ float scale_in(uint32_t word, int e) { return __uint_as_float(e < 3 ? word << (23 - 8 * e) : word >> 1); }
 
 // Which nodes every node of a draft tree sees: itself and its ancestors, a bit each.  By doubling the links, seven times for 128 nodes;
 // a node whose link is wrong is a root.  All threads of the workgroup; barriers at both ends.

@@ -140,7 +140,7 @@ struct KvqRows {
 #pragma unroll
         for (int pg = 0; pg < kStepPages; ++pg)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sc[pg][e] = scale_of((pages[pg].vs >> (8 * e)) & 255u);
+            for (int e = 0; e < 4; ++e) sc[pg][e] = scale_in(pages[pg].vs, e);
         two_columns<0>(pages, sc);
         two_columns<1>(pages, sc);
         if constexpr (D == 128) {

@@ -12,11 +12,11 @@
 //     wavefronts of twice 32 rows read V half as often but have nothing to fill the gaps with: 889 instead of 756 us on the same card
 //     (64 trees of 64 nodes on 2 K to 8 K positions).
 //   256 rows, head dimension 64: four wavefronts of twice 32 rows (half the operands a row; their scores fill the gaps).
-// What bounds it: exponentials and the other 80 vector instructions of a wavefront's step take 600 cycles, its 14 products 448, and the two
+// What bounds it: exponentials and the other 76 vector instructions of a wavefront's step take 560 cycles, its 14 products 448, and the two
 // wavefronts of a SIMD cover each other's only in part (1900 cycles); and power: the clock is at 2.0 of 2.4 GHz then.  64 trees of 64 nodes
-// on 2 K to 8 K positions, 64 and 8 heads of 128: 685 to 705 us (0.99 to 1.02 PFLOP/s), 5 % of them in front of the five blocks of a
+// on 2 K to 8 K positions, 64 and 8 heads of 128: 667 to 715 us (0.98 to 1.05 PFLOP/s), 5 % of them in front of the five blocks of a
 // workgroup (page ids, queries, first bytes, one after the other; with the queries split behind the asking there are no registers).  2
-// chunks of 512 tokens behind 20 K to 28 K: 730 to 747 us (1.06 to 1.09), where a library's product of 8192^3 reaches 1.14.
+// chunks of 512 tokens behind 20 K to 28 K: 709 to 755 us (1.05 to 1.12), where a library's product of 8192^3 reaches 1.14.
 #include "kvq_attn.h"
 
 namespace reader {
@@ -155,16 +155,17 @@ struct WideKeys {
     u32x4 codes[D / 64];
     uint32_t scale[D / 64];
     __device__ __forceinline__ void read(const char *raw, int lane) {
-        const int key = lane & 31, pg = key >> 4, row = key & 15, half = lane >> 5;
-        const char *from = raw + pg * (16 * D) + row * (D / 8), *scales = raw + WideLayout<D>::kCodes + pg * D + row;
+        const int pg = lane >> 4 & 1, row = lane & 15, half = lane >> 5;
+        const char *from = raw + (pg * (16 * D) + row * (D / 8) + half * (D == 128 ? 2 * D : 4 * D));
+        const char *scales = raw + (WideLayout<D>::kCodes + pg * D + row + half * 16);
 #pragma unroll
         for (int t = 0; t < D / 64; ++t) {
-            if constexpr (D == 128) codes[t] = *reinterpret_cast<const u32x4 *>(from + (2 * t + half) * (2 * D));
+            if constexpr (D == 128) codes[t] = *reinterpret_cast<const u32x4 *>(from + t * (4 * D));
             else {
-                const uint2 a = *reinterpret_cast<const uint2 *>(from + 2 * half * (2 * D)), b = *reinterpret_cast<const uint2 *>(from + (2 * half + 1) * (2 * D));
+                const uint2 a = *reinterpret_cast<const uint2 *>(from), b = *reinterpret_cast<const uint2 *>(from + 2 * D);
                 codes[t] = u32x4{a.x, a.y, b.x, b.y};
             }
-            scale[t] = *reinterpret_cast<const uint8_t *>(scales + (2 * t + half) * 16);
+            scale[t] = *reinterpret_cast<const uint8_t *>(scales + t * 32);
         }
     }
 };
@@ -222,7 +223,7 @@ struct Part {
         if (piece < 2) {
 #pragma unroll
             for (int e = 2 * piece; e < 2 * piece + 2; ++e)
-                y[e] = two_values<0>((D == 128 ? v[e] : v[e / 2] >> (e % 2 * 16)) >> (8 * w), scale_of(vs >> (8 * e) & 255u));
+                y[e] = two_values<0>((D == 128 ? v[e] : v[e / 2] >> (e % 2 * 16)) >> (8 * w), scale_in(vs, e));
         } else {
             // (keys 4 quad .. + 3: half quad & 1 of the operand, place quad / 2 of its lanes)
             char *at = v_to + (pg * (D / 32) + w) * W::kFrag + (i16 + 32 * (quad & 1)) * 16 + (quad >> 1) * 8;
