@@ -26,22 +26,21 @@ __device__ inline void ancestors(const int32_t *parents, int T, uint32_t (&s_mas
     int i = threadIdx.x;
     asm("" : "+v"(i));                                   // (nothing here is worth a register outside)
     uint32_t mine[4] = {};
-    int up = -1;
+    int up = i < T ? parents[i] : -1;
     __syncthreads();
     if (i < T) {
-        up = parents[i];
         if (i == 0 ? up != -1 : (up < 0 || up >= i)) { up = -1; bad |= READER_STATUS_BAD_TREE; }
         mine[i >> 5] = 1u << (i & 31);
     }
 #pragma unroll 1
-    for (int turn = 0; turn < 8; ++turn) {
+    for (int reach = 1;; reach *= 2) {                   // (nodes of a path that a mask holds, at most)
         if (i < T) {
 #pragma unroll
             for (int w = 0; w < 4; ++w) s_mask[i][w] = mine[w];
             s_up[i] = up;
         }
         __syncthreads();
-        if (turn == 7) break;
+        if (reach >= T) break;
         if (up >= 0) {
 #pragma unroll
             for (int w = 0; w < 4; ++w) mine[w] |= s_mask[up][w];

@@ -14,9 +14,9 @@
 //   256 rows, head dimension 64: four wavefronts of twice 32 rows (half the operands a row; their scores fill the gaps).
 // What bounds it: exponentials and the other 76 vector instructions of a wavefront's step take 560 cycles, its 14 products 448, and the two
 // wavefronts of a SIMD cover each other's only in part (1900 cycles); and power: the clock is at 2.0 of 2.4 GHz then.  64 trees of 64 nodes
-// on 2 K to 8 K positions, 64 and 8 heads of 128: 667 to 715 us (0.98 to 1.05 PFLOP/s), 5 % of them in front of the five blocks of a
+// on 2 K to 8 K positions, 64 and 8 heads of 128: 652 to 715 us (0.98 to 1.07 PFLOP/s), 5 % of them in front of the five blocks of a
 // workgroup (page ids, queries, first bytes, one after the other; with the queries split behind the asking there are no registers).  2
-// chunks of 512 tokens behind 20 K to 28 K: 709 to 755 us (1.05 to 1.12), where a library's product of 8192^3 reaches 1.14.
+// chunks of 512 tokens behind 20 K to 28 K: 695 to 755 us (1.05 to 1.14), where a library's product of 8192^3 reaches 1.14.
 #include "kvq_attn.h"
 
 namespace reader {
@@ -40,8 +40,8 @@ struct WideLayout {
 // floor(log2 of the largest magnitude) - 2 the pieces count in steps of 2^(E - 3), 2^(E - 7) and 2^(E - 12) at least, so that a value above
 // 1/128 of the largest keeps all bits that bf16 has and no value is off by more than 2^(E - 13), 2^-15 of the largest.  The
 // three products take 3/4 of the time of one with bf16 operands, and K needs no operands made of it (735 us without, 684 with: 64 trees
-// of 64 nodes on 2 K to 8 K positions).  The few rows of kvq_attn.hip gain 2 to 4 % where calls are long and lose up to 10 % to the
-// splitting where they are short: bf16 there.
+// of 64 nodes on 2 K to 8 K positions).  The few rows of kvq_attn.hip would gain 1 to 10 % where calls are long and lose 0.5 to
+// 1 us to the splitting where they are short: bf16 there.
 typedef uint32_t u32x6 __attribute__((ext_vector_type(6)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 struct QueryPieces {
