@@ -16,8 +16,9 @@ __device__ __forceinline__ int pages_of(int positions) { return positions / kPag
 
 // ---- reorder: two launches, a workgroup per sequence.  The first copies the tables and takes the old entries out of the counts, the
 // second writes the new rows and counts theirs.  A row that stays itself keeps the pages of its positions and their counts.  512 rows of
-// 1100 entries: 7.5 and 6.8 us, most of it the launch and two dependent trips to memory.
-constexpr int kRowThreads = 256;
+// 1100 entries: 6.9 and 5.6 us, most of it the launch and two dependent trips to memory (with 256 threads a row 0.8 us more each: another
+// trip; 1024 are slower where rows are short, 4096 of 20 entries 22 us instead of 17, restoring copies included).
+constexpr int kRowThreads = 512;
 
 // the row that row b becomes (-1: none), and what is wrong with it
 __device__ __forceinline__ int source_of(const PagesParams &p, int b, int &bad) {
