@@ -153,6 +153,91 @@ __device__ __forceinline__ bool find_range(const KvqAttnParams &p, const Sequenc
     return true;
 }
 
+// Rows of a segment whose products have passed the largest number of 32 bits, though their mean does not: a lane's weights go up to
+// kMostSum and are divided by their sum at the end, so that values from about 2^107 on can.  Such a row is gone through again over keys
+// [j0, j1) by one wavefront as a running mean, which no value is larger than: 64 keys at a time, a lane each, then D / 64 columns a lane.
+// Row numbers of the block, marked with `turn` in `odd`; the wavefronts share them out.  rec: where the block's part is left, record_rows wide,
+// or null: the rows are written to `out`, behind what is written there already (a barrier in front).
+template <int D, bool kTree, class Block>
+__device__ __forceinline__ void rows_as_means(const KvqAttnParams &p, const Block &o, int rows, const int *odd, int turn, int wave, int waves, int j0, int j1,
+                                              const uint32_t (*s_mask)[4], float *rec, int record_rows, int lane) {
+    using B = KvqBlock<D>;
+    constexpr int kPer = D / 64;
+    asm("" : "+v"(lane));                                // (nothing here is worth a register outside)
+    const int tb = p.tokens_per_block, d = lane * kPer;
+    const int32_t *table = p.page_table + (size_t)o.b * p.max_pages;
+#pragma unroll 1
+    for (int row = wave; row < rows; row += waves) {
+        if (odd[row] != turn) continue;
+        const int tok = row / p.G, g = row - tok * p.G, node = o.k * tb + tok;
+        const size_t at = ((size_t)(o.c0 + node)) * p.Hq + (size_t)o.head * p.G + g;
+        const uint16_t *q = p.q + at * D;
+        const int end = (int)min(min((long long)o.L + node + 1, (long long)p.max_seq_len), (long long)j1);
+        float m = -INFINITY, l = 0.f, mean[kPer] = {};
+#pragma unroll 1
+        for (int base = j0; base < end; base += 64) {
+            const int j = base + lane, n = j - o.L;
+            const int id = j < end ? table[j / READER_PAGE_SIZE] : -1;
+            bool sees = id >= 0 && id < p.num_pages;
+            if constexpr (kTree) sees = sees && (n < 0 || (s_mask[node][(n >> 5) & 3] >> (n & 31) & 1u) != 0);
+            const size_t block = ((size_t)(sees ? id : 0) * p.Hkv + o.head) * B::kBytes;
+            const int s = j & (READER_PAGE_SIZE - 1);
+            float x = -INFINITY;
+            if (sees) {
+                float dot = 0.f;
+#pragma unroll 1
+                for (int c = 0; c < D; c += 8) {
+                    const uint32_t codes = *reinterpret_cast<const uint32_t *>(p.cache + block + B::k_code(s, c));
+                    const float scale = scale_of(p.cache[block + B::k_scale(s, c / 32)]);
+                    const u32x4 k = {two_values<0>(codes, scale), two_values<1>(codes, scale), two_values<2>(codes, scale), two_values<3>(codes, scale)}, w = ld16(q + c);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        dot += __uint_as_float(k[i] << 16) * __uint_as_float(w[i] << 16);
+                        dot += __uint_as_float(k[i] & 0xffff0000u) * __uint_as_float(w[i] & 0xffff0000u);
+                    }
+                }
+                x = dot * p.scale_log2;
+            }
+            float top = x;
+#pragma unroll
+            for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+            top = fmaxf(top, m);
+            const float keep = l == 0.f ? 0.f : l * __builtin_amdgcn_exp2f(m - top);
+            const float w = sees && x > -INFINITY ? __builtin_amdgcn_exp2f(x - top) : 0.f;
+            float sum = w;
+#pragma unroll
+            for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off);
+            if (sum == 0.f) continue;
+            l = keep + sum;
+            m = top;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) mean[e] *= keep / l;
+            const float part = w / l;
+            for (unsigned long long todo = __ballot(w > 0.f); todo; todo &= todo - 1) {
+                const int k = (int)__builtin_ctzll(todo), ks = (base + k) & (READER_PAGE_SIZE - 1);
+                const float wk = __shfl(part, k);
+                const uint8_t *v_block = p.cache + __shfl((unsigned long long)block, k);
+                const uint32_t v = two_values<0>(v_block[B::v_code(ks, d & ~1)], scale_of(v_block[B::v_scale(ks, d / 32)]));
+                if constexpr (kPer == 2) {
+                    mean[0] += wk * __uint_as_float(v << 16);
+                    mean[1] += wk * __uint_as_float(v & 0xffff0000u);
+                } else mean[0] += wk * __uint_as_float(d & 1 ? v & 0xffff0000u : v << 16);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+            if (rec) rec[((size_t)((d + e) / 4) * record_rows + row) * 4 + (d + e) % 4] = mean[e];
+            else p.out[at * D + d + e] = (uint16_t)pack_bf16x2(mean[e], 0.f);
+        }
+        if (lane == 0) {
+            if (rec) {
+                rec[(size_t)record_rows * D + row] = m;
+                rec[(size_t)record_rows * (D + 1) + row] = l;
+            } else if (p.lse) p.lse[lse_at(p, o.b, o.c0 + o.k * tb, o.k * tb, tok, o.head * p.G + g)] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+        }
+    }
+}
+
 }  // namespace
 
 }  // namespace reader

@@ -198,18 +198,19 @@ __global__ __launch_bounds__(64 * kRowWaves * kKeyWaves) void kvq_attn_kernel(Kv
     using Rows = KvqRows<D, kBlocks>;
     constexpr int kWaveRows = kBlocks * 16, kRows = kWaveRows * kRowWaves, kWaves = kRowWaves * kKeyWaves;
     constexpr int kMinRange = 8 * kStep;
-    constexpr bool kMeet = kKeyWaves > 1;
-    __shared__ __attribute__((aligned(16))) f32x4 s_part[kMeet ? kWaves : 1][kMeet ? kWaveRows * D / 4 : 1];
+    __shared__ __attribute__((aligned(16))) f32x4 s_part[kWaves][kWaveRows * D / 4];
     __shared__ float s_sum[kWaves][2][kWaveRows];
     __shared__ uint32_t s_mask[kTree ? READER_MAX_T : 1][4];
     __shared__ int s_up[kTree ? READER_MAX_T : 1];
+    __shared__ int s_odd[kRows + 1];                     // in which turn a row, and any, was none that 32 bits hold
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row_wave = wave / kKeyWaves, key_wave = wave % kKeyWaves;
     const int i16 = lane & 15, quad = lane >> 4, tb = p.tokens_per_block;
     RangeNote *const notes = reinterpret_cast<RangeNote *>(p.workspace);
     const Sequences seqs{p.seq_lens, p.cu_tokens, p.N, p.max_seq_len, kTree ? p.nodes : 0};
     const int range = blockIdx.x;
-    int bad = 0;
+    int bad = 0, turn = 0;
+    for (int i = threadIdx.x; i <= kRows; i += 64 * kWaves) s_odd[i] = 0;
     Block o;
     PromptRange<Block> rg;
     if constexpr (kCut) {
@@ -231,6 +232,7 @@ __global__ __launch_bounds__(64 * kRowWaves * kKeyWaves) void kvq_attn_kernel(Kv
         const long long p0 = (long long)o.L + o.k * tb;
         const bool last_block = !kCut || rg.is_stop(o);
         if (t1 > t0) {
+            ++turn;
             if constexpr (kTree) {
                 if ((long long)t1 * kStep > o.L) ancestors(p.parents + (size_t)o.b * p.nodes, p.nodes, s_mask, s_up, bad);
             }
@@ -334,50 +336,50 @@ __global__ __launch_bounds__(64 * kRowWaves * kKeyWaves) void kvq_attn_kernel(Kv
                     p.lse[lse_at(p, o.b, row0, o.k * tb, tok, o.head * p.G + row - tok * p.G)] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
                 }
             };
-            if constexpr (!kMeet) {
+            // the wavefronts that share rows add them up: [D / 4 pieces][rows], a part of the pieces each
 #pragma unroll
-                for (int r = 0; r < kBlocks; ++r) {
-                    const float inv = rows.l[r] == 0.f ? 0.f : 1.f / rows.l[r];
+            for (int r = 0; r < kBlocks; ++r) {
 #pragma unroll
-                    for (int n = 0; n < kPieces; ++n) write(r, Rows::piece_at(n, quad), rows.piece(r, n) * inv);
-                    if (quad == 0) write_sums(r, rows.m[r], rows.l[r]);
+                for (int n = 0; n < kPieces; ++n) s_part[wave][Rows::piece_at(n, quad) * kWaveRows + r * 16 + i16] = rows.piece(r, n);
+                if (quad == 0) { s_sum[wave][0][r * 16 + i16] = rows.m[r]; s_sum[wave][1][r * 16 + i16] = rows.l[r]; }
+            }
+            __syncthreads();
+#pragma unroll
+            for (int r = 0; r < kBlocks; ++r) {
+                const int row = r * 16 + i16, w0 = row_wave * kKeyWaves;
+                float top = kNoReference, sum = 0.f, f[kKeyWaves];
+#pragma unroll
+                for (int w = 0; w < kKeyWaves; ++w) top = fmaxf(top, s_sum[w0 + w][0][row]);
+#pragma unroll
+                for (int w = 0; w < kKeyWaves; ++w) {
+                    // (a wavefront whose rows saw nothing has no say, whatever its reference)
+                    const float lw = s_sum[w0 + w][1][row];
+                    f[w] = lw == 0.f ? 0.f : __builtin_amdgcn_exp2f(s_sum[w0 + w][0][row] - top);
+                    sum += lw * f[w];
                 }
-            } else {
-                // the wavefronts that share rows add them up: [D / 4 pieces][rows], a part of the pieces each
+                const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                float check = 0.f;                       // (not a number once any value is none)
+                constexpr int kMine = (D / 4 + 4 * kKeyWaves - 1) / (4 * kKeyWaves);
 #pragma unroll
-                for (int r = 0; r < kBlocks; ++r) {
+                for (int c = 0; c < kMine; ++c) {
+                    const int piece = (key_wave * kMine + c) * 4 + quad;
+                    if (D / 4 % (4 * kKeyWaves) != 0 && piece >= D / 4) break;
+                    f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int n = 0; n < kPieces; ++n) s_part[wave][Rows::piece_at(n, quad) * kWaveRows + r * 16 + i16] = rows.piece(r, n);
-                    if (quad == 0) { s_sum[wave][0][r * 16 + i16] = rows.m[r]; s_sum[wave][1][r * 16 + i16] = rows.l[r]; }
+                    for (int w = 0; w < kKeyWaves; ++w) v += s_part[w0 + w][piece * kWaveRows + row] * f[w];
+                    v *= inv;
+                    check = no_number(no_number(check, v[0], v[1]), v[2], v[3]);
+                    write(r, piece, v);
                 }
+                // (a sum that is none is a query's doing)
+                if (rows.real[r] && check != 0.f && sum < INFINITY) s_odd[first + row] = s_odd[kRows] = turn;
+                if (key_wave == 0 && quad == 0) write_sums(r, top, sum);
+            }
+            __syncthreads();                             // everybody is done with the others' rows
+            if (__builtin_expect(s_odd[kRows] == turn, 0)) {
+                wait_vmcnt<0>();
                 __syncthreads();
-#pragma unroll
-                for (int r = 0; r < kBlocks; ++r) {
-                    const int row = r * 16 + i16, w0 = row_wave * kKeyWaves;
-                    float top = kNoReference, sum = 0.f, f[kKeyWaves];
-#pragma unroll
-                    for (int w = 0; w < kKeyWaves; ++w) top = fmaxf(top, s_sum[w0 + w][0][row]);
-#pragma unroll
-                    for (int w = 0; w < kKeyWaves; ++w) {
-                        // (a wavefront whose rows saw nothing has no say, whatever its reference)
-                        const float lw = s_sum[w0 + w][1][row];
-                        f[w] = lw == 0.f ? 0.f : __builtin_amdgcn_exp2f(s_sum[w0 + w][0][row] - top);
-                        sum += lw * f[w];
-                    }
-                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-                    constexpr int kMine = (D / 4 + 4 * kKeyWaves - 1) / (4 * kKeyWaves);
-#pragma unroll
-                    for (int c = 0; c < kMine; ++c) {
-                        const int piece = (key_wave * kMine + c) * 4 + quad;
-                        if (D / 4 % (4 * kKeyWaves) != 0 && piece >= D / 4) break;
-                        f32x4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                        for (int w = 0; w < kKeyWaves; ++w) v += s_part[w0 + w][piece * kWaveRows + row] * f[w];
-                        write(r, piece, v * inv);
-                    }
-                    if (key_wave == 0 && quad == 0) write_sums(r, top, sum);
-                }
-                __syncthreads();                             // everybody is done with the others' rows
+                rows_as_means<D, kTree>(p, o, nt * p.G, s_odd, turn, wave, kWaves, t0 * kStep, min(t1 * kStep, keys), s_mask, whole ? nullptr : rec, kRows, lane);
             }
         }
         if (last_block) break;

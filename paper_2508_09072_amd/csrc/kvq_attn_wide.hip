@@ -302,6 +302,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCo
     __shared__ int s_ids[kWaves][2][64];
     __shared__ uint32_t s_mask[kTree ? READER_MAX_T : 1][4];
     __shared__ int s_up[kTree ? READER_MAX_T : 1];
+    __shared__ int s_odd[kRows + 1];                     // in which turn a row, and any, was none that 32 bits hold
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i16 = lane & 15, quad = lane >> 4, half = lane >> 5, tb = p.tokens_per_block;
     const Sequences seqs{p.seq_lens, p.cu_tokens, p.N, p.max_seq_len, kTree ? p.nodes : 0};
@@ -312,7 +313,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCo
     const PromptRange<WideBlock> rg(place, t_place, p.Hkv);
     const RangeNote note = rg.note(seqs, p.B, tb, lane);
     if (threadIdx.x == 0) reinterpret_cast<RangeNote *>(p.workspace)[range] = note;
-    int bad = 0;
+    int bad = 0, turn = 0;
+    for (int i = threadIdx.x; i <= kRows; i += 64 * kWaves) s_odd[i] = 0;
     const unsigned raw_lds = (unsigned)(size_t)(lds_char *)&s_raw[0];
     // what this wavefront copies of a step: the first four 1 KB of codes each, the others the scales of a page; with four, both
     const int code_page = D == 128 ? (wave >> 1) & 1 : wave & 1, code_part = D == 128 ? wave & 1 : 0;
@@ -332,6 +334,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCo
         const long long p0 = (long long)o.L + o.k * tb;
         const bool last_block = rg.is_stop(o);
         if (t1 > t0) {
+            ++turn;
             if constexpr (kTree) {
                 if ((long long)t1 * kStep > o.L) ancestors(p.parents + (size_t)o.b * p.nodes, p.nodes, s_mask, s_up, bad);
             }
@@ -549,6 +552,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCo
                     most_now = INFINITY;
                 }
                 bool on;
+                // (the loop's first products start in front of a line of 64 bytes or well inside one: across its end, long calls take 3 % more)
+                asm volatile(".p2align 6");
                 do {
                     on = step(x0, x1);
                     if (move) break;
@@ -560,6 +565,23 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCo
 #pragma unroll
                     for (int c = 0; c < kCols; ++c) x0[c] = x1[c];
                 } while (on);
+            }
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) {
+                float check[2] = {0.f, 0.f};             // (not a number once any value is none)
+#pragma unroll
+                for (int b = 0; b < Rows::kOut; ++b)
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) {
+                        check[0] = no_number(check[0], rows[c].acc[b][e], rows[c].acc[b][e + 1]);
+                        check[1] = no_number(check[1], rows[c].acc[b][e + 2], rows[c].acc[b][e + 3]);
+                    }
+                // (a sum that is none is a query's doing)
+                if (check[0] + check[1] != 0.f && rows[c].l < INFINITY) {
+                    int r = row + c * kWaveRows;
+                    asm volatile("" : "+v"(r));
+                    if (Rows::token(p, r) < nt) s_odd[r] = s_odd[kRows] = turn;
+                }
             }
             wait_vmcnt<0>();                             // copies that nobody needed
             asm volatile("" ::: "memory");
@@ -598,6 +620,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kCo
                         p.lse[lse_at(p, o.b, row0, o.k * tb, tok, o.head * p.G + r - tok * p.G)] = sum == 0.f ? -INFINITY : (rows[c].m + __builtin_amdgcn_logf(sum)) * kLn2;
                     }
                 }
+            }
+            if (__builtin_expect(s_odd[kRows] == turn, 0)) {
+                wait_vmcnt<0>();
+                asm volatile("" ::: "memory");
+                meet();
+                rows_as_means<D, kTree>(p, o, nt * p.G, s_odd, turn, wave, kWaves, t0 * kStep, min(t1 * kStep, keys), s_mask, whole ? nullptr : rec, kRows, lane);
             }
         }
         if (last_block) break;

@@ -7,6 +7,9 @@ namespace reader {
 
 // Rows of a packed batch: sequence b owns rows cu_tokens[b] .. cu_tokens[b + 1] - 1 of N.  Bounds outside [0, N] count as the
 // nearest one inside, so nothing in a table leads an access out of the tensors.
+// `check`, which is zero, or no number once a or b is none.
+__device__ __forceinline__ float no_number(float check, float a, float b) { return fmaf(b, 0.f, fmaf(a, 0.f, check)); }
+
 __device__ inline int clamp_row(int row, int N) { return row < 0 ? 0 : (row > N ? N : row); }
 
 // Sequence that owns row t, found by a whole wavefront together: 64 bounds are compared at a time.  first: its first row.  B: nobody's.

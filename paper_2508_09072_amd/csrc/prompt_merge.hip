@@ -106,11 +106,14 @@ __global__ __launch_bounds__(64 * kMergeWaves) void prompt_merge_kernel(PromptPa
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const size_t out_row = ((size_t)mine.row0 + tok) * p.Hq + (size_t)mine.head * p.G + g;
     uint16_t *out = p.out + out_row * D + quad * kChunks * 4;
+    auto write = [&](const float4 (&v)[kChunks], float f) {
 #pragma unroll
-    for (int c = 0; c < kChunks; c += 2)
-        *reinterpret_cast<uint4 *>(out + c * 4) =
-            make_uint4(pack_bf16x2(acc[c].x * inv, acc[c].y * inv), pack_bf16x2(acc[c].z * inv, acc[c].w * inv),
-                       pack_bf16x2(acc[c + 1].x * inv, acc[c + 1].y * inv), pack_bf16x2(acc[c + 1].z * inv, acc[c + 1].w * inv));
+        for (int c = 0; c < kChunks; c += 2)
+            *reinterpret_cast<uint4 *>(out + c * 4) =
+                make_uint4(pack_bf16x2(v[c].x * f, v[c].y * f), pack_bf16x2(v[c].z * f, v[c].w * f),
+                           pack_bf16x2(v[c + 1].x * f, v[c + 1].y * f), pack_bf16x2(v[c + 1].z * f, v[c + 1].w * f));
+    };
+    write(acc, inv);
     if (quad == 0 && p.lse) {
         size_t at = out_row;
         if (p.nodes > 0) {
@@ -119,6 +122,29 @@ __global__ __launch_bounds__(64 * kMergeWaves) void prompt_merge_kernel(PromptPa
         }
         p.lse[at] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
     }
+    // Outputs that pass the largest number of 32 bits before they are divided by the sum, of parts that do not: from the parts again, each
+    // divided by it.  (A part with a value that is no number leaves them as they are.)
+    float check = 0.f;
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) check = no_number(no_number(check, acc[c].x, acc[c].y), acc[c].z, acc[c].w);
+    const bool odd = check != 0.f && l < INFINITY;
+    if (__builtin_expect(!__any(odd), 1)) return;
+    float4 mean[kChunks] = {};
+    check = 0.f;
+#pragma unroll 1
+    for (int w = range; w < p.n_ranges; ++w) {
+        if (notes[w].tiles <= 0) continue;
+        Part of;
+        load(w, of);
+        const float f = of.l == 0.f ? 0.f : of.l * __builtin_amdgcn_exp2f(of.m - m) * inv;
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+            check = no_number(no_number(check, of.v[c].x, of.v[c].y), of.v[c].z, of.v[c].w);
+            mean[c].x += of.v[c].x * f; mean[c].y += of.v[c].y * f; mean[c].z += of.v[c].z * f; mean[c].w += of.v[c].w * f;
+        }
+        if (w > range && notes[w].ends) break;
+    }
+    if (odd && check == 0.f) write(mean, 1.f);
 }
 
 }  // namespace
