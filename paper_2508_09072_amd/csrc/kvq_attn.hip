@@ -391,7 +391,7 @@ __global__ __launch_bounds__(64 * kRowWaves * kKeyWaves) void kvq_attn_kernel(Kv
     if (p.status && bad) atomicOr(p.status, bad);
 }
 
-// Blocks of a kv head, at most: every sequence has one that is not full.
+// Blocks of a kv head, at most, whatever the bounds are: every sequence has one that is not full, and no row is in two (find_block).
 int block_count(const KvqAttnParams &p) {
     if (p.nodes > 0) return p.B * ((p.nodes + p.tokens_per_block - 1) / p.tokens_per_block);
     return (int)min((long long)p.N, (long long)p.N / p.tokens_per_block + p.B);
