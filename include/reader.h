@@ -760,7 +760,7 @@ int reader_kv_evict(const reader_dims *dims, int32_t num_layers, int32_t keep, i
  * belongs to one sequence (reader_pages_reserve).
  * The attention takes up to 2^30 positions a sequence.  Scores are held in 32 bits: a row whose scores times log2(e) reach 2^30 in
  * magnitude, or whose query holds a NaN or an infinity, is unspecified; other rows are not.  Where there are many query rows, values
- * 32 g .. 32 g + 31 of a query are held to 2^-15 of the largest of them (exactly above 1/128 of it).
+ * 32 g .. 32 g + 31 of a query are held to 2^-15 of the largest of them (exactly above 1/128 of it), or to 2^-130 where that is more.
  */
 #define READER_KVQ_BLOCK_BYTES(D) (17 * (D))
 

@@ -38,7 +38,8 @@ struct WideLayout {
 // 32 values of a query row, as matrix instructions multiply them with codes of 4 bits as they are stored: three pieces of 6 bits (e2m3:
 // sign, up to 7.5, steps of 1/8 below 2, of 1/4 and 1/2 above) with scales of their own, the rounding of each left to the next.  With E =
 // floor(log2 of the largest magnitude) - 2 the pieces count in steps of 2^(E - 3), 2^(E - 7) and 2^(E - 12) at least, so that a value above
-// 1/128 of the largest keeps all bits that bf16 has and no value is off by more than 2^(E - 13), 2^-15 of the largest.  The
+// 1/128 of the largest keeps all bits that bf16 has and no value is off by more than 2^(E - 13), 2^-15 of the largest.  E is -117 at least,
+// so that the third scale's exponent is one that there is: below, no value is off by more than 2^-130.  The
 // three products take 3/4 of the time of one with bf16 operands, and K needs no operands made of it (735 us without, 684 with: 64 trees
 // of 64 nodes on 2 K to 8 K positions).  The few rows of kvq_attn.hip would gain 1 to 10 % where calls are long and lose 0.5 to
 // 1 us to the splitting where they are short: bf16 there.

@@ -123,10 +123,10 @@ def ancestors(parents):
     return sees
 
 
-def attention(q, k, v, sees, scale=None, query_step=0.0):
+def attention(q, k, v, sees, scale=None, query_step=0.0, query_floor=0.0):
     """q [n, Hq, D], k and v [Hkv, S, D] in 64 bits, sees [n, S]: (out, lse, bound on |out error|, bound on |lse error|).  A score is off
     by D roundings of its products' magnitudes and a few of its own, a weight by that much of itself and by its rounding to bf16,
-    the output by one more.  query_step: what a query's values may be off by, of the largest of each 32."""
+    the output by one more.  query_step: what a query's values may be off by, of the largest of each 32; query_floor: by whatever it is."""
     n, Hq, D = q.shape
     Hkv, S = k.shape[:2]
     G = Hq // Hkv
@@ -142,6 +142,8 @@ def attention(q, k, v, sees, scale=None, query_step=0.0):
     if query_step:
         most, sums = q.abs().unflatten(-1, (-1, 32)).amax(-1), k.abs().unflatten(-1, (-1, 32)).sum(-1)
         score = score + query_step * scale * (most @ sums[:, None].transpose(-1, -2)).masked_fill(~sees, 0.0).amax(-1)
+    if query_floor:
+        score = score + query_floor * scale * k.abs().sum(-1)[:, None, None].expand_as(x).masked_fill(~sees, 0.0).amax(-1)
     rel = 2 * score + 16 * F32 * (1 + lse.abs()) + S * F32
     bound = BF16 * (out.abs() + mass) * (1 + 2 * BF16) + rel[..., None] * mass
     flat = lambda t: t.permute(2, 0, 1, 3).reshape(n, Hq, D)  # noqa: E731

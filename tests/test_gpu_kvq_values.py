@@ -78,3 +78,24 @@ def test_the_largest_values_under_large_scores(R, rows, D, new, L):  # noqa: F81
             bound = P.BF16 * (want.abs() + mass) * (1 + 2 * P.BF16) + (8 + S) * P.F32 * mass
             flat = lambda t: t.permute(2, 0, 1, 3).reshape(new[b], 4, D)  # noqa: E731
             P.check(out[mine], flat(want), flat(bound), "out")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("tree", [False, True])
+def test_small_queries_on_the_largest_keys(R, rows, D, tree):  # noqa: F811
+    """Queries down to the smallest numbers, under keys so large that their scores matter.  Where a kernel holds queries in pieces, a value is
+    off by 2^-15 of the largest of its 32, or by 2^-130.  (The bounds are of first order in the error x of a weight, twice a score's, which is
+    below 0.3 in them: exp(x) - 1 < 1.2 x.)"""
+    p = shapes([60, 60], [300, 20], tree, D)
+    usual = p.q.clone()
+    pieces = rows in (0, 128, 256)
+    step, floor = (2.0 ** -15, 2.0 ** -130) if pieces else (0.0, 0.0)
+    for key, size in ((240, -113), (247, -120), (249, -121), (249, -125)) if pieces else ((240, -113), (249, -121), (HIGHEST, -124), (HIGHEST, -127)):
+        p.cache.data[..., torch.cat([K.scale_bytes(D, s, False) for s in range(16)])] = key
+        p.q = (usual.double() * 2.0 ** size).bfloat16()
+        out, lse = p.run(R)
+        for b in range(2):
+            mine, S = slice(60 * b, 60 * b + 60), p.L[b] + 60
+            o, s, bo, bs = K.attention(p.q[mine], p.cache.rows(b, S, False), p.cache.rows(b, S, True), p.sees(b), query_step=step, query_floor=floor)
+            P.check(out[mine], o, 1.2 * bo, "out of sequence %d, queries of 2^%d" % (b, size))
+            P.check(lse[mine], s, 1.2 * bs, "lse of sequence %d, queries of 2^%d" % (b, size))
