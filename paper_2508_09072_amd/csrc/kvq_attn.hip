@@ -12,9 +12,9 @@
 // What bounds it: bytes where each kv head has a handful of rows (16 sequences of 1 K to 16 K positions, one token each, 32 and 8 heads of
 // 128: 153 MB in 43 us, in 41 if the last-level cache holds them; 6 to find the work and the first pages, 5 for the second launch, in
 // between at the rate of a copy); the chain page id, page, products, exponentials, sums of wavefronts in small calls (a tree of 16
-// nodes on 512 positions, 8 heads of 64: 7.5 us, the launch 4 of them); exponentials and the making of operands, which every block of
+// nodes on 512 positions, 8 heads of 64: 7.3 us, the launch 4 of them); exponentials and the making of operands, which every block of
 // rows does anew, in between: the more rows a workgroup has, the fewer times (64 trees of 32 nodes on 6000 positions: 540 us
-// with 16 rows a workgroup, 319 with 32, 292 with 64, 225 with the wide kernel's 128).
+// with 16 rows a workgroup, 329 with 32, 303 with 64, 225 with the wide kernel's 128).
 #include <math.h>
 
 #include "kvq_attn.h"
@@ -435,17 +435,17 @@ hipError_t launch_rows(const KvqAttnParams &p, hipStream_t stream) {
 //   16 rows, keys cut into ranges: start and merge, steps that all compute units share out evenly, blocks' ends; 256 ranges of eight
 //     wavefronts where no compute unit has a second block (a step's loads are out sooner, half the records), else 512 of four;
 //   128, 256 rows, keys cut into ranges: the same, a range a workgroup; parts beyond four of a block cost the merge.
-// The constants are fitted to 122 shapes (32 query and 8 kv heads of 128, 8 and 8 of 64; 1 to 64 sequences, trees of 8 to 128 nodes,
-// 1 to 1000 tokens, up to 12 K positions).
-// The estimates pick the fastest on 107 of the 122 and are 0.6 % behind it on average, 14 % at most.  Some of them, in us (all of
-// them: profiles/kvq_rows_sweep.txt):
+// The constants were fitted to 122 shapes (32 query and 8 kv heads of 128, 8 and 8 of 64; 1 to 64 sequences of one length, trees of 8 to
+// 128 nodes, 1 to 1000 tokens, up to 12 K positions); other groups of heads and mixed batches go by the same estimates, unmeasured.  They pick
+// the fastest on 109 of the 122 and are 0.7 % behind it on average, 12 % at most (16 prompts of 300 tokens, 64 trees of 128 nodes on 300
+// positions).  Some of them, in us (all of them: profiles/kvq_rows_sweep.txt):
 //                                              16  16 few  16 uncut  32 uncut  64 uncut    128    256
-//   one token on 700 positions                 16.4    15.7       9.0      11.3      10.5   19.5   21.1
-//   one token on 12 K positions                25.2    20.1      52.5      64.7      80.9   37.7   33.8
-//   16 trees of 32 nodes on 1500               47.8    58.9      56.4      35.3      25.1   49.6   45.3
-//   16 trees of 64 nodes on 6000                263     268       245       159       139    124    114
-//   64 trees of 32 nodes on 6000                683     530       540       323       298    225    383
-//   4 prompts of 1000 tokens                    240     328       218       159       117   92.6   99.2
+//   one token on 700 positions                 16.5    15.9       8.7      11.2      10.6   19.7   21.4
+//   one token on 12 K positions                25.8    20.8      52.9      63.6      79.3   38.0   33.7
+//   16 trees of 32 nodes on 1500               48.2    60.0      56.0      35.0      25.0   50.1   45.7
+//   16 trees of 64 nodes on 6000                265     270       244       159       142    129    117
+//   64 trees of 32 nodes on 6000                651     540       529       329       303    225    358
+//   4 prompts of 1000 tokens                    244     337       219       157       117   93.5    101
 // A bound that is loose is taken for the longest sequence.
 int kvq_attn_rows(const KvqAttnParams &p) {
     const int forced = tuning(READER_TUNE_PROMPT_ROWS);

@@ -14,9 +14,12 @@
 //   256 rows, head dimension 64: four wavefronts of twice 32 rows (half the operands a row; their scores fill the gaps).
 // What bounds it: exponentials and the other 76 vector instructions of a wavefront's step take 560 cycles, its 14 products 448, and the two
 // wavefronts of a SIMD cover each other's only in part (1900 cycles); and power: the clock is at 2.0 of 2.4 GHz then.  64 trees of 64 nodes
-// on 2 K to 8 K positions, 64 and 8 heads of 128: 652 to 715 us (0.98 to 1.07 PFLOP/s), 5 % of them in front of the five blocks of a
+// on 2 K to 8 K positions, 64 and 8 heads of 128: 652 to 720 us (0.97 to 1.07 PFLOP/s), 5 % of them in front of the five blocks of a
 // workgroup (page ids, queries, first bytes, one after the other; with the queries split behind the asking there are no registers).  2
-// chunks of 512 tokens behind 20 K to 28 K: 695 to 755 us (1.05 to 1.14), where a library's product of 8192^3 reaches 1.14.
+// chunks of 512 tokens behind 20 K to 28 K: 695 to 760 us (1.04 to 1.14), where a library's product of 8192^3 reaches 1.14.  Blocks of few
+// steps are far from that (16 prompts of 1000 tokens from an empty cache 280 us, their products alone 115): what stands in front of a
+// block's first step and behind its last takes 8 to 9 us, nothing of the next block is asked for meanwhile, and masked steps leave the
+// pairs of steps.
 #include "kvq_attn.h"
 
 namespace reader {

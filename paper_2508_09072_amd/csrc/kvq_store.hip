@@ -166,7 +166,8 @@ __device__ inline void check_path(const KvqCompactParams &p, int b, PathShared &
 
 // One workgroup per (sequence, layer).  A row's bytes are moved in the pieces that lie together: D / 8 words of K, 16 pieces of V of
 // D / 32 bytes, single scales.  Node ids increase along a path, so no row is written before it has been read: rows go in their
-// order, a pass reads its pieces before it writes any.  Bound by the chain of loads (path, table, rows): one user's path of 6, 8 heads of
+// order, a pass reads its pieces before it writes any.  (Of 128 values, a row has four pieces of 16 bytes of K, moved as words, 16 of
+// 4 of V and 8 bytes of scales, in 7 of the block's 17 lines of 128 bytes.)  Bound by the chain of loads (path, table, rows): one user's path of 6, 8 heads of
 // 64, 5.6 us.  With many layers by the lines that the scattered pieces touch: 32 layers of 64 paths of 8, 8 heads of 128, move 15 MB in
 // 22 us and touch 105, 4.8 TB/s; the lengths' launch behind it takes 4.
 template <int D>

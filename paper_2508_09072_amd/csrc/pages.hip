@@ -96,8 +96,8 @@ __global__ __launch_bounds__(kSmallThreads) void pages_reorder_small_kernel(Page
 }
 
 // ---- reserve: four launches.  Rows are marked, settled and applied by a wavefront each; in between one workgroup adds up what they ask
-// for and finds the lowest free pages.  (One workgroup for all of that but the copies: 16 sequences the same time, 64 32 us instead
-// of 22, 256 98 instead of 41.)  16 sequences: the launches take 4, 2.5, 6 and 4 us, latency; 256 of which 174 copy a page in each of 32
+// for and finds the lowest free pages.  (One workgroup for all of that but the copies, restoring copies included: 16 sequences 18 us
+// instead of 20.5, 64 32 instead of 22, 256 98 instead of 41; there is no form of it for a few sequences.)  16 sequences: the launches take 4, 2.5, 6 and 4 us, latency; 256 of which 174 copy a page in each of 32
 // layers: 4, 3.7, 6 and 24, the copies at 8 TB/s (read and written; the caches hold a part of what the call before left).  Counts change
 // in the second and the fourth launch only, and nobody reads one there that another wavefront may be changing: what the first has read
 // of them is kept in the workspace.
