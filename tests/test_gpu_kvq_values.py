@@ -1,5 +1,7 @@
 """Attention over the cache in 4 bits at the ends of what it holds: values of V whose weighted sums pass the largest number of 32 bits
 where their mean does not, keys with the largest scales under queries that are next to nothing."""
+import functools
+
 import pytest
 import torch
 
@@ -16,27 +18,15 @@ def shapes(n, L, tree, D):
     return Problem(n, L, 4, 2, D, seed=27, parents=parents)
 
 
-def check(p, out, lse):
-    """Problem.check, with what numbers below the smallest normal one lose besides: bf16's are 2^-133 apart, so that the rounding of an
-    output is off by 2^-134 whatever its size, and each of the S products and sums of 32 bits by 2^-150, the weights' sum being at least
-    one of them of weight one."""
-    for b in range(p.B):
-        n, S, mine = p.new[b], p.L[b] + p.new[b], slice(p.cu[b], p.cu[b] + p.new[b])
-        o, s, bo, bs = K.attention(p.q[mine], p.cache.rows(b, S, False), p.cache.rows(b, S, True), p.sees(b))
-        P.check(out[mine], o, bo + 2.0 ** -134 + 2 * S * 2.0 ** -150, "out of sequence %d" % b)
-        P.check(lse[mine], s, bs, "lse of sequence %d" % b)
+SHAPES = {"short": ([3], [60], False), "single tokens": ([1, 1], [9000, 40], False), "long": ([200, 2], [900, 3000], False), "trees": ([40, 40], [700, 3], True)}
 
 
-SHORT, SINGLE, LONG, TREES = ([3], [60], False), ([1, 1], [9000, 40], False), ([200, 2], [900, 3000], False), ([40, 40], [700, 3], True)
-
-
-@pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("where,shape", [("everywhere", SHORT), ("everywhere", SINGLE), ("everywhere", LONG), ("everywhere", TREES), ("some columns", SINGLE),
-                                         ("some columns", TREES), ("some keys", LONG), ("some keys", TREES), ("behind a low reference", LONG),
-                                         ("behind a low reference", TREES)])
-def test_the_largest_values(R, rows, D, where, shape):  # noqa: F811
-    """No mean of values is larger than all of them; a sum of them is infinite from the second on."""
-    new, L, tree = shape
+@functools.lru_cache(maxsize=None)
+def largest(D, where, shape):
+    """The problem and, for each sequence, what it comes to (once for all kernels).  To the bounds of K.attention comes what numbers below
+    the smallest normal one lose: bf16's are 2^-133 apart, so that the rounding of an output is off by 2^-134 whatever its size, and each
+    of the S products and sums of 32 bits by 2^-150, the weights' sum being at least one of them of weight one."""
+    new, L, tree = SHAPES[shape]
     p = shapes(new, L, tree, D)
     pages = p.cache.data
     at = torch.cat([K.scale_bytes(D, s, True) for s in range(16)])
@@ -53,7 +43,25 @@ def test_the_largest_values(R, rows, D, where, shape):  # noqa: F811
             S = new[b] + L[b]
             for j, (page, slot) in enumerate(p.cache.place(b, S)):
                 pages[page][:, K.scale_bytes(D, slot, False)] = 122 + 5 * j // S
-    check(p, *p.run(R))
+    want = []
+    for b in range(p.B):
+        S, mine = p.L[b] + p.new[b], slice(p.cu[b], p.cu[b] + p.new[b])
+        o, lse, bo, bs = K.attention(p.q[mine], p.cache.rows(b, S, False), p.cache.rows(b, S, True), p.sees(b))
+        want.append((mine, o, bo + 2.0 ** -134 + 2 * S * 2.0 ** -150, lse, bs))
+    return p, want
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("where,shape", [("everywhere", "short"), ("everywhere", "single tokens"), ("everywhere", "long"), ("everywhere", "trees"),
+                                         ("some columns", "single tokens"), ("some columns", "trees"), ("some keys", "long"), ("some keys", "trees"),
+                                         ("behind a low reference", "long"), ("behind a low reference", "trees")])
+def test_the_largest_values(R, rows, D, where, shape):  # noqa: F811
+    """No mean of values is larger than all of them; a sum of them is infinite from the second on."""
+    p, want = largest(D, where, shape)
+    out, lse = p.run(R)
+    for b, (mine, o, bo, s, bs) in enumerate(want):
+        P.check(out[mine], o, bo, "out of sequence %d" % b)
+        P.check(lse[mine], s, bs, "lse of sequence %d" % b)
 
 
 @pytest.mark.parametrize("D", [64, 128])
